@@ -58,7 +58,8 @@ typedef enum sf_status {
 #define SF_ST_NEGATIVE 1u /* some duration (or wall time) was negative */
 #define SF_ST_RANGE 2u    /* some duration, rank total or wall time was >= 2^47 */
 #define SF_ST_TIMEOUT 4u  /* a bounded device-side wait gave up; outputs incomplete */
-#define SF_ST_INDEX 8u    /* an index input (a rank's group id) was out of range; that rank was skipped */
+#define SF_ST_INDEX 8u    /* an index input (a rank's group id, a token, an expert) was out of range; it was skipped */
+#define SF_ST_NONFINITE 16u /* training-step operators: a value that has to be finite was not */
 
 /* Label bits (Sec. 4 Tab. core labels, App. B, App. C).  RAW_ONLY marks a
    window whose denominator is below the floor: raw advances, no shares. */
@@ -437,6 +438,163 @@ sf_status sf_label_windows_noalloc(const int64_t* d, int64_t T, int64_t R, int64
                                    uint32_t* route_mask, uint32_t* amb_mask, double* share,
                                    double* gain, int64_t* X, int64_t* Y, int64_t* D,
                                    uint32_t* status, cudaStream_t stream);
+
+/*
+ * Training-step operators.  The monitor runs inside the job whose stages it
+ * times; these entry points compute, in that job's own step, what a report
+ * sets beside a stage's exposed time: the experts' loads (why one rank's
+ * forward stage leads the frontier), the loss with its clip share and KL
+ * term, and the gradient norm with the clipping that follows it.  The general
+ * conventions above hold (caller's device memory and stream, no allocation,
+ * no synchronization, host errors before anything is enqueued), except:
+ *   - Empty calls are valid: N = 0 rows, T = 0 tokens, n = 0 tensors.
+ *   - Data may start at any element's alignment; 16-byte aligned rows are
+ *     read and written faster.
+ *   - The outputs are defined when SF_ST_INDEX or SF_ST_NONFINITE is set: each
+ *     entry point says what was left out.
+ *   - Sums are held in 32 bits or more and added in a fixed order: the same
+ *     call on the same device gives the same bits.
+ */
+typedef enum sf_dtype { SF_F32 = 0, SF_BF16 = 1, SF_F16 = 2 } sf_dtype;
+
+typedef struct sf_policy_config {
+  float clip_low, clip_high; /* the ratio's bounds are 1 - clip_low and 1 + clip_high; 0 <= clip_low <= 1 */
+  float kl_coef;             /* beta >= 0 */
+  float inv_temperature;     /* tau > 0: the policy is softmax(tau * logits) */
+} sf_policy_config;
+
+/*
+ * sf_policy_loss - the clipped policy loss with a KL term, from the logits,
+ * and its gradient.  For row (token) n with logits z, chosen token y, weight
+ * w != 0 and upstream gradient g:
+ *   lp   = tau z_y - log sum_j exp(tau z_j)
+ *   r    = exp(lp - old),  held = clamp(r, 1 - clip_low, 1 + clip_high)
+ *   pg   = -min(r A, held A);  the row is clipped if held A < r A
+ *   kl   = exp(ref - lp) - (ref - lp) - 1       (0 without ref_logp)
+ *   loss = pg + beta kl
+ *   dz_j = g w tau c ([j = y] - exp(tau z_j - log sum)),
+ *          c = (clipped ? 0 : -r A) + beta (1 - exp(ref - lp))
+ * A row of weight 0 is not read: its log-probability, loss and gradient are 0.
+ * A logit of -inf is a token that is ruled out: probability and gradient 0.
+ *   logits    [N] rows of V, `ld` elements apart (ld >= V), of type dtype
+ *   target    [N] int64, the chosen tokens
+ *   old_logp, advantage [N] f32;  ref_logp [N] f32 (nullable: no KL term)
+ *   weight    [N] f32 (nullable: 1/N each)
+ *   grad_out  f32 (device, nullable: 1), the upstream gradient g of the loss
+ *   logp      [N] f32 (nullable), lp;  token_loss [N] f32 (nullable), loss
+ *   stats     [4] f32: the sums over rows of w times loss, pg, kl, clipped
+ *   dlogits   [N] rows of V, ldd elements apart, of type dtype (nullable: no
+ *             gradient); may be `logits` itself with ldd = ld, else the two
+ *             must not overlap.  Rounded once, to nearest even.
+ *   workspace device, 16-byte aligned, sf_policy_loss_workspace_size(N, V) bytes
+ * A row whose token is not in [0, V) is left out like one of weight 0, with
+ * SF_ST_INDEX; so is one whose loss, weight or derivative is not finite (a
+ * NaN or +inf logit, no logit above -inf), with SF_ST_NONFINITE.
+ * N < 2^31, 1 <= V < 2^31.
+ */
+sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V, int64_t ld, const int64_t* target,
+                         const float* old_logp, const float* ref_logp, const float* advantage, const float* weight,
+                         const sf_policy_config* cfg, const float* grad_out, float* logp, float* token_loss,
+                         float* stats, void* dlogits, int64_t ldd, void* workspace, size_t workspace_bytes,
+                         uint32_t* status, cudaStream_t stream);
+
+/* Workspace bytes sf_policy_loss needs; 0 on bad arguments and for N = 0. */
+size_t sf_policy_loss_workspace_size(int64_t N, int64_t V);
+
+#define SF_SCORE_SOFTMAX 0
+#define SF_SCORE_SIGMOID 1
+
+typedef struct sf_route_config {
+  int32_t k;          /* experts a token is sent to, 1 <= k <= 32 */
+  int32_t score;      /* SF_SCORE_SOFTMAX or SF_SCORE_SIGMOID */
+  int32_t groups;     /* the E experts are `groups` runs of E / groups, 1 <= groups <= 32 */
+  int32_t top_groups; /* groups a token may use, k <= top_groups * E / groups */
+  int32_t group_top;  /* a group's value is the sum of its 1 or 2 largest choice values */
+  int32_t renorm;     /* 1: the weights of a token's experts sum to `scale` */
+  float scale;        /* finite */
+} sf_route_config;
+
+/*
+ * sf_route_experts - the router of a layer of experts.  For token t with
+ * logits z over E experts:
+ *   choice value  u_e = z_e + bias_e (softmax) or 1 / (1 + exp(-z_e)) + bias_e
+ *                 (sigmoid): the bias balances the loads and enters nothing else
+ *   group value   the sum of the group_top largest u in the group
+ *   chosen        the k largest u among the experts of the top_groups groups of
+ *                 largest value; equal values go to the lower group or expert
+ *   weight        softmax: scale exp(z_e) / sum exp(z_j), j over the chosen
+ *                 (renorm) or over all experts; sigmoid: scale s_e / sum s_j over
+ *                 the chosen (renorm; 0 where that sum is 0) or scale s_e
+ * u is computed in 32 bits exactly as written, each operation rounded to
+ * nearest.  An expert whose logit or bias is -inf is not available: it is
+ * never chosen and a group without any has no value.  Where fewer than k
+ * experts are available the last slots hold index -1, weight 0 and count for
+ * no expert.  An expert whose choice value is NaN, or +inf logit under softmax,
+ * is taken as not available, with SF_ST_NONFINITE.
+ *   logits [T] rows of E, ld elements apart;  bias [E] f32 (nullable: 0)
+ *   index  [T][k] int32, weight [T][k] f32, by falling choice value
+ *   load   [E] int32 (nullable): tokens sent to each expert; accumulate 1 adds
+ *          to its contents (the micro-batches of a step), 0 overwrites them
+ * T < 2^31, 1 <= E <= 1024.
+ */
+sf_status sf_route_experts(const void* logits, int32_t dtype, int64_t T, int64_t E, int64_t ld, const float* bias,
+                           const sf_route_config* cfg, int32_t* index, float* weight, int32_t* load,
+                           int32_t accumulate, uint32_t* status, cudaStream_t stream);
+
+/*
+ * sf_route_experts_grad - the gradient of the router's logits from that of the
+ * weights; the choice itself and the bias have none.  With S the sum that
+ * `weight` above divides by, s the scores, q_e = exp(z_e) / S, dw the upstream
+ * gradient and j over the chosen:
+ *   sigmoid  renorm   dz_e = scale s_e (1 - s_e) / S (dw_e - sum_j dw_j s_j / S)
+ *            else     dz_e = scale s_e (1 - s_e) dw_e
+ *   softmax           dz_e = scale q_e (dw_e [e chosen] - sum_j q_j dw_j)
+ * and 0 for experts that are not chosen, but for softmax without renorm.
+ *   index   [T][k] as sf_route_experts wrote it (distinct within a token)
+ *   dweight [T][k] f32;  dlogits [T] rows of E, ldd elements apart, of type
+ *   dtype, rounded once; must not overlap logits
+ * cfg's groups, top_groups and group_top are not used.  A slot whose index is
+ * -1 is empty; any other index outside [0, E) is skipped with SF_ST_INDEX.
+ * Where S is 0, or (softmax) not finite, the row's gradient is 0; the latter
+ * sets SF_ST_NONFINITE.
+ */
+sf_status sf_route_experts_grad(const void* logits, int32_t dtype, int64_t T, int64_t E, int64_t ld,
+                                const int32_t* index, const float* dweight, const sf_route_config* cfg,
+                                void* dlogits, int64_t ldd, uint32_t* status, cudaStream_t stream);
+
+/*
+ * sf_grad_norm - the 2-norm over n gradient tensors and of each of them.
+ *   data, numel, dtype  HOST arrays of n: each tensor's device pointer (aligned
+ *               to its element; unused where numel is 0), element count and
+ *               sf_dtype.  Read before the call returns.
+ *   norm        [1] f32: sqrt(sum of squares over all tensors)
+ *   tensor_norm [n] f32 (nullable): each tensor's own
+ *   workspace   device, 16-byte aligned, sf_grad_workspace_size(...) bytes
+ * Squares that leave the range of 32 bits are summed in 64.  Where the norm is
+ * not finite (or above the largest f32) SF_ST_NONFINITE is set and `norm`
+ * holds what it is; tensor_norm tells which tensors are the cause.
+ * n <= 2^20, each numel < 2^40.
+ */
+sf_status sf_grad_norm(const void* const* data, const int64_t* numel, const int32_t* dtype, int64_t n, float* norm,
+                       float* tensor_norm, void* workspace, size_t workspace_bytes, uint32_t* status,
+                       cudaStream_t stream);
+
+/*
+ * sf_grad_clip - sf_grad_norm, then every gradient times
+ *   coef = min(1, max_norm / (norm + eps)),
+ * rounded once.  out: HOST array of n device pointers, each tensor's result
+ * (same type and count, not overlapping any input other than its own), or
+ * null: in place, where nothing is written for coef = 1.  Where the norm is not finite
+ * coef is NaN and the gradients are passed on unscaled, so that the caller can
+ * skip the step.  max_norm > 0, eps >= 0; coef [1] f32 (device, nullable).
+ */
+sf_status sf_grad_clip(const void* const* data, void* const* out, const int64_t* numel, const int32_t* dtype,
+                       int64_t n, float max_norm, float eps, float* norm, float* coef, float* tensor_norm,
+                       void* workspace, size_t workspace_bytes, uint32_t* status, cudaStream_t stream);
+
+/* Workspace bytes sf_grad_norm and sf_grad_clip need for these tensors on the
+   current device; 0 on bad arguments. */
+size_t sf_grad_workspace_size(const int64_t* numel, int64_t n);
 
 #ifdef __cplusplus
 }

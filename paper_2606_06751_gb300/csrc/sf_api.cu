@@ -1,9 +1,11 @@
 // sf_api.cu - the C ABI of libstagefrontier (declared in stagefrontier.h):
 // argument validation, output clearing, workspace carving and launch
 // sequencing.  Every computation happens in the kernels (sf_stream.cu,
-// sf_select.cu, sf_rank.cu, sf_group.cu, sf_ingest.cu); this file performs no
-// arithmetic on the data.
+// sf_select.cu, sf_rank.cu, sf_group.cu, sf_ingest.cu; for the training-step
+// operators sf_policy_loss.cu, sf_route.cu, sf_grad_norm.cu); this file
+// performs no arithmetic on the data.
 #include <atomic>
+#include <cmath>
 #include <cstring>
 
 #include "sf_device.cuh"
@@ -35,6 +37,26 @@ bool config_ok(const sf_label_config* c) {
 }
 
 sf_status cuda_status(cudaError_t e) { return e == cudaSuccess ? SF_OK : SF_ECUDA; }
+
+bool dtype_ok(int32_t t) { return t == SF_F32 || t == SF_BF16 || t == SF_F16; }
+size_t dtype_size(int32_t t) { return t == SF_F32 ? 4 : 2; }
+
+// Rows of `len` elements, `ld` apart: sizes that fit 64 bits.
+bool rows_ok(int64_t rows, int64_t len, int64_t ld) {
+  return rows >= 0 && rows < (int64_t(1) << 31) && len >= 1 && len < (int64_t(1) << 31) && ld >= len &&
+         ld <= (int64_t(1) << 60) / (rows > 0 ? rows : 1);
+}
+
+// Whether the rows at a and at b share memory (rows of `len` elements, lda and ldb apart).
+bool rows_overlap(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t rows, int64_t len, size_t size) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  const uintptr_t xn = size_t((rows - 1) * lda + len) * size, yn = size_t((rows - 1) * ldb + len) * size;
+  if (x + xn <= y || y + yn <= x) return false;
+  if (lda != ldb) return true;
+  // equal spacing: column slices of one buffer interleave without sharing an element
+  const uintptr_t step = size_t(lda) * size, off = (x > y ? x - y : y - x) % step, n = size_t(len) * size;
+  return off < n || step - off < n;
+}
 
 size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
 
@@ -446,6 +468,59 @@ sf_status sf_label_windows(const int64_t* d, int64_t T, int64_t R, int64_t S, in
   if (st != SF_OK) return st;
   return sf_label_gates(T, R, S, W, Xw, Yw, Dw, sl, (wall || other_stage >= 0) ? q : nullptr, role, missing,
                         cfg, labels, route_mask, amb_mask, share, gain, nullptr, nullptr, stream);
+}
+
+size_t sf_policy_loss_workspace_size(int64_t N, int64_t V) {
+  if (!rows_ok(N, V, V) || N == 0) return 0;
+  return policy_loss_workspace(N);
+}
+
+sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V, int64_t ld, const int64_t* target,
+                         const float* old_logp, const float* ref_logp, const float* advantage, const float* weight,
+                         const sf_policy_config* cfg, const float* grad_out, float* logp, float* token_loss,
+                         float* stats, void* dlogits, int64_t ldd, void* workspace, size_t workspace_bytes,
+                         uint32_t* status, cudaStream_t stream) {
+  if (!dtype_ok(dtype) || !rows_ok(N, V, ld) || (dlogits && !rows_ok(N, V, ldd)) || !stats || !cfg) return SF_EINVAL;
+  if (N > 0 && (!logits || !target || !old_logp || !advantage)) return SF_EINVAL;
+  if (!(cfg->clip_low >= 0.f && cfg->clip_low <= 1.f && cfg->clip_high >= 0.f && std::isfinite(cfg->clip_high) &&
+        cfg->kl_coef >= 0.f && std::isfinite(cfg->kl_coef) && cfg->inv_temperature > 0.f &&
+        std::isfinite(cfg->inv_temperature)))
+    return SF_EINVAL;
+  if (!aligned(logits, dtype_size(dtype)) || !aligned(dlogits, dtype_size(dtype)) || !aligned(target, 8) ||
+      !aligned(old_logp, 4) || !aligned(ref_logp, 4) || !aligned(advantage, 4) || !aligned(weight, 4) ||
+      !aligned(grad_out, 4) || !aligned(logp, 4) || !aligned(token_loss, 4) || !aligned(stats, 4) ||
+      !aligned(status, 4))
+    return SF_EINVAL_ALIGN;
+  if (N == 0) {
+    ZeroList z;
+    z.add(stats, 4 * sizeof(float));
+    return cuda_status(launch_zero_many(z, stream));
+  }
+  if (dlogits && !(dlogits == logits && ldd == ld) &&
+      rows_overlap(logits, ld, dlogits, ldd, N, V, dtype_size(dtype)))
+    return SF_EINVAL;
+  if (!workspace || workspace_bytes < policy_loss_workspace(N)) return SF_EWORKSPACE;
+  if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
+  PolicyJob j;
+  j.logits = logits;
+  j.dtype = dtype;
+  j.N = N;
+  j.V = V;
+  j.ld = ld;
+  j.target = target;
+  j.old_logp = old_logp;
+  j.ref_logp = ref_logp;
+  j.advantage = advantage;
+  j.weight = weight;
+  j.cfg = *cfg;
+  j.grad_out = grad_out;
+  j.logp = logp;
+  j.token_loss = token_loss;
+  j.stats = stats;
+  j.dlogits = dlogits;
+  j.ldd = ldd;
+  j.status = status;
+  return cuda_status(launch_policy_loss(j, workspace, stream));
 }
 
 }  // extern "C"

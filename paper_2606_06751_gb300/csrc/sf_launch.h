@@ -120,4 +120,25 @@ struct GateJob {
 };
 cudaError_t launch_gates(const GateJob& job, cudaStream_t stream);
 
+// ---- training-step operators
+
+struct PolicyJob {
+  const void* logits;
+  int32_t dtype;
+  int64_t N, V, ld;
+  const int64_t* target;
+  const float *old_logp, *ref_logp, *advantage, *weight;
+  sf_policy_config cfg;
+  const float* grad_out;
+  float *logp, *token_loss, *stats;
+  void* dlogits;
+  int64_t ldd;
+  uint32_t* status;
+  // set by launch_policy_loss
+  float4* terms = nullptr;  // [N] weighted terms of the sums
+  float mean = 0.f;         // the weight without a weight array
+};
+size_t policy_loss_workspace(int64_t N);
+cudaError_t launch_policy_loss(PolicyJob job, void* workspace, cudaStream_t stream);
+
 }  // namespace sf

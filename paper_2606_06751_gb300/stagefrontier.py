@@ -21,6 +21,9 @@ LIB_PATH = os.path.join(_PKG, "libstagefrontier.so")
 
 SF_OK, SF_EINVAL, SF_EINVAL_ALIGN, SF_EUNSUPPORTED, SF_ECUDA, SF_EWORKSPACE = 0, -1, -2, -3, -4, -5
 SF_ST_NEGATIVE, SF_ST_RANGE, SF_ST_TIMEOUT, SF_ST_INDEX = 1, 2, 4, 8
+SF_ST_NONFINITE = 16
+SF_F32, SF_BF16, SF_F16 = 0, 1, 2
+SF_SCORE_SOFTMAX, SF_SCORE_SIGMOID = 0, 1
 SF_STEP_CONFIDENT = 0x80
 LABEL_NAMES = ("frontier_accounting", "direct_exposure", "sync_wait_dependent", "co_critical",
                "role_aware_needed", "telemetry_limited", "raw_only")
@@ -41,6 +44,10 @@ class LabelConfig(ctypes.Structure):
                                      "gamma_switch", "gamma_elig", "closure_max", "overlap_max")] + \
                [("denom_floor_ns", ctypes.c_int64), ("max_missing_ranks", ctypes.c_int32),
                 ("model_fit_mask", ctypes.c_uint32)]
+
+
+class PolicyConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "kl_coef", "inv_temperature")]
 
 
 def _load():
@@ -73,6 +80,8 @@ def _load():
         "sf_stream_gathered_windows": [P, I, I, I, I, I32, I, ctypes.POINTER(LabelConfig), P, ctypes.c_size_t, P,
                                        ctypes.c_size_t, P, P, P, P, P, P, P, P, P, P, P, P, P, P, S, S],
         "sf_gathered_to_steps": [P, I, I, I, I, P, S],
+        "sf_policy_loss": [P, I32, I, I, I, P, P, P, P, P, ctypes.POINTER(PolicyConfig), P, P, P, P, P, I, P,
+                           ctypes.c_size_t, P, S],
     }
     for name, argt in sigs.items():
         f = getattr(L, name)
@@ -92,6 +101,8 @@ def _load():
     L.sf_label_windows_workspace_size.restype = ctypes.c_size_t
     L.sf_rank_workspace_size.argtypes = [I, I, I]
     L.sf_rank_workspace_size.restype = ctypes.c_size_t
+    L.sf_policy_loss_workspace_size.argtypes = [I, I]
+    L.sf_policy_loss_workspace_size.restype = ctypes.c_size_t
     for name in ("sf_stream_windows_staging_size", "sf_stream_gathered_staging_size"):
         getattr(L, name).argtypes = [I, I, I, I]
         getattr(L, name).restype = ctypes.c_size_t
@@ -557,3 +568,83 @@ def sf_rank_lag_windows(d, W: int, t0: int = 0, Lw=None, Gw=None, accumulate: bo
     _check(_lib.sf_rank_lag_windows(_p(d), T, R, S, t0, W, _p(Lw), _p(Gw), 1 if accumulate else 0, _p(ws),
                                     ws.numel(), _p(status), _stream(stream)), "sf_rank_lag_windows")
     return Lw, Gw
+
+
+# ---------------------------------------------------------------- training-step operators
+
+_DTYPES = {torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16}
+
+
+def _rows(t: torch.Tensor, name: str):
+    """(rows, columns, row stride) of a CUDA matrix whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or t.dim() != 2:
+        raise TypeError(f"{name} must be a CUDA matrix of float32, bfloat16 or float16")
+    n, m = t.shape
+    if m > 1 and t.stride(1) != 1:
+        raise TypeError(f"{name} must have contiguous rows")
+    return n, m, (t.stride(0) if n > 1 else m)
+
+
+def _vec(t: Optional[torch.Tensor], n: int, dtype, name: str):
+    if t is not None:
+        _dev(t, dtype, name)
+        if t.numel() != n:
+            raise ValueError(f"{name} must have {n} elements")
+    return t
+
+
+@dataclass
+class PolicyLoss:
+    logp: Optional[torch.Tensor]
+    token_loss: Optional[torch.Tensor]
+    stats: torch.Tensor
+    dlogits: Optional[torch.Tensor]
+
+
+def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=None, clip=(0.2, 0.2),
+                   kl_coef: float = 0.0, inv_temperature: float = 1.0, grad: bool = False, grad_out=None, logp=None,
+                   token_loss=None, stats=None, dlogits=None, want=("logp", "token_loss"), workspace=None,
+                   status=None, stream=None) -> PolicyLoss:
+    """Clipped policy loss with a KL term of N tokens from their logits [N][V];
+    `stats` holds the weighted sums (loss, policy term, KL, clipped share).
+    With `grad` (or a `dlogits` to write, which may be `logits` itself) also
+    the gradient of the logits for the upstream gradient `grad_out` (a device
+    scalar, 1 if absent).  Tokens of weight 0 are not read."""
+    N, V, ld = _rows(logits, "logits")
+    _vec(target, N, torch.int64, "target")
+    _vec(old_logp, N, torch.float32, "old_logp")
+    _vec(advantage, N, torch.float32, "advantage")
+    _vec(ref_logp, N, torch.float32, "ref_logp")
+    _vec(weight, N, torch.float32, "weight")
+    _vec(grad_out, 1, torch.float32, "grad_out")
+    made = []
+    if logp is None and "logp" in want:
+        logp = _empty((N,), torch.float32, logits)
+        made.append(logp)
+    if token_loss is None and "token_loss" in want:
+        token_loss = _empty((N,), torch.float32, logits)
+        made.append(token_loss)
+    if stats is None:
+        stats = _empty((4,), torch.float32, logits)
+        made.append(stats)
+    if dlogits is None and grad:
+        dlogits = _empty((N, V), logits.dtype, logits)
+        made.append(dlogits)
+    _vec(logp, N, torch.float32, "logp")
+    _vec(token_loss, N, torch.float32, "token_loss")
+    _vec(stats, 4, torch.float32, "stats")
+    ldd = V
+    if dlogits is not None:
+        n, m, ldd = _rows(dlogits, "dlogits")
+        if (n, m) != (N, V) or dlogits.dtype != logits.dtype:
+            raise ValueError("dlogits must have logits' shape and type")
+    if workspace is None:
+        workspace = torch.empty(int(_lib.sf_policy_loss_workspace_size(N, V)), dtype=torch.uint8, device=logits.device)
+        made.append(workspace)
+    _hold(made, stream)
+    cfg = PolicyConfig(clip[0], clip[1], kl_coef, inv_temperature)
+    _check(_lib.sf_policy_loss(_p(logits), _DTYPES[logits.dtype], N, V, ld, _p(target), _p(old_logp), _p(ref_logp),
+                               _p(advantage), _p(weight), ctypes.byref(cfg), _p(grad_out), _p(logp), _p(token_loss),
+                               _p(stats), _p(dlogits), ldd, _p(workspace), workspace.numel(), _p(status),
+                               _stream(stream)), "sf_policy_loss")
+    return PolicyLoss(logp, token_loss, stats, dlogits)
