@@ -58,6 +58,33 @@ bool rows_overlap(const void* a, int64_t lda, const void* b, int64_t ldb, int64_
   return off < n || step - off < n;
 }
 
+bool sizes_ok(const int64_t* numel, int64_t n) {
+  if (n < 0 || n > (int64_t(1) << 20) || (n > 0 && !numel)) return false;
+  for (int64_t i = 0; i < n; ++i)
+    if (numel[i] < 0 || numel[i] >= (int64_t(1) << 40)) return false;
+  return true;
+}
+
+// sf_grad_norm and sf_grad_clip (out: the results' pointers, null in place).
+sf_status grad_args_ok(const GradJob& j, const void* workspace, size_t workspace_bytes) {
+  if (!sizes_ok(j.numel, j.n) || !j.norm || (j.n > 0 && (!j.data || !j.dtype))) return SF_EINVAL;
+  for (int64_t i = 0; i < j.n; ++i) {
+    if (!dtype_ok(j.dtype[i])) return SF_EINVAL;
+    if (j.numel[i] == 0) continue;
+    const size_t size = dtype_size(j.dtype[i]);
+    if (!j.data[i] || (j.out && !j.out[i])) return SF_EINVAL;
+    if (!aligned(j.data[i], size) || (j.out && !aligned(j.out[i], size))) return SF_EINVAL_ALIGN;
+    if (j.out && j.out[i] != j.data[i] &&
+        rows_overlap(j.data[i], j.numel[i], j.out[i], j.numel[i], 1, j.numel[i], size))
+      return SF_EINVAL;
+  }
+  if (!aligned(j.norm, 4) || !aligned(j.coef, 4) || !aligned(j.tensor_norm, 4) || !aligned(j.status, 4))
+    return SF_EINVAL_ALIGN;
+  if (!workspace || workspace_bytes < grad_workspace(j.numel, j.n)) return SF_EWORKSPACE;
+  if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
+  return SF_OK;
+}
+
 size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct LabelLayout {
@@ -521,6 +548,45 @@ sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V
   j.ldd = ldd;
   j.status = status;
   return cuda_status(launch_policy_loss(j, workspace, stream));
+}
+
+size_t sf_grad_workspace_size(const int64_t* numel, int64_t n) {
+  return sizes_ok(numel, n) ? grad_workspace(numel, n) : 0;
+}
+
+sf_status sf_grad_norm(const void* const* data, const int64_t* numel, const int32_t* dtype, int64_t n, float* norm,
+                       float* tensor_norm, void* workspace, size_t workspace_bytes, uint32_t* status,
+                       cudaStream_t stream) {
+  GradJob j;
+  j.data = data;
+  j.numel = numel;
+  j.dtype = dtype;
+  j.n = n;
+  j.norm = norm;
+  j.tensor_norm = tensor_norm;
+  j.status = status;
+  const sf_status st = grad_args_ok(j, workspace, workspace_bytes);
+  return st != SF_OK ? st : cuda_status(launch_grad(j, workspace, stream));
+}
+
+sf_status sf_grad_clip(const void* const* data, void* const* out, const int64_t* numel, const int32_t* dtype,
+                       int64_t n, float max_norm, float eps, float* norm, float* coef, float* tensor_norm,
+                       void* workspace, size_t workspace_bytes, uint32_t* status, cudaStream_t stream) {
+  if (!(max_norm > 0.f) || !(eps >= 0.f && std::isfinite(eps))) return SF_EINVAL;
+  GradJob j;
+  j.data = data;
+  j.out = out;
+  j.numel = numel;
+  j.dtype = dtype;
+  j.n = n;
+  j.max_norm = max_norm;
+  j.eps = eps;
+  j.norm = norm;
+  j.coef = coef;
+  j.tensor_norm = tensor_norm;
+  j.status = status;
+  const sf_status st = grad_args_ok(j, workspace, workspace_bytes);
+  return st != SF_OK ? st : cuda_status(launch_grad(j, workspace, stream));
 }
 
 }  // extern "C"

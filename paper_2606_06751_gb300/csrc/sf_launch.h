@@ -141,4 +141,18 @@ struct PolicyJob {
 size_t policy_loss_workspace(int64_t N);
 cudaError_t launch_policy_loss(PolicyJob job, void* workspace, cudaStream_t stream);
 
+// data, out, numel and dtype are host arrays of n; max_norm = 0: the norms only.
+struct GradJob {
+  const void* const* data;
+  void* const* out = nullptr;
+  const int64_t* numel;
+  const int32_t* dtype;
+  int64_t n;
+  float max_norm = 0.f, eps = 0.f;
+  float *norm, *coef = nullptr, *tensor_norm;
+  uint32_t* status;
+};
+size_t grad_workspace(const int64_t* numel, int64_t n);
+cudaError_t launch_grad(const GradJob& job, void* workspace, cudaStream_t stream);
+
 }  // namespace sf

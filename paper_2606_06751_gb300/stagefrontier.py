@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from dataclasses import dataclass
 from typing import Optional
 
@@ -82,6 +83,8 @@ def _load():
         "sf_gathered_to_steps": [P, I, I, I, I, P, S],
         "sf_policy_loss": [P, I32, I, I, I, P, P, P, P, P, ctypes.POINTER(PolicyConfig), P, P, P, P, P, I, P,
                            ctypes.c_size_t, P, S],
+        "sf_grad_norm": [P, P, P, I, P, P, P, ctypes.c_size_t, P, S],
+        "sf_grad_clip": [P, P, P, P, I, ctypes.c_float, ctypes.c_float, P, P, P, P, ctypes.c_size_t, P, S],
     }
     for name, argt in sigs.items():
         f = getattr(L, name)
@@ -101,6 +104,8 @@ def _load():
     L.sf_label_windows_workspace_size.restype = ctypes.c_size_t
     L.sf_rank_workspace_size.argtypes = [I, I, I]
     L.sf_rank_workspace_size.restype = ctypes.c_size_t
+    L.sf_grad_workspace_size.argtypes = [P, I]
+    L.sf_grad_workspace_size.restype = ctypes.c_size_t
     L.sf_policy_loss_workspace_size.argtypes = [I, I]
     L.sf_policy_loss_workspace_size.restype = ctypes.c_size_t
     for name in ("sf_stream_windows_staging_size", "sf_stream_gathered_staging_size"):
@@ -648,3 +653,69 @@ def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=No
                                _p(stats), _p(dlogits), ldd, _p(workspace), workspace.numel(), _p(status),
                                _stream(stream)), "sf_policy_loss")
     return PolicyLoss(logp, token_loss, stats, dlogits)
+
+
+@dataclass
+class GradNorm:
+    norm: torch.Tensor
+    coef: Optional[torch.Tensor]
+    tensor_norm: Optional[torch.Tensor]
+
+
+def _tensor_list(tensors, name: str):
+    """Host arrays (pointers, sizes, types) of contiguous CUDA tensors."""
+    for t in tensors:
+        if not t.is_cuda or t.dtype not in _DTYPES or not t.is_contiguous():
+            raise TypeError(f"{name} must be contiguous CUDA tensors of float32, bfloat16 or float16")
+    return (array("Q", [t.data_ptr() for t in tensors]), array("q", [t.numel() for t in tensors]),
+            array("i", [_DTYPES[t.dtype] for t in tensors]))
+
+
+def _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, workspace, status, stream):
+    grads = list(grads)
+    n = len(grads)
+    ptr, numel, dtype = _tensor_list(grads, "grads")
+    device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    out_ptr = None
+    if out is not None:
+        out_ptr, out_numel, out_dtype = _tensor_list(list(out), "out")
+        if out_numel != numel or out_dtype != dtype:
+            raise ValueError("out must have the gradients' sizes and types")
+    made = []
+
+    def new(m, dt=torch.float32):
+        made.append(torch.empty(m, dtype=dt, device=device))
+        return made[-1]
+
+    norm = new(1) if norm is None else _vec(norm, 1, torch.float32, "norm")
+    if tensor_norm is None and per_tensor:
+        tensor_norm = new(n)
+    _vec(tensor_norm, n, torch.float32, "tensor_norm")
+    at = lambda a: a.buffer_info()[0]  # noqa: E731
+    if workspace is None:
+        workspace = new(int(_lib.sf_grad_workspace_size(at(numel), n)), torch.uint8)
+    if max_norm is None:
+        _hold(made, stream)
+        _check(_lib.sf_grad_norm(at(ptr), at(numel), at(dtype), n, _p(norm), _p(tensor_norm), _p(workspace),
+                                 workspace.numel(), _p(status), _stream(stream)), "sf_grad_norm")
+        return GradNorm(norm, None, tensor_norm)
+    coef = new(1) if coef is None else _vec(coef, 1, torch.float32, "coef")
+    _hold(made, stream)
+    _check(_lib.sf_grad_clip(at(ptr), None if out_ptr is None else at(out_ptr), at(numel), at(dtype), n, max_norm, eps,
+                             _p(norm), _p(coef), _p(tensor_norm), _p(workspace), workspace.numel(), _p(status),
+                             _stream(stream)), "sf_grad_clip")
+    return GradNorm(norm, coef, tensor_norm)
+
+
+def sf_grad_norm(grads, per_tensor: bool = False, norm=None, tensor_norm=None, workspace=None, status=None,
+                 stream=None) -> GradNorm:
+    """The 2-norm over a sequence of gradient tensors and, with `per_tensor`, of each."""
+    return _grad(grads, None, None, 0.0, norm, None, tensor_norm, per_tensor, workspace, status, stream)
+
+
+def sf_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, per_tensor: bool = False, norm=None, coef=None,
+                 tensor_norm=None, workspace=None, status=None, stream=None) -> GradNorm:
+    """sf_grad_norm, then the gradients times coef = min(1, max_norm / (norm + eps)):
+    in place, or into the tensors of `out`.  Where the norm is not finite, coef is
+    NaN and the gradients stay as they are."""
+    return _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, workspace, status, stream)
