@@ -85,6 +85,12 @@ sf_status grad_args_ok(const GradJob& j, const void* workspace, size_t workspace
   return SF_OK;
 }
 
+bool route_ok(const sf_route_config* c, int64_t E) {
+  return c && c->k >= 1 && c->k <= 32 && c->k <= E && E <= 1024 &&
+         (c->score == SF_SCORE_SOFTMAX || c->score == SF_SCORE_SIGMOID) && (c->renorm == 0 || c->renorm == 1) &&
+         std::isfinite(c->scale);
+}
+
 size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct LabelLayout {
@@ -587,6 +593,64 @@ sf_status sf_grad_clip(const void* const* data, void* const* out, const int64_t*
   j.status = status;
   const sf_status st = grad_args_ok(j, workspace, workspace_bytes);
   return st != SF_OK ? st : cuda_status(launch_grad(j, workspace, stream));
+}
+
+sf_status sf_route_experts(const void* logits, int32_t dtype, int64_t T, int64_t E, int64_t ld, const float* bias,
+                           const sf_route_config* cfg, int32_t* index, float* weight, int32_t* load,
+                           int32_t accumulate, uint32_t* status, cudaStream_t stream) {
+  if (!dtype_ok(dtype) || !rows_ok(T, E, ld) || !route_ok(cfg, E) || (accumulate != 0 && accumulate != 1))
+    return SF_EINVAL;
+  if (cfg->groups < 1 || cfg->groups > 32 || E % cfg->groups != 0 || cfg->top_groups < 1 ||
+      cfg->top_groups > cfg->groups || cfg->group_top < 1 || cfg->group_top > 2 ||
+      cfg->k > cfg->top_groups * (E / cfg->groups))
+    return SF_EINVAL;
+  if (T > 0 && (!logits || !index || !weight)) return SF_EINVAL;
+  if (!aligned(logits, dtype_size(dtype)) || !aligned(bias, 4) || !aligned(index, 4) || !aligned(weight, 4) ||
+      !aligned(load, 4) || !aligned(status, 4))
+    return SF_EINVAL_ALIGN;
+  if (T == 0) {
+    ZeroList z;
+    if (!accumulate) z.add(load, size_t(E) * sizeof(int32_t));
+    return cuda_status(launch_zero_many(z, stream));
+  }
+  RouteJob j;
+  j.logits = logits;
+  j.dtype = dtype;
+  j.T = T;
+  j.E = E;
+  j.ld = ld;
+  j.bias = bias;
+  j.cfg = *cfg;
+  j.index = index;
+  j.weight = weight;
+  j.load = load;
+  j.status = status;
+  return cuda_status(launch_route(j, accumulate != 0, stream));
+}
+
+sf_status sf_route_experts_grad(const void* logits, int32_t dtype, int64_t T, int64_t E, int64_t ld,
+                                const int32_t* index, const float* dweight, const sf_route_config* cfg,
+                                void* dlogits, int64_t ldd, uint32_t* status, cudaStream_t stream) {
+  if (!dtype_ok(dtype) || !rows_ok(T, E, ld) || !rows_ok(T, E, ldd) || !route_ok(cfg, E)) return SF_EINVAL;
+  if (T == 0) return SF_OK;
+  if (!logits || !index || !dweight || !dlogits) return SF_EINVAL;
+  if (!aligned(logits, dtype_size(dtype)) || !aligned(dlogits, dtype_size(dtype)) || !aligned(index, 4) ||
+      !aligned(dweight, 4) || !aligned(status, 4))
+    return SF_EINVAL_ALIGN;
+  if (rows_overlap(logits, ld, dlogits, ldd, T, E, dtype_size(dtype))) return SF_EINVAL;
+  RouteGradJob j;
+  j.logits = logits;
+  j.dtype = dtype;
+  j.T = T;
+  j.E = E;
+  j.ld = ld;
+  j.index = index;
+  j.dweight = dweight;
+  j.cfg = *cfg;
+  j.dlogits = dlogits;
+  j.ldd = ldd;
+  j.status = status;
+  return cuda_status(launch_route_grad(j, stream));
 }
 
 }  // extern "C"

@@ -123,21 +123,26 @@ __device__ __forceinline__ V block_sum(V v, V* buf) {
   return s;
 }
 
-// Launch `kern` as the programmatic dependent of the previous launch on
-// `stream`: it may be set up while that one drains, and waits for it with
-// griddep_wait() before it touches memory.
+// Launch `kern`; with `dependent`, as the programmatic dependent of the
+// previous launch on `stream`: it may start while that one drains, and waits
+// for its end in griddep_wait().
 template <typename... KArgs, typename... Args>
-cudaError_t launch_dependent(void (*kern)(KArgs...), dim3 grid, dim3 block, cudaStream_t stream, Args... args) {
+cudaError_t launch_after(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
+                         bool dependent, const Args&... args) {
+  static_assert(((sizeof(KArgs) == sizeof(Args)) && ...), "arguments of the kernel's own types");
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, args...);
+  cfg.numAttrs = dependent ? 1 : 0;
+  // parameters by address: a list of tensors is up to 32 KB
+  void* params[] = {const_cast<void*>(static_cast<const void*>(&args))...};
+  return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kern), params);
 }
 
 }  // namespace sf

@@ -299,7 +299,7 @@ cudaError_t launch_lists(const GradJob& j, void* workspace, cudaStream_t stream)
       cudaError_t e;
       count_launch();
       if (pass == 0) {
-        e = launch_dependent(grad_squares_kernel<M>, dim3(grid), dim3(kThreads), stream, list);
+        e = launch_after(grad_squares_kernel<M>, dim3(grid), dim3(kThreads), 0, stream, true, list);
       } else {
         NormOut o;
         o.total = total;
@@ -317,10 +317,10 @@ cudaError_t launch_lists(const GradJob& j, void* workspace, cudaStream_t stream)
         o.status = j.status;
         float* norms = j.tensor_norm != nullptr ? j.tensor_norm + from : nullptr;
         if (clip) {
-          e = launch_dependent(grad_scale_kernel<M>, dim3(grid), dim3(kThreads), stream, list, o, norms);
+          e = launch_after(grad_scale_kernel<M>, dim3(grid), dim3(kThreads), 0, stream, true, list, o, norms);
         } else {
           const unsigned few = norms != nullptr ? (list.count * 32 + kThreads - 1) / kThreads : 1;
-          e = launch_dependent(grad_norms_kernel<M>, dim3(std::max(1u, few)), dim3(kThreads), stream, list, o, norms);
+          e = launch_after(grad_norms_kernel<M>, dim3(std::max(1u, few)), dim3(kThreads), 0, stream, true, list, o, norms);
         }
       }
       if (e != cudaSuccess) return e;

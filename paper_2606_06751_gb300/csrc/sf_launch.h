@@ -155,4 +155,31 @@ struct GradJob {
 size_t grad_workspace(const int64_t* numel, int64_t n);
 cudaError_t launch_grad(const GradJob& job, void* workspace, cudaStream_t stream);
 
+struct RouteJob {
+  const void* logits;
+  int32_t dtype;
+  int64_t T, E, ld;
+  const float* bias;
+  sf_route_config cfg;
+  int32_t* index;
+  float* weight;
+  int32_t* load;
+  uint32_t* status;
+  bool only_cta = false;  // set by launch_route: one CTA writes the loads instead of adding to them
+};
+cudaError_t launch_route(RouteJob job, bool accumulate, cudaStream_t stream);
+
+struct RouteGradJob {
+  const void* logits;
+  int32_t dtype;
+  int64_t T, E, ld;
+  const int32_t* index;
+  const float* dweight;
+  sf_route_config cfg;
+  void* dlogits;
+  int64_t ldd;
+  uint32_t* status;
+};
+cudaError_t launch_route_grad(const RouteGradJob& job, cudaStream_t stream);
+
 }  // namespace sf

@@ -255,12 +255,11 @@ cudaError_t launch_policy_loss(PolicyJob j, void* workspace, cudaStream_t stream
   const int64_t blocks = sum_blocks(j.N);
   double* part = blocks > 1 ? reinterpret_cast<double*>(j.terms + j.N) : nullptr;
   count_launch();
-  const cudaError_t s = launch_dependent(policy_sum_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kSumThreads),
-                                         stream, static_cast<const float4*>(j.terms), j.N, part, j.stats);
+  const cudaError_t s = launch_after(policy_sum_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kSumThreads), 0,
+                                     stream, true, j.terms, j.N, part, j.stats);
   if (s != cudaSuccess || part == nullptr) return s;
   count_launch();
-  return launch_dependent(policy_sum_parts_kernel, dim3(1), dim3(128), stream, static_cast<const double*>(part),
-                          blocks, j.stats);
+  return launch_after(policy_sum_parts_kernel, dim3(1), dim3(128), 0, stream, true, part, blocks, j.stats);
 }
 
 }  // namespace sf

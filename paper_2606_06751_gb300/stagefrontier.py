@@ -51,6 +51,11 @@ class PolicyConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "kl_coef", "inv_temperature")]
 
 
+class RouteConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("k", "score", "groups", "top_groups", "group_top", "renorm")] + \
+               [("scale", ctypes.c_float)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libstagefrontier.so not built at {LIB_PATH}; run "
@@ -83,6 +88,8 @@ def _load():
         "sf_gathered_to_steps": [P, I, I, I, I, P, S],
         "sf_policy_loss": [P, I32, I, I, I, P, P, P, P, P, ctypes.POINTER(PolicyConfig), P, P, P, P, P, I, P,
                            ctypes.c_size_t, P, S],
+        "sf_route_experts": [P, I32, I, I, I, P, ctypes.POINTER(RouteConfig), P, P, P, I32, P, S],
+        "sf_route_experts_grad": [P, I32, I, I, I, P, P, ctypes.POINTER(RouteConfig), P, I, P, S],
         "sf_grad_norm": [P, P, P, I, P, P, P, ctypes.c_size_t, P, S],
         "sf_grad_clip": [P, P, P, P, I, ctypes.c_float, ctypes.c_float, P, P, P, P, ctypes.c_size_t, P, S],
     }
@@ -653,6 +660,76 @@ def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=No
                                _p(stats), _p(dlogits), ldd, _p(workspace), workspace.numel(), _p(status),
                                _stream(stream)), "sf_policy_loss")
     return PolicyLoss(logp, token_loss, stats, dlogits)
+
+
+_SCORES = {"softmax": SF_SCORE_SOFTMAX, "sigmoid": SF_SCORE_SIGMOID}
+
+
+@dataclass
+class Routing:
+    index: torch.Tensor
+    weight: torch.Tensor
+    load: Optional[torch.Tensor]
+
+
+def _score(score: str) -> int:
+    if score not in _SCORES:
+        raise ValueError(f"score must be one of {', '.join(_SCORES)}")
+    return _SCORES[score]
+
+
+def sf_route_experts(logits, k: int, bias=None, score: str = "softmax", groups: int = 1, top_groups: int = 1,
+                     group_top: int = 2, renorm: bool = True, scale: float = 1.0, index=None, weight=None, load=None,
+                     accumulate: bool = False, want=("load",), status=None, stream=None) -> Routing:
+    """Tokens' k experts from router logits [T][E]: index and weight [T][k] by
+    falling choice value, and the experts' loads [E] (added to `load` with
+    `accumulate`).  `bias` [E] takes part in the choice only."""
+    T, E, ld = _rows(logits, "logits")
+    _vec(bias, E, torch.float32, "bias")
+    if accumulate and load is None:
+        raise ValueError("accumulate adds to a load that the caller gives")
+    made = []
+
+    def new(shape, dt):
+        made.append(_empty(shape, dt, logits))
+        return made[-1]
+
+    slots = T * k if k > 0 else 0  # a bad k is the library's to refuse
+    index = new((T, max(k, 0)), torch.int32) if index is None else _vec(index, slots, torch.int32, "index")
+    weight = new((T, max(k, 0)), torch.float32) if weight is None else _vec(weight, slots, torch.float32, "weight")
+    if load is None and "load" in want:
+        load = new((E,), torch.int32)
+    _vec(load, E, torch.int32, "load")
+    _hold(made, stream)
+    cfg = RouteConfig(k, _score(score), groups, top_groups, group_top, 1 if renorm else 0, scale)
+    _check(_lib.sf_route_experts(_p(logits), _DTYPES[logits.dtype], T, E, ld, _p(bias), ctypes.byref(cfg), _p(index),
+                                 _p(weight), _p(load), 1 if accumulate else 0, _p(status), _stream(stream)),
+           "sf_route_experts")
+    return Routing(index, weight, load)
+
+
+def sf_route_experts_grad(logits, index, dweight, score: str = "softmax", renorm: bool = True, scale: float = 1.0,
+                          dlogits=None, status=None, stream=None) -> torch.Tensor:
+    """The gradient of the router's logits from that of its weights [T][k]."""
+    T, E, ld = _rows(logits, "logits")
+    _dev(index, torch.int32, "index")
+    if index.dim() != 2 or index.shape[0] != T:
+        raise ValueError("index must be [T][k]")
+    k = index.shape[1]
+    _vec(dweight, T * k, torch.float32, "dweight")
+    ldd = E
+    if dlogits is None:
+        dlogits = _empty((T, E), logits.dtype, logits)
+        _hold([dlogits], stream)
+    else:
+        n, m, ldd = _rows(dlogits, "dlogits")
+        if (n, m) != (T, E) or dlogits.dtype != logits.dtype:
+            raise ValueError("dlogits must have logits' shape and type")
+    cfg = RouteConfig(k, _score(score), 1, 1, 1, 1 if renorm else 0, scale)
+    _check(_lib.sf_route_experts_grad(_p(logits), _DTYPES[logits.dtype], T, E, ld, _p(index), _p(dweight),
+                                      ctypes.byref(cfg), _p(dlogits), ldd, _p(status), _stream(stream)),
+           "sf_route_experts_grad")
+    return dlogits
 
 
 @dataclass
