@@ -460,7 +460,7 @@ typedef enum sf_dtype { SF_F32 = 0, SF_BF16 = 1, SF_F16 = 2 } sf_dtype;
 typedef struct sf_policy_config {
   float clip_low, clip_high; /* the ratio's bounds are 1 - clip_low and 1 + clip_high; 0 <= clip_low <= 1 */
   float kl_coef;             /* beta >= 0 */
-  float inv_temperature;     /* tau > 0: the policy is softmax(tau * logits) */
+  float inv_temperature;     /* tau, 0 < tau <= 1e6: the policy is softmax(tau * logits) */
 } sf_policy_config;
 
 /*

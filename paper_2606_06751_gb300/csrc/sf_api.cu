@@ -517,7 +517,7 @@ sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V
   if (N > 0 && (!logits || !target || !old_logp || !advantage)) return SF_EINVAL;
   if (!(cfg->clip_low >= 0.f && cfg->clip_low <= 1.f && cfg->clip_high >= 0.f && std::isfinite(cfg->clip_high) &&
         cfg->kl_coef >= 0.f && std::isfinite(cfg->kl_coef) && cfg->inv_temperature > 0.f &&
-        std::isfinite(cfg->inv_temperature)))
+        cfg->inv_temperature <= 1e6f))
     return SF_EINVAL;
   if (!aligned(logits, dtype_size(dtype)) || !aligned(dlogits, dtype_size(dtype)) || !aligned(target, 8) ||
       !aligned(old_logp, 4) || !aligned(ref_logp, 4) || !aligned(advantage, 4) || !aligned(weight, 4) ||

@@ -59,6 +59,106 @@ __device__ __forceinline__ void unpack(const uint4& u, float (&f)[8], __half) {
   }
 }
 
+// Two f32 in a 64-bit register: one instruction for both.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(uint64_t r, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// A pack as pairs of f32.
+__device__ __forceinline__ void unpack2(const uint4& u, uint64_t (&z)[2], float) {
+  z[0] = pair_of(__uint_as_float(u.x), __uint_as_float(u.y));
+  z[1] = pair_of(__uint_as_float(u.z), __uint_as_float(u.w));
+}
+template <typename T>
+__device__ __forceinline__ void unpack2(const uint4& u, uint64_t (&z)[4], T t) {
+  float f[8];
+  unpack(u, f, t);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = pair_of(f[2 * i], f[2 * i + 1]);
+}
+
+// A pack of -inf.
+__device__ __forceinline__ uint4 same4(uint32_t w) { return make_uint4(w, w, w, w); }
+__device__ __forceinline__ uint4 lowest_pack(float) { return same4(0xff800000u); }
+__device__ __forceinline__ uint4 lowest_pack(__nv_bfloat16) { return same4(0xff80ff80u); }
+__device__ __forceinline__ uint4 lowest_pack(__half) { return same4(0xfc00fc00u); }
+
+// A pack to an address that is aligned to its elements only.
+__device__ __forceinline__ void store_elements(float* p, const uint4& u) {
+  p[0] = __uint_as_float(u.x);
+  p[1] = __uint_as_float(u.y);
+  p[2] = __uint_as_float(u.z);
+  p[3] = __uint_as_float(u.w);
+}
+template <typename T>
+__device__ __forceinline__ void store_elements(T* p, const uint4& u) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  unsigned short* h = reinterpret_cast<unsigned short*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    h[2 * i] = static_cast<unsigned short>(w[i]);
+    h[2 * i + 1] = static_cast<unsigned short>(w[i] >> 16);
+  }
+}
+
+// The largest value of K packs; NaN only if all are.
+template <int K>
+__device__ __forceinline__ float packs_max(const uint4 (&u)[K], float) {
+  float m = __uint_as_float(u[0].x);
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(u[k].x)), fmaxf(__uint_as_float(u[k].y), __uint_as_float(u[k].z))),
+              __uint_as_float(u[k].w));
+  return m;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <int K>
+__device__ __forceinline__ float packs_max(const uint4 (&u)[K], __nv_bfloat16) {
+  uint32_t m = u[0].x;
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    m = max_bf16x2(max_bf16x2(m, u[k].x), max_bf16x2(max_bf16x2(u[k].y, u[k].z), u[k].w));
+  return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+}
+template <int K>
+__device__ __forceinline__ float packs_max(const uint4 (&u)[K], __half) {
+  uint32_t m = u[0].x;
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    m = max_f16x2(max_f16x2(m, u[k].x), max_f16x2(max_f16x2(u[k].y, u[k].z), u[k].w));
+  return fmaxf(__half2float(__ushort_as_half(static_cast<unsigned short>(m))),
+               __half2float(__ushort_as_half(static_cast<unsigned short>(m >> 16))));
+}
+
 __device__ __forceinline__ uint4 pack(const float (&f)[4], float) {
   return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
 }
@@ -97,6 +197,18 @@ __device__ __forceinline__ void store16(void* p, const uint4& v) {
                : "memory");
 }
 
+// L2 policies: data that is not used again leaves first.
+__device__ __forceinline__ uint64_t policy_evict_first() {
+  uint64_t p;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ void store16(void* p, const uint4& v, uint64_t policy) {
+  asm volatile("st.global.L1::no_allocate.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(v.x),
+               "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy)
+               : "memory");
+}
+
 // Elements of a run of n at p that lie before its first 16-byte boundary.
 template <typename T>
 __device__ __forceinline__ int head_of(const T* p, int64_t n) {
@@ -108,6 +220,37 @@ __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0
 
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xff800000u); }
 __device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7fffffffu); }
+
+// A sum held as an unevaluated pair of f32, about 48 bits: each addition's
+// rounding error is found exactly (Knuth's two-sum) and kept in lo.
+struct Sum2 {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ void add(float v) {
+    const float s = hi + v, b = s - hi;
+    lo += (hi - (s - b)) + (v - b);
+    hi = s;
+  }
+};
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+  return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
+  return v;
+}
+// In a fixed order; the same bits in every lane (two-sum does not depend on its terms' order).
+__device__ __forceinline__ Sum2 warp_sum(Sum2 s) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float h = __shfl_xor_sync(kFull, s.hi, o), l = __shfl_xor_sync(kFull, s.lo, o);
+    s.add(h);
+    s.lo += l;
+  }
+  return s;
+}
 
 // Sum over the block in a fixed order; every thread gets it.  `buf` holds one
 // value per warp.  Callers that reuse buf synchronise in between.

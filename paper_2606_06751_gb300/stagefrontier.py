@@ -132,14 +132,23 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+# the current stream's handle without a Stream object around it (3 us), where torch has that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _hold(tensors, *streams):
     """Temporaries the binding allocated for work enqueued on `streams`: the
     caching allocator may reuse their memory only once that work is done."""
+    if all(st is None for st in streams):
+        return
     cur = torch.cuda.current_stream()
     for st in streams:
         if st is not None and st != cur:

@@ -118,7 +118,8 @@ def check(r, e, dtype, grad=True):
 
 
 SIZES = [(1, 1), (1, 2), (3, 7), (2, 33), (5, 1000), (40, 4099), (700, 257), (1, 65536), (3, 50001), (9, 32768),
-         (2, 131072), (3, 262144), (2, 300007)]
+         (2, 131072), (3, 262144), (2, 300007), (2, 136001), (90, 50001), (400, 8), (333, 5), (310, 8192), (317, 16387),
+         (650, 4099)]
 
 
 @pytest.mark.parametrize("N,V", SIZES)
@@ -140,8 +141,8 @@ def test_loss_and_gradient(sf, N, V, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V,ld,offset", [(1000, 1008, 0), (1000, 1001, 0), (1001, 1001, 1), (8190, 8200, 3), (5, 9, 2),
                                          (40001, 40003, 5)])
-def test_strides_and_offsets(sf, dtype, V, ld, offset):
-    N = 7
+@pytest.mark.parametrize("N", [7, 320])
+def test_strides_and_offsets(sf, dtype, V, ld, offset, N):
     z, h = make(N, V, dtype, V, ld, offset)
     e = reference(h)
     e["y"] = h["y"]
@@ -183,10 +184,13 @@ def test_optional_inputs(sf, N, V):
 
 @pytest.mark.parametrize("V", [64, 5000, 70001])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_masked_rows_are_not_read(sf, V, dtype):
-    N = 12
+@pytest.mark.parametrize("N", [12, 700])
+def test_masked_rows_are_not_read(sf, V, dtype, N):
+    if N * V > 10 ** 7:
+        V = 9001
     z, h = make(N, V, dtype, V)
     h["w"][[0, 3, 4, 11]] = 0.0
+    h["w"][12:690] = 0.0  # a long run of them
     e = reference(h)
     e["y"] = h["y"]
     z[0] = math.nan
@@ -208,9 +212,10 @@ def test_masked_rows_are_not_read(sf, V, dtype):
 
 @pytest.mark.parametrize("V", [64, 5000, 70001])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-def test_ruled_out_tokens(sf, V, dtype):
+@pytest.mark.parametrize("N", [6, 330])
+def test_ruled_out_tokens(sf, V, dtype, N):
     """-inf and the type's lowest value as masks, and a row of nothing but the latter."""
-    N = 6
+    V = V if N * V < 10 ** 7 else 9001
     z, h = make(N, V, dtype, V + 1)
     low = torch.finfo(TYPES[dtype]).min
     z[0, 1::2] = -math.inf
@@ -249,8 +254,9 @@ def test_chosen_token_ruled_out(sf, V):
 
 @pytest.mark.parametrize("V", [64, 5000, 70001, 300001])
 @pytest.mark.parametrize("grad", [False, True])
-def test_faulty_rows_are_left_out(sf, V, grad):
-    N = 9
+@pytest.mark.parametrize("N", [9, 400])
+def test_faulty_rows_are_left_out(sf, V, grad, N):
+    V = V if N * V < 10 ** 7 else 9001
     z, h = make(N, V, "bf16", V + 3)
     bad = h.copy()
     bad["w"] = h["w"].copy()
@@ -300,6 +306,26 @@ def test_same_bits_again_and_on_another_stream(sf, N, V):
     for o in (b, c, d):
         for k in ("logp", "token_loss", "stats", "dlogits"):
             assert torch.equal(getattr(a, k), getattr(o, k)), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V", [(3, 1000), (320, 1000), (3, 140000)])
+@pytest.mark.parametrize("level", [1e36, -1e36, 3e38, -3e38])
+def test_far_out_logits(sf, dtype, N, V, level):
+    """Rows at the end of the type's range: what counts is the differences."""
+    z, h = make(N, V, dtype, 17)
+    z[1] = level
+    z[1, V // 2:] = z[1, 0] * (0.5 if level > 0 else 1.125) if abs(level) < 1e38 else -level
+    h["x"] = z.double().cpu().numpy()
+    h["y"][1] = 3 if level > 0 or abs(level) < 1e38 else V - 1
+    lp = logprob(h["x"] * TAU)[np.arange(N), h["y"]]
+    h["old"][1] = lp[1] + 0.1
+    h["ref"][1] = lp[1] - 0.2
+    e = reference(h)
+    e["y"] = h["y"]
+    r, st = call(sf, z, h, grad=True)
+    assert st == 0
+    check(r, e, dtype)
 
 
 def test_many_rows(sf):
