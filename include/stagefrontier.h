@@ -569,7 +569,7 @@ sf_status sf_route_experts_grad(const void* logits, int32_t dtype, int64_t T, in
  *               sf_dtype.  Read before the call returns.
  *   norm        [1] f32: sqrt(sum of squares over all tensors)
  *   tensor_norm [n] f32 (nullable): each tensor's own
- *   workspace   device, 16-byte aligned, sf_grad_workspace_size(...) bytes
+ *   workspace   device, 16-byte aligned, sf_grad_workspace_size(n) bytes
  * Squares that leave the range of 32 bits are summed in 64.  Where the norm is
  * not finite (or above the largest f32) SF_ST_NONFINITE is set and `norm`
  * holds what it is; tensor_norm tells which tensors are the cause.
@@ -592,9 +592,9 @@ sf_status sf_grad_clip(const void* const* data, void* const* out, const int64_t*
                        int64_t n, float max_norm, float eps, float* norm, float* coef, float* tensor_norm,
                        void* workspace, size_t workspace_bytes, uint32_t* status, cudaStream_t stream);
 
-/* Workspace bytes sf_grad_norm and sf_grad_clip need for these tensors on the
+/* Workspace bytes sf_grad_norm and sf_grad_clip need for n tensors on the
    current device; 0 on bad arguments. */
-size_t sf_grad_workspace_size(const int64_t* numel, int64_t n);
+size_t sf_grad_workspace_size(int64_t n);
 
 #ifdef __cplusplus
 }

@@ -58,8 +58,9 @@ bool rows_overlap(const void* a, int64_t lda, const void* b, int64_t ldb, int64_
   return off < n || step - off < n;
 }
 
+constexpr int64_t kMaxTensors = int64_t(1) << 20;
 bool sizes_ok(const int64_t* numel, int64_t n) {
-  if (n < 0 || n > (int64_t(1) << 20) || (n > 0 && !numel)) return false;
+  if (n < 0 || n > kMaxTensors || (n > 0 && !numel)) return false;
   for (int64_t i = 0; i < n; ++i)
     if (numel[i] < 0 || numel[i] >= (int64_t(1) << 40)) return false;
   return true;
@@ -80,7 +81,7 @@ sf_status grad_args_ok(const GradJob& j, const void* workspace, size_t workspace
   }
   if (!aligned(j.norm, 4) || !aligned(j.coef, 4) || !aligned(j.tensor_norm, 4) || !aligned(j.status, 4))
     return SF_EINVAL_ALIGN;
-  if (!workspace || workspace_bytes < grad_workspace(j.numel, j.n)) return SF_EWORKSPACE;
+  if (!workspace || workspace_bytes < grad_workspace(j.n)) return SF_EWORKSPACE;
   if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
   return SF_OK;
 }
@@ -556,9 +557,7 @@ sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V
   return cuda_status(launch_policy_loss(j, workspace, stream));
 }
 
-size_t sf_grad_workspace_size(const int64_t* numel, int64_t n) {
-  return sizes_ok(numel, n) ? grad_workspace(numel, n) : 0;
-}
+size_t sf_grad_workspace_size(int64_t n) { return n < 0 || n > kMaxTensors ? 0 : grad_workspace(n); }
 
 sf_status sf_grad_norm(const void* const* data, const int64_t* numel, const int32_t* dtype, int64_t n, float* norm,
                        float* tensor_norm, void* workspace, size_t workspace_bytes, uint32_t* status,

@@ -152,7 +152,7 @@ struct GradJob {
   float *norm, *coef = nullptr, *tensor_norm;
   uint32_t* status;
 };
-size_t grad_workspace(const int64_t* numel, int64_t n);
+size_t grad_workspace(int64_t n);
 cudaError_t launch_grad(const GradJob& job, void* workspace, cudaStream_t stream);
 
 struct RouteJob {

@@ -1,11 +1,9 @@
 // sf_route.cu - the router of a layer of experts and its gradient
 // (sf_route_experts, sf_route_experts_grad).
 //
-// Forward: a warp a token, NV consecutive experts a lane in registers.  The
-// choice values are made orderable as unsigned keys (0: not available), so a
-// maximum is one 32-bit warp reduction; the k chosen are taken one by one, the
-// lowest lane and expert first among equals.  Loads are counted in shared
-// memory and added to the totals once a CTA.
+// A warp a token, NV consecutive experts a lane.  What it costs is
+// instructions, not memory: 256 values a token are scored, and the k largest
+// found, in the time that memory takes for a kilobyte.
 #include <algorithm>
 
 #include "sf_float.cuh"
@@ -16,134 +14,236 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 
-// Order-preserving key of a choice value; 0 for NaN and -inf (not available),
-// one key for both zeros.
-__device__ __forceinline__ uint32_t choice_key(float u) {
-  const uint32_t b = __float_as_uint(u + 0.f);
-  const uint32_t k = (b & 0x80000000u) ? ~b : b | 0x80000000u;
-  return u > neg_inf() ? k : 0u;
-}
-__device__ __forceinline__ float key_value(uint32_t k) {
-  return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
+__device__ __forceinline__ float redux_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
 }
 
+__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
 // exp(z - m) of an expert that is available, m >= z; NaN stays NaN.
 __device__ __forceinline__ float softmax_term(float z, float m) { return z == neg_inf() ? 0.f : expf(z - m); }
 
-// Lane holds experts [lane * NV, lane * NV + NV); those past E are not available.
+// A lane's NV values of a row, from e0 = lane * NV; `fill` past the row's end.
+// `packs`: whole 16-byte packs (NV values are some, they lie on their boundary
+// and no lane's are cut off by the end).
+template <typename T, int NV>
+__device__ __forceinline__ void load_lane(const T* row, int e0, int E, bool packs, float fill, float (&z)[NV]) {
+  constexpr int N = Pack<T>::kN;
+  if constexpr (NV % N == 0) {
+    if (packs) {
+      if (e0 < E) {
+#pragma unroll
+        for (int p = 0; p < NV / N; ++p) {
+          float f[N];
+          unpack(load16(row + e0 + p * N), f, T());
+#pragma unroll
+          for (int q = 0; q < N; ++q) z[p * N + q] = f[q];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) z[i] = fill;
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) z[i] = e0 + i < E ? to_f32(row[e0 + i]) : fill;
+}
+
+// Whether rows of E values, ld apart, can be taken in packs by lanes of NV values.
+template <typename T, int NV>
+bool in_packs(const void* p, int64_t E, int64_t ld) {
+  return NV % Pack<T>::kN == 0 && E % NV == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 &&
+         ld % Pack<T>::kN == 0;
+}
+
+// The two largest of a group's choice values.
+struct Top2 {
+  float a = neg_inf(), b = neg_inf();
+  __device__ __forceinline__ void add(float v) {
+    b = fmaxf(b, fminf(a, v));
+    a = fmaxf(a, v);
+  }
+  __device__ __forceinline__ void merge(float oa, float ob) {
+    b = fmaxf(fminf(a, oa), fmaxf(b, ob));
+    a = fmaxf(a, oa);
+  }
+};
+
+// The k largest: a bound first, the k-th largest of the lanes' own maxima, which
+// at least k values reach; the few that do (k to k + 3 of 256, as a rule) go one
+// to a lane, which counts those before it.  That is 160 instructions where
+// taking them one by one from all lanes' values, each time with a new maximum
+// a lane, is 230; more than 32 (equal values) are taken that way.
+
 template <typename T, int NV, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads) route_kernel(const RouteJob j) {
-  extern __shared__ int32_t shared[];  // loads [E]; with groups, keys [kWarps][E]
-  int32_t* hist = shared;
+__global__ void __launch_bounds__(kThreads) route_kernel(const RouteJob j, const bool packs) {
+  extern __shared__ int32_t hist[];  // loads [E]; with groups, choice values [kWarps][E]
+  __shared__ float2 all_keys[kWarps][32];
+  __shared__ float all_logits[kWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int E = static_cast<int>(j.E), k = j.cfg.k, e0 = lane * NV;
-  const bool grouped = j.cfg.top_groups < j.cfg.groups;
-  uint32_t* keys = reinterpret_cast<uint32_t*>(shared + E) + warp * E;
+  const int G = j.cfg.groups, per = E / G;
+  const bool grouped = j.cfg.top_groups < G;
+  // groups of a power of two of lanes: by shuffles; others through shared memory
+  const int group_lanes = per % NV == 0 ? per / NV : 0;
+  const bool shuffles = group_lanes > 0 && (group_lanes & (group_lanes - 1)) == 0;
+  float* values = reinterpret_cast<float*>(hist + E) + warp * E;
+  float2* keys = all_keys[warp];
+  float* logits = all_logits[warp];
   for (int e = threadIdx.x; e < E; e += kThreads) hist[e] = 0;
+  float bias[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) bias[i] = j.bias != nullptr && e0 + i < E ? j.bias[e0 + i] : 0.f;
   __syncthreads();
   uint32_t bits = 0;
   for (int64_t t = blockIdx.x * int64_t(kWarps) + warp; t < j.T; t += int64_t(gridDim.x) * kWarps) {
-    const T* row = static_cast<const T*>(j.logits) + t * j.ld;
-    float z[NV];
-    uint32_t key[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) z[i] = e0 + i < E ? to_f32(row[e0 + i]) : neg_inf();
-    float zmax = neg_inf();
+    float z[NV], u[NV];
+    load_lane<T, NV>(static_cast<const T*>(j.logits) + t * j.ld, e0, E, packs, neg_inf(), z);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const float b = j.bias != nullptr && e0 + i < E ? j.bias[e0 + i] : 0.f;
-      float u = kSigmoid ? 1.f / (1.f + expf(-z[i])) : z[i];
-      u = u + b;
-      if (z[i] == neg_inf()) {
-        u = neg_inf();
-      } else if (u != u || (!kSigmoid && z[i] == -neg_inf())) {
+      const float v = (kSigmoid ? sigmoid(z[i]) : z[i]) + bias[i];
+      const bool faulty = z[i] != neg_inf() && (v != v || (!kSigmoid && z[i] == -neg_inf()));
+      if (faulty) {
         bits |= SF_ST_NONFINITE;
-        u = z[i] = neg_inf();
+        z[i] = neg_inf();
       }
-      key[i] = choice_key(u);
-      zmax = fmaxf(zmax, z[i]);
+      u[i] = z[i] == neg_inf() ? neg_inf() : v;
     }
     if (grouped) {
-      const int G = j.cfg.groups, per = E / G;
-      __syncwarp();
+      Top2 best;
+      float value = neg_inf();  // of this lane's group
+      if (shuffles) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (e0 + i < E) keys[e0 + i] = key[i];
-      __syncwarp();
-      uint32_t gk = 0;  // this lane's group
-      if (lane < G) {
-        uint32_t a = 0, b = 0;
-        for (int i = 0; i < per; ++i) {
-          const uint32_t v = keys[lane * per + i];
-          b = max(b, min(a, v));
-          a = max(a, v);
-        }
-        if (a != 0) gk = choice_key(j.cfg.group_top > 1 && b != 0 ? key_value(a) + key_value(b) : key_value(a));
+        for (int i = 0; i < NV; ++i) best.add(u[i]);
+        for (int o = 1; o < group_lanes; o <<= 1)
+          best.merge(__shfl_xor_sync(kFull, best.a, o), __shfl_xor_sync(kFull, best.b, o));
+      } else {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (e0 + i < E) values[e0 + i] = u[i];
+        __syncwarp();
+        if (lane < G)
+          for (int i = 0; i < per; ++i) best.add(values[lane * per + i]);
       }
-      // a group is kept if fewer than top_groups others come before it
+      value = j.cfg.group_top > 1 && best.b != neg_inf() ? best.a + best.b : best.a;
+      // a group is kept if fewer than top_groups come before it
+      const int mine = shuffles ? lane / group_lanes : lane, stride = shuffles ? group_lanes : 1;
       int before = 0;
       for (int g = 0; g < G; ++g) {
-        const uint32_t o = __shfl_sync(kFull, gk, g);
-        before += o > gk || (o == gk && g < lane);
+        const float o = __shfl_sync(kFull, value, g * stride);
+        before += o > value || (o == value && g < mine);
       }
-      const uint32_t kept = __ballot_sync(kFull, lane < G && before < j.cfg.top_groups);
+      const bool keep = before < j.cfg.top_groups;
+      if (shuffles) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (e0 + i < E && !((kept >> ((e0 + i) / per)) & 1u)) key[i] = 0;
+        for (int i = 0; i < NV; ++i) u[i] = keep ? u[i] : neg_inf();
+      } else {
+        const uint32_t kept = __ballot_sync(kFull, lane < G && keep);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (e0 + i < E && !((kept >> ((e0 + i) / per)) & 1u)) u[i] = neg_inf();
+      }
     }
-    // the chosen, one by one; lane c keeps the c-th
-    int mine = -1;
-    float mine_z = 0.f;
+    // the bound
+    float top = u[0];
+#pragma unroll
+    for (int i = 1; i < NV; ++i) top = fmaxf(top, u[i]);
+    float bound = neg_inf();
     for (int c = 0; c < k; ++c) {
-      uint32_t best = 0;
-      int at = 0;
+      bound = redux_max(top);
+      if (bound == neg_inf()) break;
+      if (lane == __ffs(static_cast<int>(__ballot_sync(kFull, top == bound))) - 1) top = neg_inf();
+    }
+    // the values that reach it
+    int n = 0;
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (key[i] > best) {
-          best = key[i];
-          at = i;
+    for (int i = 0; i < NV; ++i) {
+      const bool in = u[i] >= bound && u[i] != neg_inf();
+      const uint32_t b = __ballot_sync(kFull, in);
+      const int at = n + __popc(b & ((1u << lane) - 1u));
+      if (in && at < 32) {
+        keys[at] = make_float2(u[i], __int_as_float(e0 + i));
+        logits[at] = z[i];
+      }
+      n += __popc(b);
+    }
+    int e = -1, rank = 32;
+    float zc = neg_inf();
+    if (n <= 32) {
+      __syncwarp();
+      if (lane < n) {
+        const float2 own = keys[lane];
+        e = __float_as_int(own.y);
+        zc = logits[lane];
+        rank = 0;
+        for (int i = 0; i < n; ++i) {
+          const float2 o = keys[i];
+          rank += o.x > own.x || (o.x == own.x && __float_as_int(o.y) < e);
         }
-      const uint32_t top = __reduce_max_sync(kFull, best);
-      if (top == 0) break;
-      const int owner = __ffs(__ballot_sync(kFull, best == top)) - 1;
-      float zc = 0.f;
+      }
+      __syncwarp();
+    } else {
+      for (int c = 0; c < k; ++c) {
+        float m = u[0];
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (i == at) {
-          zc = z[i];
-          if (lane == owner) key[i] = 0;
+        for (int i = 1; i < NV; ++i) m = fmaxf(m, u[i]);
+        const float best = redux_max(m);
+        if (best == neg_inf()) break;
+        const int owner = __ffs(static_cast<int>(__ballot_sync(kFull, m == best))) - 1;
+        int at = e0;
+        float za = 0.f;
+        bool found = lane != owner;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (!found && u[i] == best) {
+            found = true;
+            at = e0 + i;
+            za = z[i];
+            u[i] = neg_inf();
+          }
+        at = __shfl_sync(kFull, at, owner);
+        za = __shfl_sync(kFull, za, owner);
+        if (lane == c) {
+          e = at;
+          zc = za;
+          rank = c;
         }
-      const int e = __shfl_sync(kFull, e0 + at, owner);
-      zc = __shfl_sync(kFull, zc, owner);
-      if (lane == c) {
-        mine = e;
-        mine_z = zc;
       }
     }
+    const bool chosen = rank < k;
     // weights
     float w = 0.f;
     if (kSigmoid) {
-      w = mine >= 0 ? 1.f / (1.f + expf(-mine_z)) : 0.f;
+      w = chosen ? sigmoid(zc) : 0.f;
+    } else if (j.cfg.renorm) {
+      const float m = redux_max(chosen ? zc : neg_inf());
+      w = chosen ? expf(zc - m) : 0.f;
     } else {
-      float m = zmax;
-      if (j.cfg.renorm) m = mine >= 0 ? mine_z : neg_inf();
-      m = warp_max(m);
-      w = mine >= 0 ? expf(mine_z - m) : 0.f;
-      if (!j.cfg.renorm) {
-        float s = 0.f;
+      float m = z[0], s = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) s += softmax_term(z[i], m);
-        w = w / warp_sum(s);
-      }
+      for (int i = 1; i < NV; ++i) m = fmaxf(m, z[i]);
+      m = redux_max(m);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) s += softmax_term(z[i], m);
+      s = warp_sum(s);
+      w = chosen ? expf(zc - m) / s : 0.f;
     }
     if (j.cfg.renorm) {
       const float s = warp_sum(w);
       w = s > 0.f ? w / s : 0.f;
     }
-    if (lane < k) {
-      j.index[t * k + lane] = mine;
-      j.weight[t * k + lane] = mine >= 0 ? w * j.cfg.scale : 0.f;
-      if (mine >= 0) atomicAdd(hist + mine, 1);
+    if (chosen) {
+      j.index[t * k + rank] = e;
+      j.weight[t * k + rank] = w * j.cfg.scale;
+      atomicAdd(hist + e, 1);
+    }
+    const int found = __popc(__ballot_sync(kFull, chosen));
+    if (lane >= found && lane < k) {  // fewer experts than k
+      j.index[t * k + lane] = -1;
+      j.weight[t * k + lane] = 0.f;
     }
   }
   report(j.status, bits);
@@ -166,7 +266,7 @@ cudaError_t launch_route_nv(const RouteJob& j, bool after_clear, cudaStream_t st
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ctas, int64_t(sm_count()) * 8)));
   count_launch();
   const auto kern = j.cfg.score == SF_SCORE_SIGMOID ? route_kernel<T, NV, true> : route_kernel<T, NV, false>;
-  return launch_after(kern, grid, dim3(kThreads), smem, stream, after_clear, j);
+  return launch_after(kern, grid, dim3(kThreads), smem, stream, after_clear, j, in_packs<T, NV>(j.logits, j.E, j.ld));
 }
 
 template <typename T>
@@ -180,15 +280,20 @@ cudaError_t launch_route_t(const RouteJob& j, bool after_clear, cudaStream_t str
   return launch_route_nv<T, 32>(j, after_clear, stream);
 }
 
-// Gradient: a warp a token; the row is put together in shared memory.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteGradJob j) {
-  extern __shared__ float rows[];
+// Gradient: the chosen experts' lanes put their own values (or, where all
+// experts have a gradient, their upstream gradients) into a row of zeros in
+// shared memory, from which every lane takes its NV.
+template <typename T, int NV>
+__global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteGradJob j, const bool packs) {
+  constexpr int N = Pack<T>::kN;
+  extern __shared__ __align__(16) float rows[];  // [kWarps][32 * NV]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int E = static_cast<int>(j.E), k = j.cfg.k;
-  float* d = rows + warp * E;
-  const bool sigmoid = j.cfg.score == SF_SCORE_SIGMOID, dense = !sigmoid && !j.cfg.renorm;
+  const int E = static_cast<int>(j.E), k = j.cfg.k, e0 = lane * NV;
+  float* d = rows + warp * (32 * NV);
+  const bool sigmoids = j.cfg.score == SF_SCORE_SIGMOID, dense = !sigmoids && !j.cfg.renorm;
   uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) d[i * 32 + lane] = 0.f;
   for (int64_t t = blockIdx.x * int64_t(kWarps) + warp; t < j.T; t += int64_t(gridDim.x) * kWarps) {
     const T* row = static_cast<const T*>(j.logits) + t * j.ld;
     int e = -1;
@@ -204,9 +309,9 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteGradJob
         z = to_f32(row[e]);
       }
     }
-    float m = z, g = 0.f, s = 0.f, inner = 0.f;
-    if (sigmoid) {
-      const float p = e >= 0 ? 1.f / (1.f + expf(-z)) : 0.f;
+    float g = 0.f, all[NV], s = 0.f, inner = 0.f;
+    if (sigmoids) {
+      const float p = e >= 0 ? sigmoid(z) : 0.f;
       const float slope = e >= 0 ? p * (1.f / (1.f + expf(z))) : 0.f;
       if (j.cfg.renorm) {
         s = warp_sum(p);
@@ -216,41 +321,83 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteGradJob
         g = slope * dw;
       }
     } else {
-      if (dense)
-        for (int i = lane; i < E; i += 32) m = fmaxf(m, to_f32(row[i]));
+      float m = z;
+      if (dense) {
+        load_lane<T, NV>(row, e0, E, packs, neg_inf(), all);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) m = fmaxf(m, all[i]);
+      }
       m = warp_max(m);
       const float q = softmax_term(z, m);
       s = q;
       if (dense) {
         s = 0.f;
-        for (int i = lane; i < E; i += 32) s += softmax_term(to_f32(row[i]), m);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          all[i] = softmax_term(all[i], m);
+          s += all[i];
+        }
       }
       s = warp_sum(s);
       inner = warp_sum(q * dw);
       if (!finite(s)) bits |= SF_ST_NONFINITE;
       s = finite(s) && s > 0.f ? 1.f / s : 0.f;  // no gradient without a distribution
       inner *= s;
-      g = s > 0.f ? q * s * (dw - inner) : 0.f;
+      g = dense ? dw : s > 0.f ? q * s * (dw - inner) : 0.f;
     }
-    __syncwarp();
-    for (int i = lane; i < E; i += 32)
-      d[i] = dense && s > 0.f ? -softmax_term(to_f32(row[i]), m) * s * inner : 0.f;
-    __syncwarp();
+    __syncwarp();  // the row is zeros
     if (e >= 0) d[e] = g;
     __syncwarp();
+    float v[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      v[i] = d[e0 + i];
+      if (dense) v[i] = s > 0.f ? all[i] * s * (v[i] - inner) : 0.f;
+      v[i] *= j.cfg.scale;
+    }
+    __syncwarp();
+    if (e >= 0) d[e] = 0.f;
     T* out = static_cast<T*>(j.dlogits) + t * j.ldd;
-    for (int i = lane; i < E; i += 32) out[i] = from_f32<T>(d[i] * j.cfg.scale);
+    if constexpr (NV % N == 0) {
+      if (packs) {
+        if (e0 < E) {
+#pragma unroll
+          for (int p = 0; p < NV / N; ++p) {
+            float f[N];
+#pragma unroll
+            for (int q = 0; q < N; ++q) f[q] = v[p * N + q];
+            store16(out + e0 + p * N, pack(f, T()));
+          }
+        }
+        continue;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (e0 + i < E) out[e0 + i] = from_f32<T>(v[i]);
   }
   report(j.status, bits);
 }
 
-template <typename T>
-cudaError_t launch_grad_t(const RouteGradJob& j, cudaStream_t stream) {
+template <typename T, int NV>
+cudaError_t launch_grad_nv(const RouteGradJob& j, cudaStream_t stream) {
   const int64_t ctas = (j.T + kWarps - 1) / kWarps;
   const int grid = static_cast<int>(std::min<int64_t>(ctas, int64_t(sm_count()) * 8));
+  const bool packs = in_packs<T, NV>(j.logits, j.E, j.ld) && in_packs<T, NV>(j.dlogits, j.E, j.ldd);
   count_launch();
-  route_grad_kernel<T><<<grid, kThreads, size_t(j.E) * 4 * kWarps, stream>>>(j);
+  route_grad_kernel<T, NV><<<grid, kThreads, size_t(kWarps) * 32 * NV * 4, stream>>>(j, packs);
   return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_grad_t(const RouteGradJob& j, cudaStream_t stream) {
+  const int64_t nv = (j.E + 31) / 32;
+  if (nv <= 1) return launch_grad_nv<T, 1>(j, stream);
+  if (nv <= 2) return launch_grad_nv<T, 2>(j, stream);
+  if (nv <= 4) return launch_grad_nv<T, 4>(j, stream);
+  if (nv <= 8) return launch_grad_nv<T, 8>(j, stream);
+  if (nv <= 16) return launch_grad_nv<T, 16>(j, stream);
+  return launch_grad_nv<T, 32>(j, stream);
 }
 
 }  // namespace

@@ -111,7 +111,7 @@ def _load():
     L.sf_label_windows_workspace_size.restype = ctypes.c_size_t
     L.sf_rank_workspace_size.argtypes = [I, I, I]
     L.sf_rank_workspace_size.restype = ctypes.c_size_t
-    L.sf_grad_workspace_size.argtypes = [P, I]
+    L.sf_grad_workspace_size.argtypes = [I]
     L.sf_grad_workspace_size.restype = ctypes.c_size_t
     L.sf_policy_loss_workspace_size.argtypes = [I, I]
     L.sf_policy_loss_workspace_size.restype = ctypes.c_size_t
@@ -648,6 +648,9 @@ def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=No
     if stats is None:
         stats = _empty((4,), torch.float32, logits)
         made.append(stats)
+    if workspace is None:
+        workspace = _empty((int(_lib.sf_policy_loss_workspace_size(N, V)),), torch.uint8, logits)
+        made.append(workspace)
     if dlogits is None and grad:
         dlogits = _empty((N, V), logits.dtype, logits)
         made.append(dlogits)
@@ -659,9 +662,6 @@ def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=No
         n, m, ldd = _rows(dlogits, "dlogits")
         if (n, m) != (N, V) or dlogits.dtype != logits.dtype:
             raise ValueError("dlogits must have logits' shape and type")
-    if workspace is None:
-        workspace = torch.empty(int(_lib.sf_policy_loss_workspace_size(N, V)), dtype=torch.uint8, device=logits.device)
-        made.append(workspace)
     _hold(made, stream)
     cfg = PolicyConfig(clip[0], clip[1], kl_coef, inv_temperature)
     _check(_lib.sf_policy_loss(_p(logits), _DTYPES[logits.dtype], N, V, ld, _p(target), _p(old_logp), _p(ref_logp),
@@ -748,13 +748,20 @@ class GradNorm:
     tensor_norm: Optional[torch.Tensor]
 
 
+# as C calls over a whole list: half the time of a loop (0.2 us a tensor)
+_is_cuda, _dtype_of = torch.Tensor.is_cuda.__get__, torch.Tensor.dtype.__get__
+
+
 def _tensor_list(tensors, name: str):
     """Host arrays (pointers, sizes, types) of contiguous CUDA tensors."""
-    for t in tensors:
-        if not t.is_cuda or t.dtype not in _DTYPES or not t.is_contiguous():
-            raise TypeError(f"{name} must be contiguous CUDA tensors of float32, bfloat16 or float16")
-    return (array("Q", [t.data_ptr() for t in tensors]), array("q", [t.numel() for t in tensors]),
-            array("i", [_DTYPES[t.dtype] for t in tensors]))
+    try:
+        types = array("i", map(_DTYPES.__getitem__, map(_dtype_of, tensors)))
+        fine = all(map(_is_cuda, tensors)) and all(map(torch.Tensor.is_contiguous, tensors))
+    except (KeyError, TypeError):
+        fine = False
+    if not fine:
+        raise TypeError(f"{name} must be contiguous CUDA tensors of float32, bfloat16 or float16")
+    return array("Q", map(torch.Tensor.data_ptr, tensors)), array("q", map(torch.Tensor.numel, tensors)), types
 
 
 def _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, workspace, status, stream):
@@ -779,7 +786,7 @@ def _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, worksp
     _vec(tensor_norm, n, torch.float32, "tensor_norm")
     at = lambda a: a.buffer_info()[0]  # noqa: E731
     if workspace is None:
-        workspace = new(int(_lib.sf_grad_workspace_size(at(numel), n)), torch.uint8)
+        workspace = new(int(_lib.sf_grad_workspace_size(n)), torch.uint8)
     if max_norm is None:
         _hold(made, stream)
         _check(_lib.sf_grad_norm(at(ptr), at(numel), at(dtype), n, _p(norm), _p(tensor_norm), _p(workspace),
