@@ -638,30 +638,30 @@ def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=No
     _vec(ref_logp, N, torch.float32, "ref_logp")
     _vec(weight, N, torch.float32, "weight")
     _vec(grad_out, 1, torch.float32, "grad_out")
-    made = []
-    if logp is None and "logp" in want:
-        logp = _empty((N,), torch.float32, logits)
-        made.append(logp)
-    if token_loss is None and "token_loss" in want:
-        token_loss = _empty((N,), torch.float32, logits)
-        made.append(token_loss)
-    if stats is None:
-        stats = _empty((4,), torch.float32, logits)
-        made.append(stats)
-    if workspace is None:
-        workspace = _empty((int(_lib.sf_policy_loss_workspace_size(N, V)),), torch.uint8, logits)
-        made.append(workspace)
-    if dlogits is None and grad:
-        dlogits = _empty((N, V), logits.dtype, logits)
-        made.append(dlogits)
-    _vec(logp, N, torch.float32, "logp")
-    _vec(token_loss, N, torch.float32, "token_loss")
-    _vec(stats, 4, torch.float32, "stats")
+    device, made = logits.device, []
+
+    def new(n, dtype=torch.float32):
+        made.append(torch.empty(n, dtype=dtype, device=device))
+        return made[-1]
+
+    if logp is not None:
+        _vec(logp, N, torch.float32, "logp")
+    elif "logp" in want:
+        logp = new(N)
+    if token_loss is not None:
+        _vec(token_loss, N, torch.float32, "token_loss")
+    elif "token_loss" in want:
+        token_loss = new(N)
+    stats = new(4) if stats is None else _vec(stats, 4, torch.float32, "stats")
     ldd = V
     if dlogits is not None:
         n, m, ldd = _rows(dlogits, "dlogits")
         if (n, m) != (N, V) or dlogits.dtype != logits.dtype:
             raise ValueError("dlogits must have logits' shape and type")
+    elif grad:
+        dlogits = new((N, V), logits.dtype)
+    if workspace is None:
+        workspace = new(_lib.sf_policy_loss_workspace_size(N, V), torch.uint8)
     _hold(made, stream)
     cfg = PolicyConfig(clip[0], clip[1], kl_coef, inv_temperature)
     _check(_lib.sf_policy_loss(_p(logits), _DTYPES[logits.dtype], N, V, ld, _p(target), _p(old_logp), _p(ref_logp),
@@ -697,18 +697,19 @@ def sf_route_experts(logits, k: int, bias=None, score: str = "softmax", groups: 
     _vec(bias, E, torch.float32, "bias")
     if accumulate and load is None:
         raise ValueError("accumulate adds to a load that the caller gives")
-    made = []
+    device, made = logits.device, []
 
-    def new(shape, dt):
-        made.append(_empty(shape, dt, logits))
+    def new(shape, dtype):
+        made.append(torch.empty(shape, dtype=dtype, device=device))
         return made[-1]
 
     slots = T * k if k > 0 else 0  # a bad k is the library's to refuse
     index = new((T, max(k, 0)), torch.int32) if index is None else _vec(index, slots, torch.int32, "index")
     weight = new((T, max(k, 0)), torch.float32) if weight is None else _vec(weight, slots, torch.float32, "weight")
-    if load is None and "load" in want:
-        load = new((E,), torch.int32)
-    _vec(load, E, torch.int32, "load")
+    if load is not None:
+        _vec(load, E, torch.int32, "load")
+    elif "load" in want:
+        load = new(E, torch.int32)
     _hold(made, stream)
     cfg = RouteConfig(k, _score(score), groups, top_groups, group_top, 1 if renorm else 0, scale)
     _check(_lib.sf_route_experts(_p(logits), _DTYPES[logits.dtype], T, E, ld, _p(bias), ctypes.byref(cfg), _p(index),
@@ -781,12 +782,13 @@ def _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, worksp
         return made[-1]
 
     norm = new(1) if norm is None else _vec(norm, 1, torch.float32, "norm")
-    if tensor_norm is None and per_tensor:
+    if tensor_norm is not None:
+        _vec(tensor_norm, n, torch.float32, "tensor_norm")
+    elif per_tensor:
         tensor_norm = new(n)
-    _vec(tensor_norm, n, torch.float32, "tensor_norm")
     at = lambda a: a.buffer_info()[0]  # noqa: E731
     if workspace is None:
-        workspace = new(int(_lib.sf_grad_workspace_size(n)), torch.uint8)
+        workspace = new(_lib.sf_grad_workspace_size(n), torch.uint8)
     if max_norm is None:
         _hold(made, stream)
         _check(_lib.sf_grad_norm(at(ptr), at(numel), at(dtype), n, _p(norm), _p(tensor_norm), _p(workspace),
