@@ -14,6 +14,7 @@
 // or more than 32 values are gathered, the token's values are all computed
 // exactly, and taken one by one if there are too many equal ones.
 #include <algorithm>
+#include <type_traits>
 
 #include "sf_float.cuh"
 #include "sf_launch.h"
@@ -83,33 +84,35 @@ __device__ __forceinline__ void store_value(void* p, int64_t i, int dtype, float
     static_cast<__half*>(p)[i] = from_f32<__half>(v);
 }
 
-template <typename T, int NV>
-__device__ __forceinline__ void load_packs(const T* row, int e0, int E, float (&z)[NV]) {
+// NV values of a row at p[at], a lane's, as packs or one by one: pack q holds the
+// lane's values q N .. q N + N - 1 and starts at element first(q, N), value i is
+// element first(i, 1); elements from `end` on are 0, and are not written.  Packs
+// are whole where they are used (see in_packs).
+template <typename T, int NV, typename First>
+__device__ __forceinline__ void load_packs(const T* row, int end, const First& first, float (&z)[NV]) {
   constexpr int N = Pack<T>::kN;
   if constexpr (NV % N == 0) {
 #pragma unroll
     for (int p = 0; p < NV / N; ++p) {
       float f[N];
-      unpack(e0 + p * N < E ? *reinterpret_cast<const uint4*>(row + e0 + p * N) : same4(0u), f, T());
+      unpack(first(p, N) < end ? *reinterpret_cast<const uint4*>(row + first(p, N)) : same4(0u), f, T());
 #pragma unroll
       for (int q = 0; q < N; ++q) z[p * N + q] = f[q];
     }
   }
 }
-// A lane's NV values of the row that starts at element `at`, from e0; 0 past the
-// row's end.  `packs`: in 16-byte packs (see in_packs).
-template <int NV>
-__device__ __forceinline__ void load_lane(const void* p, int64_t at, int dtype, int e0, int E, bool packs,
-                                          float (&z)[NV]) {
-  if (packs && dtype == SF_F32) return load_packs(static_cast<const float*>(p) + at, e0, E, z);
-  if (packs && dtype == SF_BF16) return load_packs(static_cast<const __nv_bfloat16*>(p) + at, e0, E, z);
-  if (packs) return load_packs(static_cast<const __half*>(p) + at, e0, E, z);
+template <int NV, typename First>
+__device__ __forceinline__ void load_lane(const void* p, int64_t at, int dtype, int end, bool packs,
+                                          const First& first, float (&z)[NV]) {
+  if (packs && dtype == SF_F32) return load_packs(static_cast<const float*>(p) + at, end, first, z);
+  if (packs && dtype == SF_BF16) return load_packs(static_cast<const __nv_bfloat16*>(p) + at, end, first, z);
+  if (packs) return load_packs(static_cast<const __half*>(p) + at, end, first, z);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) z[i] = e0 + i < E ? load_value(p, at + e0 + i, dtype) : 0.f;
+  for (int i = 0; i < NV; ++i) z[i] = first(i, 1) < end ? load_value(p, at + first(i, 1), dtype) : 0.f;
 }
 
-template <typename T, int NV>
-__device__ __forceinline__ void store_packs(T* row, int e0, int E, const float (&v)[NV]) {
+template <typename T, int NV, typename First>
+__device__ __forceinline__ void store_packs(T* row, int end, const First& first, const float (&v)[NV]) {
   constexpr int N = Pack<T>::kN;
   if constexpr (NV % N == 0) {
 #pragma unroll
@@ -117,19 +120,19 @@ __device__ __forceinline__ void store_packs(T* row, int e0, int E, const float (
       float f[N];
 #pragma unroll
       for (int q = 0; q < N; ++q) f[q] = v[p * N + q];
-      if (e0 + p * N < E) store16(row + e0 + p * N, pack(f, T()));
+      if (first(p, N) < end) store16(row + first(p, N), pack(f, T()));
     }
   }
 }
-template <int NV>
-__device__ __forceinline__ void store_lane(void* p, int64_t at, int dtype, int e0, int E, bool packs,
+template <int NV, typename First>
+__device__ __forceinline__ void store_lane(void* p, int64_t at, int dtype, int end, bool packs, const First& first,
                                            const float (&v)[NV]) {
-  if (packs && dtype == SF_F32) return store_packs(static_cast<float*>(p) + at, e0, E, v);
-  if (packs && dtype == SF_BF16) return store_packs(static_cast<__nv_bfloat16*>(p) + at, e0, E, v);
-  if (packs) return store_packs(static_cast<__half*>(p) + at, e0, E, v);
+  if (packs && dtype == SF_F32) return store_packs(static_cast<float*>(p) + at, end, first, v);
+  if (packs && dtype == SF_BF16) return store_packs(static_cast<__nv_bfloat16*>(p) + at, end, first, v);
+  if (packs) return store_packs(static_cast<__half*>(p) + at, end, first, v);
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    if (e0 + i < E) store_value(p, at + e0 + i, dtype, v[i]);
+    if (first(i, 1) < end) store_value(p, at + first(i, 1), dtype, v[i]);
 }
 // Whether rows of E values, ld apart, are whole packs on their boundaries, for lanes of NV values.
 bool in_packs(const void* p, int dtype, int64_t E, int64_t ld, int NV) {
@@ -150,34 +153,41 @@ struct Top2 {
   }
 };
 
-constexpr int kGathered = 32;  // values of a token that are ranked
-
-// Shared memory of a warp: a token's gathered values each.
+// Values of a token that are ranked, kRounds a lane.
 template <int LPT>
-struct Gathered {
-  float2 key[32 / LPT][kGathered];  // (choice value, expert)
+struct Gather {
+  static constexpr int kRounds = LPT == 8 ? 4 : LPT == 16 ? 3 : 2, kMost = LPT * kRounds;
+};
+
+// How a token's experts lie in its lanes: a group's in `lanes` lanes (a power of
+// two), `each` consecutive ones a lane.
+struct RouteShape {
+  int lanes, each;
+  bool packs;
 };
 
 template <int NV, int LPT, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const RouteJob j, const bool packs) {
+__global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const RouteJob j, const RouteShape shape) {
   constexpr int kTokens = 32 / LPT;  // of a warp
-  constexpr int kRounds = kGathered / LPT;
+  constexpr int kRounds = Gather<LPT>::kRounds, kGathered = Gather<LPT>::kMost;
   constexpr int kPad = NV % 4 == 0 ? 4 : 0;  // of a lane's biases, which then lie in banks of their own
-  extern __shared__ __align__(16) float dynamic[];  // biases, loads [E]; where needed, choice values [kWarps * kTokens][E]
-  __shared__ Gathered<LPT> gathered[kWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = lane & (LPT - 1), first = lane - slot;
-  const int E = static_cast<int>(j.E), k = j.cfg.k, e0 = slot * NV, dtype = j.dtype;
-  const int G = j.cfg.groups, per = E / G, top_groups = j.cfg.top_groups;
-  const bool grouped = top_groups < G;
-  // groups of a power of two of whole lanes: by shuffles; others through shared memory
-  const int group_lanes = per % NV == 0 ? per / NV : 0;
-  const bool shuffles = group_lanes > 0 && (group_lanes & (group_lanes - 1)) == 0;
+  extern __shared__ __align__(16) float dynamic[];  // biases, loads [E]
+  __shared__ float2 all_keys[kWarps][kTokens][kGathered];  // (choice value, expert)
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = lane & (LPT - 1), first_lane = lane - slot;
+  const int E = static_cast<int>(j.E), k = j.cfg.k, dtype = j.dtype, top_groups = j.cfg.top_groups;
+  const bool grouped = top_groups < j.cfg.groups;
+  const int G = grouped ? j.cfg.groups : 1, per = E / G;
+  const int group = slot / shape.lanes, within = (slot & (shape.lanes - 1)) * shape.each;
+  const int e0 = group * per + within;  // this lane's first expert, and how many it has
+  const int count = group < G ? max(0, min(shape.each, per - within)) : 0;
+  const auto consecutive = [&](int p, int n) { return e0 + p * n; };
   float* biases = dynamic;
   int32_t* hist = reinterpret_cast<int32_t*>(biases + LPT * (NV + kPad));
-  float* values = reinterpret_cast<float*>(hist + E) + (warp * kTokens + lane / LPT) * E;
-  float2* keys = gathered[warp].key[lane / LPT];
-  for (int e = threadIdx.x; e < LPT * NV; e += kThreads)  // past the last expert: not available
-    biases[e + e / NV * kPad] = e >= E ? neg_inf() : j.bias != nullptr ? j.bias[e] : 0.f;
+  float2* keys = all_keys[warp][lane / LPT];
+  if (threadIdx.x < LPT) {  // a token's lanes, each its own; not available past its last expert
+    for (int i = 0; i < NV; ++i)
+      biases[slot * (NV + kPad) + i] = i >= count ? neg_inf() : j.bias != nullptr ? j.bias[e0 + i] : 0.f;
+  }
   for (int e = threadIdx.x; e < E; e += kThreads) hist[e] = 0;
   __syncthreads();
   const float* bias = biases + slot * (NV + kPad);
@@ -185,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
   bool odd_bias = false;  // biases that are not finite
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    if (e0 + i < E) {
+    if (i < count) {
       odd_bias |= !finite(bias[i]);
       if (finite(bias[i])) error = fmaxf(error, kSigmoidError + fabsf(bias[i]) * 0x1p-22f);  // its sums' roundings
     }
@@ -207,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
     for (bool exact = !kSigmoid;; exact = true) {
       float u[NV], odd = 0.f;
       Top2 best;
-      load_lane<NV>(j.logits, t * j.ld, dtype, e0, real ? E : 0, packs, u);
+      load_lane<NV>(j.logits, t * j.ld, dtype, real ? e0 + count : 0, shape.packs, consecutive, u);
       if (!exact) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -227,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
         best = Top2();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          const float z = real && e0 + i < E ? load_value(j.logits, t * j.ld + e0 + i, dtype) : neg_inf();
+          const float z = real && i < count ? load_value(j.logits, t * j.ld + e0 + i, dtype) : neg_inf();
           if (z == neg_inf()) {
             u[i] = neg_inf();
           } else if (u[i] != u[i] || (!kSigmoid && z == -neg_inf())) {
@@ -242,50 +252,19 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
       bool live = real;                                // whether this lane's group may be chosen from
       if (grouped) {
         // a group is kept if fewer than top_groups come before it
-        const auto kept = [&](float value, int mine, const auto& other) {
-          int before = 0, close = 0;  // for certain, perhaps
-          for (int g = 0; g < G; ++g) {
-            const float o = other(g);
-            const bool tie = exact && o == value && g < mine;
-            before += o > value + 2.f * margin || tie;
-            close += (g != mine && o > value - 2.f * margin) || tie;
-          }
-          open |= value != neg_inf() && before < top_groups && close >= top_groups;
-          return before < top_groups;
-        };
-        if (shuffles) {
-          Top2 all = best;
-          for (int o = 1; o < group_lanes; o <<= 1)
-            all.merge(__shfl_xor_sync(kFull, all.a, o), __shfl_xor_sync(kFull, all.b, o));
-          const float value = j.cfg.group_top > 1 && all.b != neg_inf() ? all.a + all.b : all.a;
-          live &= kept(value, slot / group_lanes,
-                       [&](int g) { return __shfl_sync(kFull, value, first + g * group_lanes); });
-        } else {
-          __syncwarp();
-#pragma unroll
-          for (int i = 0; i < NV; ++i)
-            if (e0 + i < E) values[e0 + i] = u[i];
-          __syncwarp();
-          for (int g = slot; g < G; g += LPT) {
-            Top2 b;
-            for (int i = 0; i < per; ++i) b.add(values[g * per + i]);
-            // in the group's first place, which only this lane has read
-            values[g * per] = j.cfg.group_top > 1 && b.b != neg_inf() ? b.a + b.b : b.a;
-          }
-          __syncwarp();
-          uint32_t mask = 0;
-          for (int r = 0; r < G; r += LPT) {
-            const int g = r + slot;
-            const bool keep = g < G && kept(values[g * per], g, [&](int o) { return values[o * per]; });
-            mask |= token_bits<LPT>(__ballot_sync(kFull, keep), lane) << r;
-          }
-          best = Top2();
-#pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            if (e0 + i < E && !((mask >> ((e0 + i) / per)) & 1u)) u[i] = neg_inf();
-            best.add(u[i]);
-          }
+        Top2 all = best;
+        for (int o = 1; o < shape.lanes; o <<= 1)
+          all.merge(__shfl_xor_sync(kFull, all.a, o), __shfl_xor_sync(kFull, all.b, o));
+        const float value = j.cfg.group_top > 1 && all.b != neg_inf() ? all.a + all.b : all.a;
+        int before = 0, close = 0;  // for certain, perhaps
+        for (int g = 0; g < G; ++g) {
+          const float o = __shfl_sync(kFull, value, first_lane + g * shape.lanes);
+          const bool tie = exact && o == value && g < group;
+          before += o > value + 2.f * margin || tie;
+          close += (g != group && o > value - 2.f * margin) || tie;
         }
+        open = value != neg_inf() && before < top_groups && close >= top_groups;
+        live &= before < top_groups;
       }
       if (!live) best = Top2();
       // the bound: the k-th largest of the lanes' two largest
@@ -352,7 +331,7 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
           e[r] = __float_as_int(keys[r * LPT + slot].y);
           score[r] = load_value(j.logits, t * j.ld + e[r], dtype);
           if (kSigmoid) score[r] = sigmoid(score[r]);
-          uc[r] = score[r] + biases[e[r] + e[r] / NV * kPad];
+          uc[r] = score[r] + (j.bias != nullptr ? j.bias[e[r]] : 0.f);
           keys[r * LPT + slot].x = uc[r];
           rank[r] = 0;
         }
@@ -379,10 +358,10 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) m = fmaxf(m, rank[r] < k ? score[r] : neg_inf());
       } else {
-        load_lane<NV>(j.logits, t * j.ld, dtype, e0, real ? E : 0, packs, z);
+        load_lane<NV>(j.logits, t * j.ld, dtype, real ? e0 + count : 0, shape.packs, consecutive, z);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          if (!(z[i] < -neg_inf()) || e0 + i >= E) z[i] = neg_inf();  // faulty ones, and no experts
+          if (!(z[i] < -neg_inf()) || i >= count) z[i] = neg_inf();  // faulty ones, and no experts
           m = fmaxf(m, z[i]);
         }
       }
@@ -430,17 +409,146 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
     if (hist[e] != 0) atomicAdd(j.load + e, hist[e]);
 }
 
+// Any number of experts and groups, by a warp a token and from shared memory:
+// for shapes whose groups do not lie in whole lanes of up to 32 values (more
+// than 32 (32 / groups) experts a group).  The k chosen are taken one by one.
+__global__ void __launch_bounds__(kThreads) route_any_kernel(const RouteJob j) {
+  extern __shared__ __align__(16) float dynamic[];  // choice values [kWarps][E], loads [E]
+  __shared__ float group_values[kWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int E = static_cast<int>(j.E), k = j.cfg.k, G = j.cfg.groups, per = E / G, dtype = j.dtype;
+  const bool sigmoids = j.cfg.score == SF_SCORE_SIGMOID;
+  float* u = dynamic + warp * E;
+  int32_t* hist = reinterpret_cast<int32_t*>(dynamic + kWarps * E);
+  for (int e = threadIdx.x; e < E; e += kThreads) hist[e] = 0;
+  __syncthreads();
+  uint32_t bits = 0;
+  for (int64_t t = blockIdx.x * int64_t(kWarps) + warp; t < j.T; t += int64_t(gridDim.x) * kWarps) {
+    float m = neg_inf(), sum = 0.f;
+    __syncwarp();
+    for (int e = lane; e < E; e += 32) {
+      const float z = load_value(j.logits, t * j.ld + e, dtype);
+      float v = (sigmoids ? sigmoid(z) : z) + (j.bias != nullptr ? j.bias[e] : 0.f);
+      if (z == neg_inf()) v = neg_inf();
+      if (z != neg_inf() && (v != v || (!sigmoids && z == -neg_inf()))) {
+        bits |= SF_ST_NONFINITE;
+        v = neg_inf();
+      }
+      u[e] = v;
+      if (z < -neg_inf()) m = fmaxf(m, z);
+    }
+    __syncwarp();
+    Top2 best;
+    if (lane < G)
+      for (int i = 0; i < per; ++i) best.add(u[lane * per + i]);
+    const float value = j.cfg.group_top > 1 && best.b != neg_inf() ? best.a + best.b : best.a;
+    if (lane < G) group_values[warp][lane] = value;
+    __syncwarp();
+    int before = 0;
+    for (int g = 0; g < G; ++g) {
+      const float o = group_values[warp][g];
+      before += o > value || (o == value && g < lane);
+    }
+    const uint32_t kept = __ballot_sync(kFull, lane < G && before < j.cfg.top_groups);
+    int chosen = -1;
+    float score = neg_inf();
+    for (int c = 0; c < k; ++c) {
+      float top = neg_inf();
+      int at = E;
+      for (int e = lane; e < E; e += 32)
+        if (((kept >> (e / per)) & 1u) && u[e] > top) {
+          top = u[e];
+          at = e;
+        }
+      const float most = token_max<32>(top);
+      if (most == neg_inf()) break;
+      at = __reduce_min_sync(kFull, top == most ? at : E);
+      if (lane == 0) u[at] = neg_inf();
+      __syncwarp();
+      if (lane == c) {
+        chosen = at;
+        score = load_value(j.logits, t * j.ld + at, dtype);
+      }
+    }
+    float w;
+    if (sigmoids) {
+      w = chosen >= 0 ? sigmoid(score) : 0.f;
+      sum = 1.f;
+    } else {
+      m = token_max<32>(j.cfg.renorm ? score : m);
+      w = chosen >= 0 ? expf(score - m) : 0.f;
+      if (!j.cfg.renorm)
+        for (int e = lane; e < E; e += 32) {
+          const float z = load_value(j.logits, t * j.ld + e, dtype);
+          if (z < -neg_inf() && z != neg_inf()) sum += exp_fast(z - m);
+        }
+      sum = token_sum<32>(sum);
+    }
+    if (j.cfg.renorm) sum = token_sum<32>(w);
+    if (lane < k) {
+      j.index[t * k + lane] = chosen;
+      j.weight[t * k + lane] = chosen >= 0 && sum > 0.f ? w / sum * j.cfg.scale : 0.f;
+      if (chosen >= 0) atomicAdd(hist + chosen, 1);
+    }
+  }
+  report(j.status, bits);
+  if (j.load == nullptr) return;
+  griddep_wait();  // the totals have been cleared
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += kThreads) {
+    if (j.only_cta)
+      j.load[e] = hist[e];
+    else if (hist[e] != 0)
+      atomicAdd(j.load + e, hist[e]);
+  }
+}
+
 template <int NV, int LPT>
-cudaError_t launch_route_lanes(const RouteJob& j, bool after_clear, cudaStream_t stream) {
+cudaError_t launch_route_lanes(const RouteJob& j, const RouteShape& shape, bool after_clear, cudaStream_t stream) {
   constexpr int kTokens = kWarps * 32 / LPT;  // of a CTA
-  const bool grouped = j.cfg.top_groups < j.cfg.groups;
-  const size_t smem = (size_t(LPT) * (NV + 4) + size_t(j.E) * (grouped ? 1 + kTokens : 1)) * 4;
+  const size_t smem = (size_t(LPT) * (NV + 4) + size_t(j.E)) * 4;
   const int64_t ctas = (j.T + kTokens - 1) / kTokens;
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ctas, int64_t(sm_count()) * 8)));
   count_launch();
   const auto kern = j.cfg.score == SF_SCORE_SIGMOID ? route_kernel<NV, LPT, true> : route_kernel<NV, LPT, false>;
-  return launch_after(kern, grid, dim3(kThreads), smem, stream, after_clear, j,
-                      in_packs(j.logits, j.dtype, j.E, j.ld, NV));
+  return launch_after(kern, grid, dim3(kThreads), smem, stream, after_clear, j, shape);
+}
+
+template <int LPT>
+cudaError_t launch_route_width(const RouteJob& j, RouteShape shape, bool after_clear, cudaStream_t stream) {
+  const auto go = [&](auto nv) {
+    constexpr int NV = decltype(nv)::value;
+    const int N = j.dtype == SF_F32 ? 4 : 8;
+    const int64_t per = j.cfg.top_groups < j.cfg.groups ? j.E / j.cfg.groups : j.E;
+    shape.packs = shape.each % N == 0 && in_packs(j.logits, j.dtype, per, j.ld, NV);
+    return launch_route_lanes<NV, LPT>(j, shape, after_clear, stream);
+  };
+  if constexpr (LPT == 32) {
+    if (shape.each <= 1) return go(std::integral_constant<int, 1>());
+    if (shape.each <= 2) return go(std::integral_constant<int, 2>());
+  }
+  if (shape.each <= 4) return go(std::integral_constant<int, 4>());
+  if (shape.each <= 8) return go(std::integral_constant<int, 8>());
+  if (shape.each <= 16) return go(std::integral_constant<int, 16>());
+  if (shape.each <= 24) return go(std::integral_constant<int, 24>());
+  return go(std::integral_constant<int, 32>());
+}
+
+// The shape for LPT lanes a token; each = 0: they do not do.
+RouteShape shape_of(const RouteJob& j, int LPT) {
+  RouteShape s{0, 0, false};
+  const bool grouped = j.cfg.top_groups < j.cfg.groups;
+  const int G = grouped ? j.cfg.groups : 1, kept = grouped ? j.cfg.top_groups : 1;
+  if (G > LPT) return s;
+  s.lanes = 1;
+  while (s.lanes * 2 * G <= LPT) s.lanes *= 2;
+  const int per = static_cast<int>(j.E) / G, N = j.dtype == SF_F32 ? 4 : 8;
+  int each = (per + s.lanes - 1) / s.lanes;
+  if (per % N == 0 && each > 2) each = (each + N - 1) / N * N;  // whole packs
+  // two values each of the lanes that are kept bound the k-th largest; rows in 32 values
+  if (each > 32 || (LPT < 32 && 2 * s.lanes * kept < j.cfg.k)) return s;
+  s.each = each;
+  return s;
 }
 
 // Gradient: the chosen experts' lanes put their own values (or, where all
@@ -452,37 +560,51 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteGradJob
   constexpr int kTokens = 32 / LPT;  // of a warp
   extern __shared__ __align__(16) float rows[];  // [kWarps * 32][NV]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = lane & (LPT - 1);
-  const int E = static_cast<int>(j.E), k = j.cfg.k, e0 = slot * NV, dtype = j.dtype;
+  const int E = static_cast<int>(j.E), k = j.cfg.k, dtype = j.dtype;
   float* d = rows + (warp * 32 + lane - slot) * NV;
+  // a token's lanes take its packs in turn, whether they are read as packs or not: the sums' order is one
+  const int width = dtype == SF_F32 ? 4 : 8;
+  const auto in_turn = [&](int p, int n) {
+    return n == 1 ? (p / width * LPT + slot) * width + p % width : (p * LPT + slot) * n;
+  };
   const bool sigmoids = j.cfg.score == SF_SCORE_SIGMOID;
   uint32_t bits = 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) d[e0 + i] = 0.f;
-  for (int64_t t0 = (blockIdx.x * int64_t(kWarps) + warp) * kTokens; t0 < j.T; t0 += int64_t(gridDim.x) * kWarps * kTokens) {
-    const int64_t t = t0 + lane / LPT;
+  for (int i = 0; i < NV; ++i) d[i * LPT + slot] = 0.f;
+  // the slots of the token after this one are read ahead: a logit waits for its index
+  const int64_t step = int64_t(gridDim.x) * kWarps * kTokens;
+  int64_t t = (blockIdx.x * int64_t(kWarps) + warp) * kTokens + lane / LPT;
+  int next_e = -1;
+  float next_dw = 0.f;
+  if (t < j.T && slot < k) {
+    next_e = j.index[t * k + slot];
+    next_dw = j.dweight[t * k + slot];
+  }
+  for (; t - lane / LPT < j.T; t += step) {
     const bool real = t < j.T;
+    int e = next_e;
+    float dw = next_dw, z = neg_inf();
+    if (e < -1 || e >= E) {
+      bits |= SF_ST_INDEX;
+      e = -1;
+    }
+    if (e >= 0)
+      z = load_value(j.logits, t * j.ld + e, dtype);
+    else
+      dw = 0.f;
     float all[NV];
     if (kDense) {
-      load_lane<NV>(j.logits, t * j.ld, dtype, e0, real ? E : 0, packs, all);
-      if (e0 + NV > E) {
+      load_lane<NV>(j.logits, t * j.ld, dtype, real ? E : 0, packs, in_turn, all);
+      if (in_turn(NV - 1, 1) >= E) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if (e0 + i >= E) all[i] = neg_inf();
+          if (in_turn(i, 1) >= E) all[i] = neg_inf();
       }
     }
-    int e = -1;
-    float dw = 0.f, z = neg_inf();
-    if (real && slot < k) {
-      e = j.index[t * k + slot];
-      dw = j.dweight[t * k + slot];
-      if (e < -1 || e >= E) {
-        bits |= SF_ST_INDEX;
-        e = -1;
-      }
-      if (e >= 0)
-        z = load_value(j.logits, t * j.ld + e, dtype);
-      else
-        dw = 0.f;
+    next_e = -1;
+    if (t + step < j.T && slot < k) {
+      next_e = j.index[(t + step) * k + slot];
+      next_dw = j.dweight[(t + step) * k + slot];
     }
     float g = 0.f, s, inner;
     if (kDense) {
@@ -532,14 +654,22 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteGradJob
     __syncwarp();
     float v[NV];
     const float c = kDense ? s * j.cfg.scale : 0.f, shift = kDense ? -inner * c : 0.f;
+    const auto take = [&](auto n) {
+      constexpr int N = decltype(n)::value;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[i] = d[((i / N) * LPT + slot) * N + i % N];
+    };
+    if (width == 8)
+      take(std::integral_constant<int, 8>());
+    else
+      take(std::integral_constant<int, 4>());
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      v[i] = d[e0 + i];
       if (kDense) v[i] = all[i] * fmaf(v[i], c, shift);
     }
     __syncwarp();
     if (e >= 0) d[e] = 0.f;
-    store_lane<NV>(j.dlogits, t * j.ldd, dtype, e0, real ? E : 0, packs, v);
+    store_lane<NV>(j.dlogits, t * j.ldd, dtype, real ? E : 0, packs, in_turn, v);
   }
   report(j.status, bits);
 }
@@ -568,27 +698,14 @@ cudaError_t launch_route(RouteJob j, bool accumulate, cudaStream_t stream) {
     const cudaError_t e = launch_zero_many(z, stream, &after_clear);
     if (e != cudaSuccess) return e;
   }
-  // As few lanes a token as hold its row in 32 values and, two values each, one and a half times k values
-  // of the groups that are kept (else the bound is loose, or there is none).
-  const int64_t held = int64_t(4) * j.cfg.top_groups, need = int64_t(3) * j.cfg.k * j.cfg.groups;
-  if (8 * held >= need) {
-    if (j.E <= 32) return launch_route_lanes<4, 8>(j, after_clear, stream);
-    if (j.E <= 64) return launch_route_lanes<8, 8>(j, after_clear, stream);
-    if (j.E <= 128) return launch_route_lanes<16, 8>(j, after_clear, stream);
-    if (j.E <= 256) return launch_route_lanes<32, 8>(j, after_clear, stream);
-  }
-  if (16 * held >= need) {
-    if (j.E <= 64) return launch_route_lanes<4, 16>(j, after_clear, stream);
-    if (j.E <= 128) return launch_route_lanes<8, 16>(j, after_clear, stream);
-    if (j.E <= 256) return launch_route_lanes<16, 16>(j, after_clear, stream);
-    if (j.E <= 512) return launch_route_lanes<32, 16>(j, after_clear, stream);
-  }
-  if (j.E <= 32) return launch_route_lanes<1, 32>(j, after_clear, stream);
-  if (j.E <= 64) return launch_route_lanes<2, 32>(j, after_clear, stream);
-  if (j.E <= 128) return launch_route_lanes<4, 32>(j, after_clear, stream);
-  if (j.E <= 256) return launch_route_lanes<8, 32>(j, after_clear, stream);
-  if (j.E <= 512) return launch_route_lanes<16, 32>(j, after_clear, stream);
-  return launch_route_lanes<32, 32>(j, after_clear, stream);
+  // as few lanes a token as do: what is not per value is shared by more tokens
+  if (const RouteShape s = shape_of(j, 8); s.each > 0) return launch_route_width<8>(j, s, after_clear, stream);
+  if (const RouteShape s = shape_of(j, 16); s.each > 0) return launch_route_width<16>(j, s, after_clear, stream);
+  if (const RouteShape s = shape_of(j, 32); s.each > 0) return launch_route_width<32>(j, s, after_clear, stream);
+  const int64_t ctas = std::min<int64_t>((j.T + kWarps - 1) / kWarps, int64_t(sm_count()) * 4);
+  count_launch();
+  return launch_after(route_any_kernel, dim3(static_cast<unsigned>(ctas)), dim3(kThreads),
+                      size_t(j.E) * 4 * (kWarps + 1), stream, after_clear, j);
 }
 
 cudaError_t launch_route_grad(const RouteGradJob& j, cudaStream_t stream) {
