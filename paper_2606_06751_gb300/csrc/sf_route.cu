@@ -556,7 +556,7 @@ RouteShape shape_of(const RouteJob& j, int LPT) {
 // shared memory, from which every lane takes its NV.  Several tokens a warp:
 // their reads, two of which wait for one another, are in flight together.
 template <int NV, int LPT, bool kDense>
-__global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteGradJob j, const bool packs) {
+__global__ void __launch_bounds__(kThreads, NV > 16 ? 2 : kDense ? 4 : 5) route_grad_kernel(const RouteGradJob j, const bool packs) {
   constexpr int kTokens = 32 / LPT;  // of a warp
   extern __shared__ __align__(16) float rows[];  // [kWarps * 32][NV]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = lane & (LPT - 1);
