@@ -718,12 +718,12 @@ cudaError_t launch_rows(const PolicyJob& j, cudaStream_t stream) {
   while (C <= kMaxCluster && int64_t(C) * kClusterThreads * kHeld < packs) C *= 2;
   while (C < kMaxCluster && j.N * C * 2 <= int64_t(sm_count()) * 2 && packs > int64_t(C) * kClusterThreads) C *= 2;
   if (C <= kMaxCluster && j.N * C <= int64_t(sm_count()) * 2) return launch_cluster<T, kHeld, kGrad>(j, C, stream);
-  // As many CTAs an SM as leave their rows in L2 (129 MB) until the second read, here a row each of
-  // 84 MB in all (us with 4 / 2 / 1 an SM: 4096 x 32768 bf16, 40 MB with 4, 101 / 117 / 167; 2048 x 50001
-  // f32, 122 MB, 179 / 153 / 163; 6144 x 131072 bf16, 159 MB, 735 / 587 / 642; 2048 x 131072 f32, 319 MB,
-  // 491 / 489 / 389).  Without a second read always four.
+  // As many CTAs an SM as leave their rows in L2 (129 MB) until the second read, a row each, with four 76 MB
+  // in all, with two 84 (us with 4 / 2 / 1 an SM: 4096 x 32768 bf16, 40 MB with 4, 100 / 117 / 167; 4096 x
+  // 65536, 80 MB, 209 / 197; 2048 x 50001 f32, 122 MB, 179 / 153 / 163; 6144 x 131072 bf16, 159 MB, 735 / 587 /
+  // 642; 2048 x 131072 f32, 319 MB, 491 / 489 / 389).  Without a second read always four.
   const double rows = double(j.V) * sizeof(T) * sm_count();  // bytes of a row on every SM
-  if (!kGrad || rows * 4 <= 84e6) return launch_ring<T, 256, 4, 4, kGrad>(j, stream);
+  if (!kGrad || rows * 4 <= 76e6) return launch_ring<T, 256, 4, 4, kGrad>(j, stream);
   if (rows * 2 <= 84e6) return launch_ring<T, 512, 2, 2, kGrad>(j, stream);
   return launch_ring<T, 992, 2, 1, kGrad>(j, stream);
 }

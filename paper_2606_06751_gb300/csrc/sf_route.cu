@@ -159,6 +159,12 @@ struct Gather {
   static constexpr int kRounds = LPT == 8 ? 4 : LPT == 16 ? 3 : 2, kMost = LPT * kRounds;
 };
 
+// Larger for the larger choice value, and for the lower of two experts with equal ones (both zeros are).
+__device__ __forceinline__ uint64_t rank_key(float u, int e) {
+  const uint32_t b = __float_as_uint(u + 0.f);
+  return uint64_t((b & 0x80000000u) ? ~b : b | 0x80000000u) << 32 | (0xffffffffu - static_cast<uint32_t>(e));
+}
+
 // How a token's experts lie in its lanes: a group's in `lanes` lanes (a power of
 // two), `each` consecutive ones a lane.
 struct RouteShape {
@@ -172,7 +178,8 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
   constexpr int kRounds = Gather<LPT>::kRounds, kGathered = Gather<LPT>::kMost;
   constexpr int kPad = NV % 4 == 0 ? 4 : 0;  // of a lane's biases, which then lie in banks of their own
   extern __shared__ __align__(16) float dynamic[];  // biases, loads [E]
-  __shared__ float2 all_keys[kWarps][kTokens][kGathered];  // (choice value, expert)
+  __shared__ uint64_t all_keys[kWarps][kTokens][kGathered];  // choice value and expert, by rank_key
+  __shared__ float2 all_picked[kWarps][kTokens][32];         // (score or weight, expert) of the chosen
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = lane & (LPT - 1), first_lane = lane - slot;
   const int E = static_cast<int>(j.E), k = j.cfg.k, dtype = j.dtype, top_groups = j.cfg.top_groups;
   const bool grouped = top_groups < j.cfg.groups;
@@ -183,7 +190,8 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
   const auto consecutive = [&](int p, int n) { return e0 + p * n; };
   float* biases = dynamic;
   int32_t* hist = reinterpret_cast<int32_t*>(biases + LPT * (NV + kPad));
-  float2* keys = all_keys[warp][lane / LPT];
+  uint64_t* keys = all_keys[warp][lane / LPT];
+  float2* picked = all_picked[warp][lane / LPT];
   if (threadIdx.x < LPT) {  // a token's lanes, each its own; not available past its last expert
     for (int i = 0; i < NV; ++i)
       biases[slot * (NV + kPad) + i] = i >= count ? neg_inf() : j.bias != nullptr ? j.bias[e0 + i] : 0.f;
@@ -206,14 +214,7 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
        t0 += int64_t(gridDim.x) * kWarps * kTokens) {
     const int64_t t = t0 + lane / LPT;
     const bool real = t < j.T;
-    int e[kRounds], rank[kRounds];  // of this lane's gathered values
-    float score[kRounds];           // sigmoid or logit
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      e[r] = -1;
-      rank[r] = kGathered;
-      score[r] = 0.f;
-    }
+    int found = 0;  // experts chosen
     for (bool exact = !kSigmoid;; exact = true) {
       float u[NV], odd = 0.f;
       Top2 best;
@@ -310,92 +311,91 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
               u[i] = neg_inf();
             }
           taken = __shfl_sync(kFull, taken, owner, LPT);
-#pragma unroll
-          for (int r = 0; r < kRounds; ++r)
-            if (r * LPT + slot == c && taken >= 0) {
-              e[r] = taken;
-              rank[r] = c;
-              score[r] = load_value(j.logits, t * j.ld + taken, dtype);
-              if (kSigmoid) score[r] = sigmoid(score[r]);
+          if (taken >= 0) {
+            if (slot == owner) {
+              const float z = load_value(j.logits, t * j.ld + taken, dtype);
+              picked[c] = make_float2(kSigmoid ? sigmoid(z) : z, __int_as_float(taken));
             }
+            found = c + 1;
+          }
         }
         break;
       }
-      for (; mine != 0; mine &= mine - 1) keys[at++].y = __int_as_float(e0 + __ffs(static_cast<int>(mine)) - 1);
+      found = min(n, k);
+      for (; mine != 0; mine &= mine - 1) keys[at++] = static_cast<uint32_t>(e0 + __ffs(static_cast<int>(mine)) - 1);
       __syncwarp();
-      float uc[kRounds];
+      const int most = kTokens == 1 ? n : __reduce_max_sync(kFull, n);  // of the warp's tokens
+      int e[kRounds], rank[kRounds];  // of this lane's gathered values
+      float score[kRounds];           // sigmoid or logit
+      uint64_t key[kRounds];
 #pragma unroll
       for (int r = 0; r < kRounds; ++r) {
-        uc[r] = neg_inf();
+        if (r * LPT >= most) break;
+        rank[r] = kGathered;
+        key[r] = ~uint64_t(0);
         if (r * LPT + slot < n) {
-          e[r] = __float_as_int(keys[r * LPT + slot].y);
+          e[r] = static_cast<int>(keys[r * LPT + slot]);
           score[r] = load_value(j.logits, t * j.ld + e[r], dtype);
           if (kSigmoid) score[r] = sigmoid(score[r]);
-          uc[r] = score[r] + (j.bias != nullptr ? j.bias[e[r]] : 0.f);
-          keys[r * LPT + slot].x = uc[r];
+          key[r] = rank_key(score[r] + (j.bias != nullptr ? j.bias[e[r]] : 0.f), e[r]);
+          keys[r * LPT + slot] = key[r];
           rank[r] = 0;
         }
       }
       __syncwarp();
       for (int i = 0; i < n; ++i) {
-        const float2 o = keys[i];
+        const uint64_t o = keys[i];
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) rank[r] += o.x > uc[r] || (o.x == uc[r] && __float_as_int(o.y) < e[r]);
-      }
-      __syncwarp();
-      break;
-    }
-    // weights
-    float w[kRounds], sum = 0.f;
-    int found = 0;
-    if (kSigmoid) {
-#pragma unroll
-      for (int r = 0; r < kRounds; ++r) w[r] = rank[r] < k ? score[r] : 0.f;
-    } else {
-      float m = neg_inf();
-      float z[NV];
-      if (j.cfg.renorm) {
-#pragma unroll
-        for (int r = 0; r < kRounds; ++r) m = fmaxf(m, rank[r] < k ? score[r] : neg_inf());
-      } else {
-        load_lane<NV>(j.logits, t * j.ld, dtype, real ? e0 + count : 0, shape.packs, consecutive, z);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          if (!(z[i] < -neg_inf()) || i >= count) z[i] = neg_inf();  // faulty ones, and no experts
-          m = fmaxf(m, z[i]);
+        for (int r = 0; r < kRounds; ++r) {
+          if (r * LPT >= most) break;
+          rank[r] += o > key[r];
         }
       }
-      m = token_max<LPT>(m);
 #pragma unroll
-      for (int r = 0; r < kRounds; ++r) w[r] = rank[r] < k ? expf(score[r] - m) : 0.f;
-      if (!j.cfg.renorm) {
-        if (m == neg_inf()) m = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) sum += exp_fast(z[i] - m);
-        sum = token_sum<LPT>(sum);
+      for (int r = 0; r < kRounds; ++r) {
+        if (r * LPT >= most) break;
+        if (rank[r] < k) picked[rank[r]] = make_float2(score[r], __int_as_float(e[r]));
       }
+      break;
     }
-    if (j.cfg.renorm) {
+    __syncwarp();
+    // weights, by the order of choice
+    float m = neg_inf(), sum = 0.f;
+    if (!kSigmoid && j.cfg.renorm) {
+      for (int c = slot; c < found; c += LPT) m = fmaxf(m, picked[c].x);
+      m = token_max<LPT>(m);
+    } else if (!kSigmoid) {
+      float z[NV];
+      load_lane<NV>(j.logits, t * j.ld, dtype, real ? e0 + count : 0, shape.packs, consecutive, z);
 #pragma unroll
-      for (int r = 0; r < kRounds; ++r) sum += w[r];
+      for (int i = 0; i < NV; ++i) {
+        if (!(z[i] < -neg_inf()) || i >= count) z[i] = neg_inf();  // faulty ones, and no experts
+        m = fmaxf(m, z[i]);
+      }
+      m = token_max<LPT>(m);
+      const float from = m == neg_inf() ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) sum += exp_fast(z[i] - from);
+    }
+    if (!kSigmoid || j.cfg.renorm) {
+      for (int c = slot; c < found; c += LPT) {
+        float w = picked[c].x;
+        if (!kSigmoid) picked[c].x = w = expf(w - m);
+        if (j.cfg.renorm) sum += w;
+      }
       sum = token_sum<LPT>(sum);
-    } else if (kSigmoid) {
+    } else {
       sum = 1.f;
     }
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      if (rank[r] < k) {
-        j.index[t * k + rank[r]] = e[r];
-        j.weight[t * k + rank[r]] = sum > 0.f ? w[r] / sum * j.cfg.scale : 0.f;
-        atomicAdd(hist + e[r], 1);
-      }
-      found += __popc(token_bits<LPT>(__ballot_sync(kFull, rank[r] < k), lane));
-    }
     if (real)
-      for (int c = found + slot; c < k; c += LPT) {  // fewer experts than k
-        j.index[t * k + c] = -1;
-        j.weight[t * k + c] = 0.f;
+      for (int c = slot; c < k; c += LPT) {
+        const bool is = c < found;  // fewer experts than k: -1
+        const float2 o = is ? picked[c] : make_float2(0.f, __int_as_float(-1));
+        j.index[t * k + c] = __float_as_int(o.y);
+        j.weight[t * k + c] = is && sum > 0.f ? o.x / sum * j.cfg.scale : 0.f;
+        if (is) atomicAdd(hist + __float_as_int(o.y), 1);
       }
+    __syncwarp();
   }
   report(j.status, bits);
   if (j.load == nullptr) return;
