@@ -488,9 +488,9 @@ typedef struct sf_policy_config {
  *             must not overlap.  Rounded once, to nearest even.
  *   workspace device, 16-byte aligned, sf_policy_loss_workspace_size(N, V) bytes
  * A row whose token is not in [0, V) is left out like one of weight 0, with
- * SF_ST_INDEX; so is one whose loss, weight or derivative is not finite (a
- * NaN or +inf logit, no logit above -inf), with SF_ST_NONFINITE.
- * N < 2^31, 1 <= V < 2^31.
+ * SF_ST_INDEX; so is one whose loss, KL term, weight or derivative is not
+ * finite (a NaN or +inf logit, no logit above -inf), with SF_ST_NONFINITE.
+ * N < 2^31, 1 <= V <= 2^30.
  */
 sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V, int64_t ld, const int64_t* target,
                          const float* old_logp, const float* ref_logp, const float* advantage, const float* weight,

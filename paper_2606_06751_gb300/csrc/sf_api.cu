@@ -58,6 +58,7 @@ bool rows_overlap(const void* a, int64_t lda, const void* b, int64_t ldb, int64_
   return off < n || step - off < n;
 }
 
+constexpr int64_t kMaxVocabulary = int64_t(1) << 30;
 constexpr int64_t kMaxTensors = int64_t(1) << 20;
 bool sizes_ok(const int64_t* numel, int64_t n) {
   if (n < 0 || n > kMaxTensors || (n > 0 && !numel)) return false;
@@ -505,7 +506,7 @@ sf_status sf_label_windows(const int64_t* d, int64_t T, int64_t R, int64_t S, in
 }
 
 size_t sf_policy_loss_workspace_size(int64_t N, int64_t V) {
-  if (!rows_ok(N, V, V) || N == 0) return 0;
+  if (!rows_ok(N, V, V) || V > kMaxVocabulary || N == 0) return 0;
   return policy_loss_workspace(N);
 }
 
@@ -514,7 +515,9 @@ sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V
                          const sf_policy_config* cfg, const float* grad_out, float* logp, float* token_loss,
                          float* stats, void* dlogits, int64_t ldd, void* workspace, size_t workspace_bytes,
                          uint32_t* status, cudaStream_t stream) {
-  if (!dtype_ok(dtype) || !rows_ok(N, V, ld) || (dlogits && !rows_ok(N, V, ldd)) || !stats || !cfg) return SF_EINVAL;
+  if (!dtype_ok(dtype) || !rows_ok(N, V, ld) || (dlogits && !rows_ok(N, V, ldd)) || V > kMaxVocabulary ||
+      !stats || !cfg)
+    return SF_EINVAL;
   if (N > 0 && (!logits || !target || !old_logp || !advantage)) return SF_EINVAL;
   if (!(cfg->clip_low >= 0.f && cfg->clip_low <= 1.f && cfg->clip_high >= 0.f && std::isfinite(cfg->clip_high) &&
         cfg->kl_coef >= 0.f && std::isfinite(cfg->kl_coef) && cfg->inv_temperature > 0.f &&

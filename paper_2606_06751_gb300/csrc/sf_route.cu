@@ -262,7 +262,8 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
           const float o = __shfl_sync(kFull, value, first_lane + g * shape.lanes);
           const bool tie = exact && o == value && g < group;
           before += o > value + 2.f * margin || tie;
-          close += (g != group && o > value - 2.f * margin) || tie;
+          // also equal ones, so that infinite values (of biases, or sums of two) are told apart exactly
+          close += exact ? o > value || tie : g != group && o >= value - 2.f * margin;
         }
         open = value != neg_inf() && before < top_groups && close >= top_groups;
         live &= before < top_groups;

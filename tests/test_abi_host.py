@@ -140,3 +140,74 @@ def test_host_validation(sf):
 def test_no_cpu_fallback_in_binding():
     src = open(os.path.join(ROOT, "paper_2606_06751_gb300", "stagefrontier.py")).read()
     assert "oracle" not in src and "numpy" not in src
+
+
+def test_host_validation_of_training_step_operators(sf):
+    """Refusals before anything is enqueued: null pointers, alignment, shapes, configurations, workspaces."""
+    L = sf.lib()
+    ok = sf.PolicyConfig(0.2, 0.2, 0.1, 1.0)
+
+    def loss(logits=FAKE, dtype=1, N=4, V=16, ld=16, target=FAKE, old=FAKE, adv=FAKE, cfg=ok, stats=FAKE, d=None, ldd=16,
+             ws=FAKE, size=1 << 20, logp=None):
+        return L.sf_policy_loss(logits, dtype, N, V, ld, target, old, None, adv, None,
+                                None if cfg is None else ctypes.byref(cfg), None, logp, None, stats, d, ldd, ws, size,
+                                None, None)
+
+    for kw in (dict(logits=None), dict(dtype=3), dict(dtype=-1), dict(N=-1), dict(V=0), dict(V=(1 << 30) + 1, ld=1 << 31),
+               dict(ld=15), dict(target=None), dict(old=None), dict(adv=None), dict(cfg=None), dict(stats=None),
+               dict(d=FAKE + 32), dict(d=FAKE, ldd=15), dict(d=FAKE, ldd=17), dict(N=1 << 31),
+               dict(cfg=sf.PolicyConfig(-0.1, 0.2, 0.0, 1.0)), dict(cfg=sf.PolicyConfig(0.2, -0.2, 0.0, 1.0)),
+               dict(cfg=sf.PolicyConfig(0.2, 0.2, 0.0, 2e6))):
+        assert loss(**kw) == sf.SF_EINVAL, kw
+    for kw in (dict(logits=FAKE + 1), dict(target=FAKE + 4), dict(old=FAKE + 2), dict(stats=FAKE + 2), dict(ws=FAKE + 8),
+               dict(logp=FAKE + 1)):
+        assert loss(**kw) == sf.SF_EINVAL_ALIGN, kw
+    assert loss(ws=None) == sf.SF_EWORKSPACE and loss(size=63) == sf.SF_EWORKSPACE
+    assert L.sf_policy_loss_workspace_size(4, 16) == 64 and L.sf_policy_loss_workspace_size(0, 16) == 0
+    assert L.sf_policy_loss_workspace_size(-1, 16) == 0 and L.sf_policy_loss_workspace_size(4, 0) == 0
+
+    def route(logits=FAKE, T=4, E=64, ld=64, k=4, score=0, groups=1, top=1, best=2, renorm=1, scale=1.0, index=FAKE,
+              weight=FAKE, load=None, acc=0, cfg=True):
+        c = sf.RouteConfig(k, score, groups, top, best, renorm, scale)
+        return L.sf_route_experts(logits, 0, T, E, ld, None, ctypes.byref(c) if cfg else None, index, weight, load, acc,
+                                  None, None)
+
+    for kw in (dict(logits=None), dict(T=-1), dict(E=0), dict(E=1025, ld=1025), dict(ld=63), dict(k=0), dict(k=33),
+               dict(k=9, groups=8), dict(score=2), dict(groups=0), dict(groups=33, E=66, ld=66), dict(groups=5),
+               dict(top=2), dict(top=0), dict(best=0), dict(best=3), dict(renorm=2), dict(scale=float("inf")),
+               dict(index=None), dict(weight=None), dict(acc=2), dict(cfg=False)):
+        assert route(**kw) == sf.SF_EINVAL, kw
+    for kw in (dict(logits=FAKE + 2), dict(index=FAKE + 2), dict(weight=FAKE + 1), dict(load=FAKE + 2)):
+        assert route(**kw) == sf.SF_EINVAL_ALIGN, kw
+    c = sf.RouteConfig(4, 0, 1, 1, 1, 1, 1.0)
+    grad = lambda z, i, w, d, ldd: L.sf_route_experts_grad(z, 0, 4, 64, 64, i, w, ctypes.byref(c), d, ldd, None, None)  # noqa: E731
+    far = FAKE + (1 << 16)
+    assert grad(None, FAKE, FAKE, far, 64) == sf.SF_EINVAL and grad(FAKE, None, FAKE, far, 64) == sf.SF_EINVAL
+    assert grad(FAKE, FAKE, None, far, 64) == sf.SF_EINVAL and grad(FAKE, FAKE, FAKE, None, 64) == sf.SF_EINVAL
+    assert grad(FAKE, FAKE, FAKE, FAKE, 64) == sf.SF_EINVAL and grad(FAKE, FAKE, FAKE, FAKE + 128, 64) == sf.SF_EINVAL
+    assert grad(FAKE, FAKE, FAKE, far, 63) == sf.SF_EINVAL
+    assert grad(FAKE, FAKE + 1, FAKE, far, 64) == sf.SF_EINVAL_ALIGN
+
+    def clip(data=(FAKE, far), out=None, numel=(8, 5), dtype=(0, 1), norm=FAKE, ws=FAKE, size=1 << 20, most=1.0, eps=0.0):
+        n = len(numel)
+        p = (ctypes.c_void_p * n)(*data)
+        o = None if out is None else (ctypes.c_void_p * n)(*out)
+        s, t = (ctypes.c_int64 * n)(*numel), (ctypes.c_int32 * n)(*dtype)
+        if most is None:
+            return L.sf_grad_norm(p, s, t, n, norm, None, ws, size, None, None)
+        return L.sf_grad_clip(p, o, s, t, n, most, eps, norm, None, None, ws, size, None, None)
+
+    for most in (None, 1.0):
+        for kw in (dict(data=(None, far)), dict(numel=(-1, 5)), dict(numel=(1 << 40, 5)), dict(dtype=(0, 3)),
+                   dict(norm=None)):
+            assert clip(most=most, **kw) == sf.SF_EINVAL, kw
+        for kw in (dict(data=(FAKE + 2, far)), dict(data=(FAKE, far + 1)), dict(norm=FAKE + 2), dict(ws=FAKE + 8)):
+            assert clip(most=most, **kw) == sf.SF_EINVAL_ALIGN, kw
+        assert clip(most=most, ws=None) == sf.SF_EWORKSPACE and clip(most=most, size=64) == sf.SF_EWORKSPACE
+    for kw in (dict(most=0.0), dict(most=float("nan")), dict(eps=-1.0), dict(eps=float("inf")),
+               dict(out=(FAKE + 16, far)), dict(out=(None, far))):
+        assert clip(**kw) == sf.SF_EINVAL, kw
+    assert L.sf_grad_norm(None, None, None, 1, FAKE, None, FAKE, 1 << 20, None, None) == sf.SF_EINVAL
+    assert L.sf_grad_norm(None, None, None, (1 << 20) + 1, FAKE, None, FAKE, 1 << 20, None, None) == sf.SF_EINVAL
+    assert L.sf_grad_workspace_size(-1) == 0 and L.sf_grad_workspace_size(10) > 0
+    assert sf.launch_count() == 0

@@ -166,6 +166,18 @@ def test_norm_beyond_the_result_type(sf):
     assert int(st.item()) == sf.SF_ST_NONFINITE and math.isinf(float(r.norm))
 
 
+def test_more_than_32_bits_of_elements(sf):
+    n = (1 << 31) + 12345
+    g = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    g[-3:] = 100.0
+    r = sf.sf_grad_clip([g[:77], g[77:]], 1.0, per_tensor=True)
+    total = math.sqrt(n - 3 + 3e4)
+    assert abs(float(r.norm) - total) <= REL * total
+    assert abs(float(r.tensor_norm[1]) - math.sqrt(n - 80 + 3e4)) <= REL * total
+    want = torch.tensor([1.0, 100.0], device="cuda").mul(1.0 / total).bfloat16()
+    assert bool((g[:-3] == want[0]).all()) and bool((g[-3:] == want[1]).all())
+
+
 def test_no_tensors(sf):
     r = sf.sf_grad_norm([], per_tensor=True)
     assert float(r.norm) == 0.0 and r.tensor_norm.numel() == 0

@@ -339,6 +339,25 @@ def test_many_rows(sf):
     check(r, e, "f32")
 
 
+@pytest.mark.parametrize("N,V", [(17000, 131072), (1100, 2000003)])
+def test_offsets_beyond_32_bits(sf, N, V):
+    """More than 2^31 logits, in place: the last rows against the same rows alone."""
+    z = torch.zeros((N, V), dtype=torch.bfloat16, device="cuda")
+    last, h = make(8, V, "bf16", 21)
+    e = reference(h)
+    e["y"] = h["y"]
+    z[-8:] = last
+    t = {k: torch.zeros(N, dtype=v.dtype, device="cuda") for k, v in on_gpu(h).items()}
+    for k, v in on_gpu(h).items():
+        t[k][-8:] = v
+    st = sf.new_status("cuda")
+    r = sf.sf_policy_loss(z, clip=(LO, HI), kl_coef=BETA, inv_temperature=TAU, status=st, dlogits=z, **t)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0 and not z[:100].any()
+    r.logp, r.token_loss, r.dlogits = r.logp[-8:], r.token_loss[-8:], z[-8:]
+    check(r, e, "bf16")
+
+
 def test_no_rows(sf):
     z = torch.empty((0, 16), device="cuda")
     f = lambda n, t=torch.float32: torch.empty(n, dtype=t, device="cuda")  # noqa: E731

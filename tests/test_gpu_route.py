@@ -242,6 +242,38 @@ def test_faulty_values(sf, score):
     assert st == sf.SF_ST_NONFINITE and not bool((r.index == 9).any())
 
 
+@pytest.mark.parametrize("big", [math.inf, 3e38])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_infinite_choice_values(sf, score, big):
+    """Biases that force an expert, and groups whose values are infinite together."""
+    z, bias = make(9, 64, "f32", 8)
+    bias[[5, 20, 21, 40, 41]] = big
+    r, st = route(sf, z, bias, 3, score=score, groups=4, top_groups=1)
+    assert st == 0
+    # groups 1 and 2 have two such experts each (group 0 one): the lower of equal ones is kept, in 32 bits
+    # 3e38 + 3e38 is infinite, and so is the sum of group 0 only where the bias is
+    first = 0 if big == math.inf else 16
+    assert bool(((r.index >= first) & (r.index < first + 16)).all())
+    r, st = route(sf, z, bias, 6, score=score)
+    got = np.sort(r.index.cpu().numpy(), 1)
+    assert st == 0 and all(set([5, 20, 21, 40, 41]) <= set(row) for row in got.tolist())
+
+
+def test_offsets_beyond_32_bits(sf):
+    """More than 2^31 logits: the last tokens against the same tokens alone."""
+    T, E, k = (1 << 23) + 1000, 256, 8
+    z = torch.zeros((T, E), dtype=torch.bfloat16, device="cuda")
+    z[-500:] = torch.randn(500, E, device="cuda").to(torch.bfloat16)
+    a = sf.sf_route_experts(z, k)
+    b = sf.sf_route_experts(z[-500:], k)
+    assert torch.equal(a.index[-500:], b.index) and torch.equal(a.weight[-500:], b.weight)
+    assert int(a.load.sum()) == T * k and bool((a.index[:1000] == torch.arange(8, device="cuda")).all())
+    dw = torch.randn(T, k, device="cuda")
+    for renorm in (True, False):
+        d = sf.sf_route_experts_grad(z, a.index, dw, renorm=renorm)
+        assert torch.equal(d[-500:], sf.sf_route_experts_grad(z[-500:], b.index, dw[-500:], renorm=renorm))
+
+
 def test_saturated_scores(sf):
     """Sigmoids that are 0 in 32 bits: a sum of 0, weights and gradients of 0."""
     z = torch.full((3, 40), -200.0, device="cuda")
