@@ -463,6 +463,8 @@ typedef struct sf_policy_config {
   float inv_temperature;     /* tau, 0 < tau <= 1e6: the policy is softmax(tau * logits) */
 } sf_policy_config;
 
+#define SF_POLICY_DIRECT_ROWS 1024
+
 /*
  * sf_policy_loss - the clipped policy loss with a KL term, from the logits,
  * and its gradient.  For row (token) n with logits z, chosen token y, weight
@@ -486,7 +488,8 @@ typedef struct sf_policy_config {
  *   dlogits   [N] rows of V, ldd elements apart, of type dtype (nullable: no
  *             gradient); may be `logits` itself with ldd = ld, else the two
  *             must not overlap.  Rounded once, to nearest even.
- *   workspace device, 16-byte aligned, sf_policy_loss_workspace_size(N, V) bytes
+ *   workspace device, 16-byte aligned, sf_policy_loss_workspace_size(N, V) bytes;
+ *             may be null for up to SF_POLICY_DIRECT_ROWS rows with logp given
  * A row whose token is not in [0, V) is left out like one of weight 0, with
  * SF_ST_INDEX; so is one whose loss, KL term, weight or derivative is not
  * finite (a NaN or +inf logit, no logit above -inf), with SF_ST_NONFINITE.
@@ -498,7 +501,7 @@ sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V
                          float* stats, void* dlogits, int64_t ldd, void* workspace, size_t workspace_bytes,
                          uint32_t* status, cudaStream_t stream);
 
-/* Workspace bytes sf_policy_loss needs; 0 on bad arguments and for N = 0. */
+/* Workspace bytes of sf_policy_loss; 0 on bad arguments and for N = 0. */
 size_t sf_policy_loss_workspace_size(int64_t N, int64_t V);
 
 #define SF_SCORE_SOFTMAX 0

@@ -536,7 +536,7 @@ sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V
   if (dlogits && !(dlogits == logits && ldd == ld) &&
       rows_overlap(logits, ld, dlogits, ldd, N, V, dtype_size(dtype)))
     return SF_EINVAL;
-  if (!workspace || workspace_bytes < policy_loss_workspace(N)) return SF_EWORKSPACE;
+  if (workspace ? workspace_bytes < policy_loss_workspace(N) : !policy_loss_direct(N, logp)) return SF_EWORKSPACE;
   if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
   PolicyJob j;
   j.logits = logits;

@@ -135,10 +135,11 @@ struct PolicyJob {
   int64_t ldd;
   uint32_t* status;
   // set by launch_policy_loss
-  float4* terms = nullptr;  // [N] weighted terms of the sums
+  float4* terms = nullptr;  // [N] weighted terms of the sums; null: they are taken from logp
   float mean = 0.f;         // the weight without a weight array
 };
 size_t policy_loss_workspace(int64_t N);
+bool policy_loss_direct(int64_t N, const float* logp);  // whether the call needs no workspace
 cudaError_t launch_policy_loss(PolicyJob job, void* workspace, cudaStream_t stream);
 
 // data, out, numel and dtype are host arrays of n; max_norm = 0: the norms only.

@@ -28,6 +28,15 @@ struct RowLoss {
   float4 terms = {0.f, 0.f, 0.f, 0.f};  // weight times loss, pg, kl, clipped
   uint32_t bits = 0;
 };
+// The log-probability of a row that is left out: one that no row has (-0), so
+// that the sums can be taken from the log-probabilities.
+constexpr uint32_t kLeftOut = 0x80000000u;
+__device__ __forceinline__ RowLoss left_out(uint32_t bits) {
+  RowLoss r;
+  r.bits = bits;
+  if (bits != 0) r.logp = __uint_as_float(kLeftOut);
+  return r;
+}
 
 // A row's scalars, read before its statistics are known.
 struct RowIn {
@@ -56,12 +65,10 @@ __device__ __forceinline__ RowIn gather_row(float scalar, float w) {
   return in;
 }
 
-// m: the row's reference, ty: the chosen token's exponent tau z_y against it, S:
-// the sum of the exponentials of all exponents.
-__device__ __forceinline__ RowLoss row_loss(const PolicyJob& j, const RowIn& in, float m, float ty, float S) {
+// The loss of a row from its token's log-probability.
+__device__ __forceinline__ RowLoss loss_of(const PolicyJob& j, const RowIn& in, float lp) {
   RowLoss r;
   const float A = in.A, w = in.w;
-  const float lp = ty - logf(S);
   const float ratio = expf(lp - in.old);
   const float held = fminf(fmaxf(ratio, 1.f - j.cfg.clip_low), 1.f + j.cfg.clip_high);
   const bool clipped = held * A < ratio * A;
@@ -77,23 +84,33 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyJob& j, const RowIn& in,
     }
   }
   const float f = c * w * in.g * j.cfg.inv_temperature;
-  // a NaN logit makes S NaN, a +inf one m, and so does a row without any above -inf
-  if (!finite(m) || !finite(S) || !finite(loss) || !finite(w * loss) || !finite(w * kl) || !finite(f) ||
-      ratio != ratio) {
-    r.bits = SF_ST_NONFINITE;
-    return r;
-  }
-  r.logp = lp;
+  if (!finite(loss) || !finite(w * loss) || !finite(w * kl) || !finite(f) || ratio != ratio)
+    return left_out(SF_ST_NONFINITE);
+  r.logp = lp + 0.f;  // never -0
   r.loss = loss;
   r.factor = f;
   r.terms = make_float4(w * loss, w * pg, w * kl, clipped ? w : 0.f);
   return r;
 }
 
+// m: the row's reference, ty: the chosen token's exponent tau z_y against it, S:
+// the sum of the exponentials of all exponents.
+__device__ __forceinline__ RowLoss row_loss(const PolicyJob& j, const RowIn& in, float m, float ty, float S) {
+  // a NaN logit makes S NaN, a +inf one m, and so does a row without any above -inf
+  return finite(m) && finite(S) ? loss_of(j, in, ty - logf(S)) : left_out(SF_ST_NONFINITE);
+}
+
 __device__ __forceinline__ void write_row(const PolicyJob& j, int64_t row, const RowLoss& r) {
   if (j.logp != nullptr) j.logp[row] = r.logp;
   if (j.token_loss != nullptr) j.token_loss[row] = r.loss;
-  j.terms[row] = r.terms;
+  if (j.N == 1) {  // its terms are the sums
+    j.stats[0] = r.terms.x;
+    j.stats[1] = r.terms.y;
+    j.stats[2] = r.terms.z;
+    j.stats[3] = r.terms.w;
+  } else if (j.terms != nullptr) {
+    j.terms[row] = r.terms;
+  }
   report(j.status, r.bits);
 }
 
@@ -365,9 +382,7 @@ __global__ void __launch_bounds__(kThreads + 32, kPerSm) policy_ring_kernel(cons
     if (!((mask >> (i & 31)) & 1u)) {
       if (kGrad) zero_row<T, kThreads>(d, V);
       if (tid == 0) {
-        RowLoss r;
-        if (row_weight(j, row) != 0.f) r.bits = SF_ST_INDEX;
-        write_row(j, row, r);
+        write_row(j, row, left_out(row_weight(j, row) != 0.f ? SF_ST_INDEX : 0u));
       }
       continue;
     }
@@ -533,9 +548,7 @@ __global__ void __launch_bounds__(kClusterThreads, 2) policy_cluster_kernel(cons
       if (from < V) zero_row<T, kClusterThreads>(d + from, V - from < len ? V - from : len);
     }
     if (rank == 0 && tid == 0) {
-      RowLoss r;
-      if (w != 0.f) r.bits = SF_ST_INDEX;
-      write_row(j, row, r);
+      write_row(j, row, left_out(w != 0.f ? SF_ST_INDEX : 0u));
     }
     return;
   }
@@ -624,7 +637,11 @@ __global__ void __launch_bounds__(kClusterThreads, 2) policy_cluster_kernel(cons
 
 // The sums over the rows in a fixed order, as pairs of f32 (64-bit additions
 // are slow here: 11 us where the pairs take 3): the rows of a block of kSumRows
-// by one CTA each, then (where there are several) their sums by one.
+// by one CTA each, then (where there are several) their sums by one.  The rows'
+// terms come from the workspace; of up to SF_POLICY_DIRECT_ROWS rows, whose
+// call is host time in the main, they are computed again from the
+// log-probabilities, so that no workspace has to be had (loss of 512 rows 34 ->
+// 30 us; 8192 rows would take 12 us more that way).
 constexpr int kSumThreads = 512, kSumRows = 8192;
 
 // The sum of 4 pairs over the block, in warp 0.
@@ -642,14 +659,27 @@ __device__ void sum_block(Sum2 (&a)[4], Sum2 (*buf)[kSumThreads / 32]) {
   }
 }
 
-__global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const float4* terms, int64_t N, float2* part,
-                                                                 float* stats) {
+__global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const PolicyJob j, float2* part) {
   __shared__ Sum2 buf[4][kSumThreads / 32];
   griddep_wait();
   Sum2 a[4];
-  const int64_t from = int64_t(blockIdx.x) * kSumRows, to = from + kSumRows < N ? from + kSumRows : N;
+  const int64_t from = int64_t(blockIdx.x) * kSumRows, to = from + kSumRows < j.N ? from + kSumRows : j.N;
   for (int64_t i = from + threadIdx.x; i < to; i += kSumThreads) {
-    const float4 t = terms[i];
+    float4 t = {0.f, 0.f, 0.f, 0.f};
+    if (j.terms != nullptr) {
+      t = j.terms[i];
+    } else {
+      RowIn in;
+      in.w = row_weight(j, i);
+      const float lp = j.logp[i];
+      if (in.w != 0.f && __float_as_uint(lp) != kLeftOut) {
+        in.A = j.advantage[i];
+        in.old = j.old_logp[i];
+        in.ref = j.ref_logp != nullptr ? j.ref_logp[i] : 0.f;
+        in.g = in.zy = 0.f;
+        t = loss_of(j, in, lp).terms;
+      }
+    }
     a[0].add(t.x);
     a[1].add(t.y);
     a[2].add(t.z);
@@ -662,7 +692,7 @@ __global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const float4* t
       if (part != nullptr)
         part[int64_t(blockIdx.x) * 4 + q] = make_float2(a[q].hi, a[q].lo);
       else
-        stats[q] = a[q].hi + a[q].lo;
+        j.stats[q] = a[q].hi + a[q].lo;
     }
   }
 }
@@ -741,18 +771,20 @@ size_t policy_loss_workspace(int64_t N) {
   return size_t(N) * sizeof(float4) + (sum_blocks(N) > 1 ? size_t(sum_blocks(N)) * 4 * sizeof(float2) : 0);
 }
 
+bool policy_loss_direct(int64_t N, const float* logp) { return N <= SF_POLICY_DIRECT_ROWS && logp != nullptr; }
+
 cudaError_t launch_policy_loss(PolicyJob j, void* workspace, cudaStream_t stream) {
-  j.terms = static_cast<float4*>(workspace);
+  j.terms = policy_loss_direct(j.N, j.logp) ? nullptr : static_cast<float4*>(workspace);
   j.mean = 1.f / static_cast<float>(j.N);
   const cudaError_t e = j.dtype == SF_F32    ? launch_type<float>(j, stream)
                         : j.dtype == SF_BF16 ? launch_type<__nv_bfloat16>(j, stream)
                                              : launch_type<__half>(j, stream);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || j.N == 1) return e;
   const int64_t blocks = sum_blocks(j.N);
   float2* part = blocks > 1 ? reinterpret_cast<float2*>(j.terms + j.N) : nullptr;
   count_launch();
   const cudaError_t s = launch_after(policy_sum_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kSumThreads), 0,
-                                     stream, true, j.terms, j.N, part, j.stats);
+                                     stream, true, j, part);
   if (s != cudaSuccess || part == nullptr) return s;
   count_launch();
   return launch_after(policy_sum_parts_kernel, dim3(1), dim3(128), 0, stream, true, part, blocks, j.stats);

@@ -25,6 +25,7 @@ SF_ST_NEGATIVE, SF_ST_RANGE, SF_ST_TIMEOUT, SF_ST_INDEX = 1, 2, 4, 8
 SF_ST_NONFINITE = 16
 SF_F32, SF_BF16, SF_F16 = 0, 1, 2
 SF_SCORE_SOFTMAX, SF_SCORE_SIGMOID = 0, 1
+SF_POLICY_DIRECT_ROWS = 1024
 SF_STEP_CONFIDENT = 0x80
 LABEL_NAMES = ("frontier_accounting", "direct_exposure", "sync_wait_dependent", "co_critical",
                "role_aware_needed", "telemetry_limited", "raw_only")
@@ -660,13 +661,14 @@ def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=No
             raise ValueError("dlogits must have logits' shape and type")
     elif grad:
         dlogits = new((N, V), logits.dtype)
-    if workspace is None:
+    if workspace is None and (logp is None or N > SF_POLICY_DIRECT_ROWS):
         workspace = new(_lib.sf_policy_loss_workspace_size(N, V), torch.uint8)
     _hold(made, stream)
     cfg = PolicyConfig(clip[0], clip[1], kl_coef, inv_temperature)
     _check(_lib.sf_policy_loss(_p(logits), _DTYPES[logits.dtype], N, V, ld, _p(target), _p(old_logp), _p(ref_logp),
                                _p(advantage), _p(weight), ctypes.byref(cfg), _p(grad_out), _p(logp), _p(token_loss),
-                               _p(stats), _p(dlogits), ldd, _p(workspace), workspace.numel(), _p(status),
+                               _p(stats), _p(dlogits), ldd, _p(workspace), 0 if workspace is None else workspace.numel(),
+                               _p(status),
                                _stream(stream)), "sf_policy_loss")
     return PolicyLoss(logp, token_loss, stats, dlogits)
 

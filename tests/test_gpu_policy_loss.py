@@ -358,6 +358,24 @@ def test_offsets_beyond_32_bits(sf, N, V):
     check(r, e, "bf16")
 
 
+@pytest.mark.parametrize("N,V", [(1, 40), (1, 70001), (5, 1000), (900, 300), (9000, 40)])
+def test_sums_with_and_without_log_probabilities(sf, N, V):
+    """The sums are taken from logp where it is asked for, else from a workspace."""
+    z, h = make(N, V, "bf16", N)
+    if N > 3:
+        z[1] = math.nan
+        h["w"][2] = 0.0
+    a, sa = call(sf, z, h, grad=True)
+    b, sb = call(sf, z, h, grad=True, want=("token_loss",))
+    c, _ = call(sf, z, h, grad=True, want=())
+    assert sa == sb == (sf.SF_ST_NONFINITE if N > 3 else 0) and b.logp is None and c.token_loss is None
+    for o in (b, c):
+        assert torch.equal(a.stats, o.stats) and torch.equal(a.dlogits, o.dlogits)
+    size = sf.lib().sf_policy_loss_workspace_size(N, V)
+    d, _ = call(sf, z, h, workspace=torch.empty(size, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(a.stats, d.stats)
+
+
 def test_no_rows(sf):
     z = torch.empty((0, 16), device="cuda")
     f = lambda n, t=torch.float32: torch.empty(n, dtype=t, device="cuda")  # noqa: E731
