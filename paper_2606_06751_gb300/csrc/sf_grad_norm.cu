@@ -11,7 +11,9 @@
 // there.  A second kernel adds what the CTAs found (every CTA for itself: they
 // are few) and, for clipping, scales the data, from the end of each range
 // back, as L2 still holds what was read last.  All sums go in a fixed order.
-// Bound by memory: a conversion and a multiply-add an element.
+// Bound by memory: a conversion and a multiply-add an element.  1.5 G bf16 values
+// of 400 tensors are normed in 418 us (7.2 TB/s), 1 G of 300 clipped into other
+// buffers in 932 us (6.4 TB/s over two reads and a write).
 #include <algorithm>
 
 #include "sf_float.cuh"
@@ -337,8 +339,8 @@ int64_t packs_of(int64_t numel, int32_t dtype) {
 }
 
 // The ranges of one list.  Long ranges are a CTA's: fewer places of memory are
-// read at a time (2 GB of gradients clipped into other buffers: 911 us, with a
-// warp's ranges 970), short ones a warp's (150 tensors of 60 MB in all: the
+// read at a time (2 GB of gradients clipped into other buffers: 932-944 us, with
+// a warp's ranges 970), short ones a warp's (150 tensors of 60 MB in all: the
 // warps of a CTA would take its tensors one after another).
 struct Cut {
   int32_t group;

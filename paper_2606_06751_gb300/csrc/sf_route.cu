@@ -12,7 +12,10 @@
 // margin for their error; only the gathered ones are computed as the operator
 // defines them, which decides.  Where the margin leaves a group's choice open,
 // or more than 32 values are gathered, the token's values are all computed
-// exactly, and taken one by one if there are too many equal ones.
+// exactly, and taken one by one if there are too many equal ones.  65536 tokens
+// to 8 of 256 experts in 8 groups, f32: 52 us, 520 instructions a token at 62 % of
+// the issue slots (memory would allow 11 us); taking the k largest one by one
+// from all values, a warp a token, 150 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -557,7 +560,10 @@ RouteShape shape_of(const RouteJob& j, int LPT) {
 // Gradient: the chosen experts' lanes put their own values (or, where all
 // experts have a gradient, their upstream gradients) into a row of zeros in
 // shared memory, from which every lane takes its NV.  Several tokens a warp:
-// their reads, two of which wait for one another, are in flight together.
+// their reads, two of which wait for one another, are in flight together.  Bound
+// by the latency of those reads, so registers are kept few for more warps
+// (100003 x 160 bf16 over all experts: 51 us with three CTAs an SM, 33 with four).
+// 65536 x 256 f32: 17 us (4.0 TB/s written), over all experts 23 us (5.8 TB/s).
 template <int NV, int LPT, bool kDense>
 __global__ void __launch_bounds__(kThreads, NV > 16 ? 2 : kDense ? 4 : 5) route_grad_kernel(const RouteGradJob j, const bool packs) {
   constexpr int kTokens = 32 / LPT;  // of a warp
