@@ -572,7 +572,8 @@ sf_status sf_route_experts_grad(const void* logits, int32_t dtype, int64_t T, in
  *               sf_dtype.  Read before the call returns.
  *   norm        [1] f32: sqrt(sum of squares over all tensors)
  *   tensor_norm [n] f32 (nullable): each tensor's own
- *   workspace   device, 16-byte aligned, sf_grad_workspace_size(n) bytes
+ *   workspace   device, 16-byte aligned, sf_grad_workspace_size(n) bytes; may be
+ *               null where sf_grad_needs_workspace says 0
  * Squares that leave the range of 32 bits are summed in 64.  Where the norm is
  * not finite (or above the largest f32) SF_ST_NONFINITE is set and `norm`
  * holds what it is; tensor_norm tells which tensors are the cause.
@@ -598,6 +599,10 @@ sf_status sf_grad_clip(const void* const* data, void* const* out, const int64_t*
 /* Workspace bytes sf_grad_norm and sf_grad_clip need for n tensors on the
    current device; 0 on bad arguments. */
 size_t sf_grad_workspace_size(int64_t n);
+
+/* Whether sf_grad_norm and sf_grad_clip need a workspace for these tensors
+   (HOST arrays): 0 for up to 6 MB, which take one launch, and on bad arguments. */
+int32_t sf_grad_needs_workspace(const int64_t* numel, const int32_t* dtype, int64_t n);
 
 #ifdef __cplusplus
 }

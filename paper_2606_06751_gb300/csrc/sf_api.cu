@@ -82,7 +82,7 @@ sf_status grad_args_ok(const GradJob& j, const void* workspace, size_t workspace
   }
   if (!aligned(j.norm, 4) || !aligned(j.coef, 4) || !aligned(j.tensor_norm, 4) || !aligned(j.status, 4))
     return SF_EINVAL_ALIGN;
-  if (!workspace || workspace_bytes < grad_workspace(j.n)) return SF_EWORKSPACE;
+  if (workspace ? workspace_bytes < grad_workspace(j.n) : !grad_small(j.numel, j.dtype, j.n)) return SF_EWORKSPACE;
   if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
   return SF_OK;
 }
@@ -561,6 +561,11 @@ sf_status sf_policy_loss(const void* logits, int32_t dtype, int64_t N, int64_t V
 }
 
 size_t sf_grad_workspace_size(int64_t n) { return n < 0 || n > kMaxTensors ? 0 : grad_workspace(n); }
+
+int32_t sf_grad_needs_workspace(const int64_t* numel, const int32_t* dtype, int64_t n) {
+  if (!sizes_ok(numel, n) || (n > 0 && !dtype)) return 0;
+  return grad_small(numel, dtype, n) ? 0 : 1;
+}
 
 sf_status sf_grad_norm(const void* const* data, const int64_t* numel, const int32_t* dtype, int64_t n, float* norm,
                        float* tensor_norm, void* workspace, size_t workspace_bytes, uint32_t* status,

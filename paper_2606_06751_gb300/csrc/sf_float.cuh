@@ -266,6 +266,30 @@ __device__ __forceinline__ V block_sum(V v, V* buf) {
   return s;
 }
 
+// Thread-block clusters.
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+// All threads of the cluster: what was written before (also to another CTA's
+// shared memory) is seen after.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address of `p` in the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  return at;
+}
+
 // Launch `kern`; with `dependent`, as the programmatic dependent of the
 // previous launch on `stream`: it may start while that one drains, and waits
 // for its end in griddep_wait().

@@ -154,6 +154,7 @@ struct GradJob {
   uint32_t* status;
 };
 size_t grad_workspace(int64_t n);
+bool grad_small(const int64_t* numel, const int32_t* dtype, int64_t n);  // whether the call needs no workspace
 cudaError_t launch_grad(const GradJob& job, void* workspace, cudaStream_t stream);
 
 struct RouteJob {

@@ -502,29 +502,6 @@ __global__ void __launch_bounds__(kThreads + 32, kPerSm) policy_ring_kernel(cons
 // 4.2 us (13.4 by one CTA), 32 rows of 131072 with gradients 10.5 us.
 constexpr int kClusterThreads = 512, kClusterWarps = kClusterThreads / 32, kMaxCluster = 8;
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-// All threads of the cluster: what was written before (also to another CTA's
-// shared memory) is seen after.
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// The address of `p` in the shared memory of CTA `rank` of the cluster.
-__device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
-  uint32_t at;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
-  return at;
-}
 __device__ __forceinline__ void store_at(uint32_t at, float2 v) {
   asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(v.x), "f"(v.y) : "memory");
 }

@@ -13,7 +13,7 @@
 // defines them, which decides.  Where the margin leaves a group's choice open,
 // or more than 32 values are gathered, the token's values are all computed
 // exactly, and taken one by one if there are too many equal ones.  65536 tokens
-// to 8 of 256 experts in 8 groups, f32: 52 us, 520 instructions a token at 62 % of
+// to 8 of 256 experts in 8 groups, f32: 48 us, 460 instructions a token at 62 % of
 // the issue slots (memory would allow 11 us); taking the k largest one by one
 // from all values, a warp a token, 150 us.
 #include <algorithm>
@@ -57,6 +57,16 @@ __device__ __forceinline__ float token_max(float v) {
   } else {
 #pragma unroll
     for (int o = LPT / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
+    return v;
+  }
+}
+template <int LPT>
+__device__ __forceinline__ uint32_t token_max(uint32_t v) {
+  if constexpr (LPT == 32) {
+    return __reduce_max_sync(kFull, v);
+  } else {
+#pragma unroll
+    for (int o = LPT / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(kFull, v, o));
     return v;
   }
 }
@@ -168,6 +178,18 @@ __device__ __forceinline__ uint64_t rank_key(float u, int e) {
   return uint64_t((b & 0x80000000u) ? ~b : b | 0x80000000u) << 32 | (0xffffffffu - static_cast<uint32_t>(e));
 }
 
+// An ordered integer of a lane's value; -inf is 0 but for the lane's bits.
+template <int LPT>
+__device__ __forceinline__ uint32_t lane_key(float u, int slot) {
+  const uint32_t b = __float_as_uint(u);
+  const uint32_t k = u == neg_inf() ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+  return (k & ~uint32_t(LPT - 1)) | static_cast<uint32_t>(LPT - 1 - slot);
+}
+// The value of an ordered integer; 0 (no value): -inf.
+__device__ __forceinline__ float key_value(uint32_t k) {
+  return k == 0 ? neg_inf() : __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
+}
+
 // How a token's experts lie in its lanes: a group's in `lanes` lanes (a power of
 // two), `each` consecutive ones a lane.
 struct RouteShape {
@@ -181,7 +203,7 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
   constexpr int kRounds = Gather<LPT>::kRounds, kGathered = Gather<LPT>::kMost;
   constexpr int kPad = NV % 4 == 0 ? 4 : 0;  // of a lane's biases, which then lie in banks of their own
   extern __shared__ __align__(16) float dynamic[];  // biases, loads [E]
-  __shared__ uint64_t all_keys[kWarps][kTokens][kGathered];  // choice value and expert, by rank_key
+  __shared__ __align__(16) uint64_t all_keys[kWarps][kTokens][kGathered];  // choice value and expert, by rank_key
   __shared__ float2 all_picked[kWarps][kTokens][32];         // (score or weight, expert) of the chosen
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = lane & (LPT - 1), first_lane = lane - slot;
   const int E = static_cast<int>(j.E), k = j.cfg.k, dtype = j.dtype, top_groups = j.cfg.top_groups;
@@ -261,27 +283,35 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
           all.merge(__shfl_xor_sync(kFull, all.a, o), __shfl_xor_sync(kFull, all.b, o));
         const float value = j.cfg.group_top > 1 && all.b != neg_inf() ? all.a + all.b : all.a;
         int before = 0, close = 0;  // for certain, perhaps
-        for (int g = 0; g < G; ++g) {
-          const float o = __shfl_sync(kFull, value, first_lane + g * shape.lanes);
-          const bool tie = exact && o == value && g < group;
-          before += o > value + 2.f * margin || tie;
-          // also equal ones, so that infinite values (of biases, or sums of two) are told apart exactly
-          close += exact ? o > value || tie : g != group && o >= value - 2.f * margin;
+        if (exact) {
+          for (int g = 0; g < G; ++g) {
+            const float o = __shfl_sync(kFull, value, first_lane + g * shape.lanes);
+            before += o > value || (o == value && g < group);
+          }
+        } else {
+          const float above = value + 2.f * margin, near = value - 2.f * margin;
+          for (int g = 0; g < G; ++g) {
+            const float o = __shfl_sync(kFull, value, first_lane + g * shape.lanes);
+            before += o > above;
+            close += o >= near;  // itself and equal ones, so that infinite values are told apart exactly
+          }
+          --close;
         }
         open = value != neg_inf() && before < top_groups && close >= top_groups;
         live &= before < top_groups;
       }
       if (!live) best = Top2();
-      // the bound: the k-th largest of the lanes' two largest
-      float bound = neg_inf();
+      // the bound: the k-th largest of the lanes' two largest, as ordered integers whose lowest bits are the
+      // lane's, so that no two are equal (and the bound a little lower than it could be)
+      uint32_t a = lane_key<LPT>(best.a, slot), b = lane_key<LPT>(best.b, slot), kth = 0;
       for (int c = 0; c < k; ++c) {
-        bound = token_max<LPT>(best.a);
-        const uint32_t at = token_bits<LPT>(__ballot_sync(kFull, best.a == bound), lane);
-        if (slot == __ffs(static_cast<int>(at)) - 1) {
-          best.a = best.b;
-          best.b = neg_inf();
+        kth = token_max<LPT>(a);
+        if (a == kth) {
+          a = b;
+          b = 0;
         }
       }
+      float bound = key_value(kth & ~uint32_t(LPT - 1));
       bound = fmaxf(bound - margin, -3.402823466e38f);  // not -inf: no expert that is not available
       // the values that may be among the k largest
       uint32_t mine = 0;
@@ -347,12 +377,13 @@ __global__ void __launch_bounds__(kThreads, NV > 8 ? 3 : 4) route_kernel(const R
         }
       }
       __syncwarp();
-      for (int i = 0; i < n; ++i) {
-        const uint64_t o = keys[i];
+      for (int i = 0; i < n; i += 2) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(keys + i);
+        const uint64_t second = i + 1 < n ? o.y : 0;
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
           if (r * LPT >= most) break;
-          rank[r] += o > key[r];
+          rank[r] += (o.x > key[r]) + (second > key[r]);
         }
       }
 #pragma unroll
@@ -561,11 +592,12 @@ RouteShape shape_of(const RouteJob& j, int LPT) {
 // experts have a gradient, their upstream gradients) into a row of zeros in
 // shared memory, from which every lane takes its NV.  Several tokens a warp:
 // their reads, two of which wait for one another, are in flight together.  Bound
-// by the latency of those reads, so registers are kept few for more warps
-// (100003 x 160 bf16 over all experts: 51 us with three CTAs an SM, 33 with four).
-// 65536 x 256 f32: 17 us (4.0 TB/s written), over all experts 23 us (5.8 TB/s).
+// by the latency of those reads: as many tokens a warp, and warps an SM, as the
+// registers allow (100003 x 160 bf16 over all experts: 35 us with two tokens of 16
+// lanes, 29 with four of 8).  65536 x 256 f32: 17 us (4.0 TB/s written), over all
+// experts 23 us (5.8 TB/s).
 template <int NV, int LPT, bool kDense>
-__global__ void __launch_bounds__(kThreads, NV > 16 ? 2 : kDense ? 4 : 5) route_grad_kernel(const RouteGradJob j, const bool packs) {
+__global__ void __launch_bounds__(kThreads, NV > 16 ? 3 : kDense ? 4 : 5) route_grad_kernel(const RouteGradJob j, const bool packs) {
   constexpr int kTokens = 32 / LPT;  // of a warp
   extern __shared__ __align__(16) float rows[];  // [kWarps * 32][NV]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = lane & (LPT - 1);
@@ -718,9 +750,11 @@ cudaError_t launch_route(RouteJob j, bool accumulate, cudaStream_t stream) {
 }
 
 cudaError_t launch_route_grad(const RouteGradJob& j, cudaStream_t stream) {
-  // as few lanes a token as have its k experts one each and its row in 16 values
+  // as few lanes a token as have its k experts one each and its row in 16 to 32 values
   if (j.cfg.k <= 8 && j.E <= 64) return launch_grad_lanes<8, 8>(j, stream);
   if (j.cfg.k <= 8 && j.E <= 128) return launch_grad_lanes<16, 8>(j, stream);
+  if (j.cfg.k <= 8 && j.E <= 192) return launch_grad_lanes<24, 8>(j, stream);
+  if (j.cfg.k <= 8 && j.E <= 256) return launch_grad_lanes<32, 8>(j, stream);
   if (j.cfg.k <= 16 && j.E <= 128) return launch_grad_lanes<8, 16>(j, stream);
   if (j.cfg.k <= 16 && j.E <= 256) return launch_grad_lanes<16, 16>(j, stream);
   if (j.E <= 256) return launch_grad_lanes<8, 32>(j, stream);

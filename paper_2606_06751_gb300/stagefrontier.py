@@ -112,6 +112,8 @@ def _load():
     L.sf_label_windows_workspace_size.restype = ctypes.c_size_t
     L.sf_rank_workspace_size.argtypes = [I, I, I]
     L.sf_rank_workspace_size.restype = ctypes.c_size_t
+    L.sf_grad_needs_workspace.argtypes = [P, P, I]
+    L.sf_grad_needs_workspace.restype = I32
     L.sf_grad_workspace_size.argtypes = [I]
     L.sf_grad_workspace_size.restype = ctypes.c_size_t
     L.sf_policy_loss_workspace_size.argtypes = [I, I]
@@ -789,18 +791,19 @@ def _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, worksp
     elif per_tensor:
         tensor_norm = new(n)
     at = lambda a: a.buffer_info()[0]  # noqa: E731
-    if workspace is None:
+    if workspace is None and _lib.sf_grad_needs_workspace(at(numel), at(dtype), n):
         workspace = new(_lib.sf_grad_workspace_size(n), torch.uint8)
+    size = 0 if workspace is None else workspace.numel()
     if max_norm is None:
         _hold(made, stream)
-        _check(_lib.sf_grad_norm(at(ptr), at(numel), at(dtype), n, _p(norm), _p(tensor_norm), _p(workspace),
-                                 workspace.numel(), _p(status), _stream(stream)), "sf_grad_norm")
+        _check(_lib.sf_grad_norm(at(ptr), at(numel), at(dtype), n, _p(norm), _p(tensor_norm), _p(workspace), size,
+                                 _p(status), _stream(stream)), "sf_grad_norm")
         return GradNorm(norm, None, tensor_norm)
     coef = new(1) if coef is None else _vec(coef, 1, torch.float32, "coef")
     _hold(made, stream)
     _check(_lib.sf_grad_clip(at(ptr), None if out_ptr is None else at(out_ptr), at(numel), at(dtype), n, max_norm, eps,
-                             _p(norm), _p(coef), _p(tensor_norm), _p(workspace), workspace.numel(), _p(status),
-                             _stream(stream)), "sf_grad_clip")
+                             _p(norm), _p(coef), _p(tensor_norm), _p(workspace), size, _p(status), _stream(stream)),
+           "sf_grad_clip")
     return GradNorm(norm, coef, tensor_norm)
 
 

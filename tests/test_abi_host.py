@@ -203,11 +203,15 @@ def test_host_validation_of_training_step_operators(sf):
             assert clip(most=most, **kw) == sf.SF_EINVAL, kw
         for kw in (dict(data=(FAKE + 2, far)), dict(data=(FAKE, far + 1)), dict(norm=FAKE + 2), dict(ws=FAKE + 8)):
             assert clip(most=most, **kw) == sf.SF_EINVAL_ALIGN, kw
-        assert clip(most=most, ws=None) == sf.SF_EWORKSPACE and clip(most=most, size=64) == sf.SF_EWORKSPACE
+        assert clip(most=most, size=64) == sf.SF_EWORKSPACE
+        assert clip(most=most, ws=None, numel=(2 << 20, 5)) == sf.SF_EWORKSPACE  # smaller lists need none
     for kw in (dict(most=0.0), dict(most=float("nan")), dict(eps=-1.0), dict(eps=float("inf")),
                dict(out=(FAKE + 16, far)), dict(out=(None, far))):
         assert clip(**kw) == sf.SF_EINVAL, kw
     assert L.sf_grad_norm(None, None, None, 1, FAKE, None, FAKE, 1 << 20, None, None) == sf.SF_EINVAL
     assert L.sf_grad_norm(None, None, None, (1 << 20) + 1, FAKE, None, FAKE, 1 << 20, None, None) == sf.SF_EINVAL
     assert L.sf_grad_workspace_size(-1) == 0 and L.sf_grad_workspace_size(10) > 0
+    sizes, types = (ctypes.c_int64 * 2)(3 << 20, 16), (ctypes.c_int32 * 2)(1, 0)
+    assert L.sf_grad_needs_workspace(sizes, types, 1) == 0 and L.sf_grad_needs_workspace(sizes, types, 2) == 1
+    assert L.sf_grad_needs_workspace(None, None, 0) == 0
     assert sf.launch_count() == 0

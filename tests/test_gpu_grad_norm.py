@@ -120,6 +120,21 @@ def test_many_tensors(sf, n):
     check(sf, grads, 2.0)
 
 
+@pytest.mark.parametrize("n,each", [(24, 50000), (960, 1000), (961, 1000), (3, 1048576), (3, 1048577), (200, 7)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_around_the_size_of_one_launch(sf, n, each, packed):
+    """Up to 6 MB in up to 960 tensors go by one cluster, without a workspace; the same bits with one."""
+    sizes = [each + (i % 3 - 1) * (i % 5) for i in range(n)] if n > 3 else [each] * n
+    grads, _ = tensors(sizes, [["bf16", "f32", "f16"][i % 3] for i in range(n)] if n > 3 else ["bf16"] * n, n, packed)
+    check(sf, grads)
+    a = sf.sf_grad_norm(grads, per_tensor=True)
+    ws = torch.empty(sf.lib().sf_grad_workspace_size(n), dtype=torch.uint8, device="cuda")
+    b = sf.sf_grad_norm(grads, per_tensor=True, workspace=ws)
+    assert torch.equal(a.norm, b.norm) and torch.equal(a.tensor_norm, b.tensor_norm)
+    check(sf, grads, 0.5, [torch.empty_like(g) for g in grads])
+    check(sf, grads, 0.5)
+
+
 def test_equal_values(sf):
     """Sums of equal squares, which round the same way over and over in 32 bits."""
     for t, v in (("f32", 0.1), ("bf16", 1.1015625), ("f16", 0.3)):
