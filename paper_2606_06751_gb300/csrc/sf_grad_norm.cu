@@ -272,6 +272,10 @@ __global__ void __launch_bounds__(kThreads)
   if (blockIdx.x == 0) finish_norm(o);
 }
 
+// Fewer packs in flight than the sums have: each has its result beside it (with
+// eight the registers do not do).
+constexpr int kScaleUnroll = 4;
+
 template <typename T>
 __device__ void scale_piece(const T* p, T* q, int64_t n, float coef, const Share& w) {
   const int lane = w.lane;
@@ -297,22 +301,22 @@ __device__ void scale_piece(const T* p, T* q, int64_t n, float coef, const Share
     else
       store_elements(q + head + at * N, u);
   };
-  const int64_t step = 32 * kUnroll * w.group;
-  int64_t i = nv - 1 - lane - 32 * kUnroll * w.sub;
-  for (; i - (kUnroll - 1) * 32 >= 0; i -= step) {
-    uint4 u[kUnroll];
+  const int64_t step = 32 * kScaleUnroll * w.group;
+  int64_t i = nv - 1 - lane - 32 * kScaleUnroll * w.sub;
+  for (; i - (kScaleUnroll - 1) * 32 >= 0; i -= step) {
+    uint4 u[kScaleUnroll];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) u[k] = load16(p + head + (i - k * 32) * N);
+    for (int k = 0; k < kScaleUnroll; ++k) u[k] = load16(p + head + (i - k * 32) * N);
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) store(i - k * 32, scaled(u[k]));
+    for (int k = 0; k < kScaleUnroll; ++k) store(i - k * 32, scaled(u[k]));
   }
   if (i >= 0) {
-    uint4 u[kUnroll];
+    uint4 u[kScaleUnroll];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k)
+    for (int k = 0; k < kScaleUnroll; ++k)
       if (i - k * 32 >= 0) u[k] = load16(p + head + (i - k * 32) * N);
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k)
+    for (int k = 0; k < kScaleUnroll; ++k)
       if (i - k * 32 >= 0) store(i - k * 32, scaled(u[k]));
   }
   __syncwarp();
@@ -337,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm)
 // All of it by one cluster: each warp's sums of squares go to the first CTA's
 // shared memory, which adds them up, in the same order whatever came first, and
 // hands the coefficient back.
-constexpr int kSmallCtas = 8, kSmallThreads = 512, kSmallWarps = kSmallCtas * kSmallThreads / 32;
+constexpr int kSmallCtas = 16, kSmallThreads = 512, kSmallWarps = kSmallCtas * kSmallThreads / 32;
 constexpr int64_t kSmallPacks = 6 << 16;  // 6 MB
 
 template <int M, bool kClip>
@@ -448,9 +452,12 @@ cudaError_t launch_small(TensorList<M>& list, const NormOut& o, bool clip, cudaS
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   void* params[] = {&list, const_cast<NormOut*>(&o)};
+  const void* kern = clip ? reinterpret_cast<const void*>(grad_small_kernel<M, true>)
+                          : reinterpret_cast<const void*>(grad_small_kernel<M, false>);
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);  // 16 CTAs
+  if (e != cudaSuccess) return e;
   count_launch();
-  return cudaLaunchKernelExC(&cfg, clip ? reinterpret_cast<const void*>(grad_small_kernel<M, true>)
-                                        : reinterpret_cast<const void*>(grad_small_kernel<M, false>), params);
+  return cudaLaunchKernelExC(&cfg, kern, params);
 }
 
 template <int M>
@@ -533,9 +540,10 @@ size_t grad_workspace(int64_t n) {
 cudaError_t launch_grad(const GradJob& j, void* workspace, cudaStream_t stream) {
   if (grad_small(j.numel, j.dtype, j.n)) workspace = nullptr;  // by size alone: the order of the sums is one
   if (j.n <= 32) return launch_lists<32>(j, workspace, stream);
-  if (j.n <= 128) return launch_lists<128>(j, workspace, stream);
-  if (j.n <= 256) return launch_lists<256>(j, workspace, stream);
-  if (j.n <= 512) return launch_lists<512>(j, workspace, stream);
+  if (j.n <= 64) return launch_lists<64>(j, workspace, stream);
+  if (j.n <= 160) return launch_lists<160>(j, workspace, stream);
+  if (j.n <= 320) return launch_lists<320>(j, workspace, stream);
+  if (j.n <= 480) return launch_lists<480>(j, workspace, stream);
   return launch_lists<kListMax>(j, workspace, stream);
 }
 
