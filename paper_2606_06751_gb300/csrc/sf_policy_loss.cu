@@ -207,7 +207,8 @@ __device__ __forceinline__ uint4 load_shared16(const void* p) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"(smem_u32(p)));
+               : "r"(smem_u32(p))
+               : "memory");
   return v;
 }
 
@@ -362,6 +363,11 @@ __global__ void __launch_bounds__(kThreads + 32, kPerSm) policy_ring_kernel(cons
 #pragma unroll
     for (int p = 0; p < kPacks; ++p)
       u[p] = p * kThreads + tid < left ? load_shared16(src + p * kThreads * 16) : lowest_pack(T());
+  };
+  // The slot may be filled again.  After the packs' use, and with a fence: without one nothing orders these
+  // reads before the next copy's writes, and packs of the chunk after next came out of reads that went late.
+  const auto done_chunk = [&] {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) mbar_arrive(empty + slot);
     if (++slot == uint32_t(slots)) {
@@ -415,6 +421,7 @@ __global__ void __launch_bounds__(kThreads + 32, kPerSm) policy_ring_kernel(cons
 #pragma unroll
         for (int q = 0; q < N / 2; ++q) a.add(z2[q], e);
       }
+      done_chunk();
     }
     const float wr = warp_max(a.r);
     const float ws = warp_sum(a.sum() * exp2_fast(Ref::between(a.r, wr, scale)));
@@ -439,6 +446,7 @@ __global__ void __launch_bounds__(kThreads + 32, kPerSm) policy_ring_kernel(cons
         for (int c = 0; c < rp.packs; c += kChunk) {  // copies that are on their way all the same
           uint4 u[kPacks];
           next_chunk(0, u);
+          done_chunk();
         }
         for (int q = tid; q < V; q += kThreads) {
           const float g = q == r.y ? r.chosen : r.y < 0 ? 0.f : exp2_fast((to_f32(z[q]) - r.r) * scale) * r.p;
@@ -454,6 +462,7 @@ __global__ void __launch_bounds__(kThreads + 32, kPerSm) policy_ring_kernel(cons
       for (int c = 0; c < rp.packs; c += kChunk) {
         uint4 u[kPacks];
         next_chunk(0, u);
+        done_chunk();
       }
       zero_row<T, kThreads>(d, V);
       continue;
@@ -490,6 +499,7 @@ __global__ void __launch_bounds__(kThreads + 32, kPerSm) policy_ring_kernel(cons
           if (at == chosen) d[o.y] = from_f32<T>(o.chosen);
         }
       }
+      done_chunk();
     }
   }
   if (timeout) report(j.status, SF_ST_TIMEOUT);

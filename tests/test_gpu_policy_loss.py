@@ -415,3 +415,25 @@ def test_refusals(sf):
     with pytest.raises(ValueError):
         sf.sf_policy_loss(z, dlogits=torch.empty(4, 15, device="cuda"), **a)
     assert sf.launch_count() == before
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,V,ld,offset,ldd", [(320, 40001, 40003, 5, 40001), (320, 40008, 40008, 0, 40009),
+                                               (320, 40008, 40008, 0, 40008), (640, 20001, 20001, 0, 20001)])
+def test_calls_repeat(sf, dtype, N, V, ld, offset, ldd):
+    # every call the same bits: no pack of a chunk that came later
+    z, h = make(N, V, dtype, V + ldd, ld, offset)
+    flat = torch.empty(N * ldd, dtype=TYPES[dtype], device="cuda")
+    d = torch.as_strided(flat, (N, V), (ldd, 1), 0)
+    e = reference(h)
+    e["y"] = h["y"]
+    first = None
+    for _ in range(12):
+        flat.fill_(7.0)
+        r, st = call(sf, z, h, dlogits=d)
+        assert st == 0
+        if first is None:
+            check(r, e, dtype)
+            first = d.clone(), r.logp.clone(), r.stats.clone()
+        for a, b in zip(first, (d, r.logp, r.stats)):
+            assert torch.equal(a, b)
