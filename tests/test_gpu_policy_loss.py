@@ -437,3 +437,63 @@ def test_calls_repeat(sf, dtype, N, V, ld, offset, ldd):
             first = d.clone(), r.logp.clone(), r.stats.clone()
         for a, b in zip(first, (d, r.logp, r.stats)):
             assert torch.equal(a, b)
+
+
+SUM_UNITS = 64  # roundings of 2^-24 in a row's sum, whatever the row's length: see test_equal_terms
+
+
+def loss_of_rows(sf, z, y, lp, rows, grad, tau=1.0):
+    """sf_policy_loss of the given rows of z, the others without weight; the gradient's factor."""
+    N = z.shape[0]
+    w = torch.zeros(N, device="cuda")
+    w[rows] = 1.0
+    old = torch.full((N,), lp + 0.1, device="cuda")
+    st = sf.new_status("cuda")
+    r = sf.sf_policy_loss(z, torch.full((N,), y, device="cuda"), old, torch.ones(N, device="cuda"), weight=w,
+                          clip=(LO, HI), inv_temperature=tau, grad=grad, status=st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    return r, -math.exp(lp - float(old[0]))
+
+
+@pytest.mark.parametrize("N,V", [(40, 131072), (2, 2000003), (2, 1 << 24)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("grad", [False, True])
+def test_equal_terms(sf, N, V, dtype, grad):
+    """Rows of two values: a run at the maximum, then terms so small beside its
+    sum that each addition to a sum in 32 bits rounds the same way.  Held to
+    what does not grow with the row: sums of at most 16 terms (15 roundings),
+    their halves (1), a compensated sum (3), reductions over lanes and warps
+    with one exponential each (2 (5 + 5)), the terms' own exponentials (4, and
+    15 for an argument of 22) and the last reductions' products (2): 60 units
+    of 2^-24; then 4 units of log S for the logarithm and the result."""
+    z = torch.zeros((N, V), dtype=TYPES[dtype], device="cuda")
+    rows = [0, N - 1]
+    for first in (8192, 15872):
+        for low in (13.9375, 14.625, 15.3125):  # half a unit of sums of 16, 8 and 4, a little less
+            z[rows] = -low
+            z[rows, :first] = 0.0
+            S = first + (V - first) * math.exp(-low)
+            lp = -math.log(S)
+            r, f = loss_of_rows(sf, z, 5, lp, rows, grad)
+            tol = 2.0 ** -24 * (SUM_UNITS + 4 * abs(lp))
+            assert float((r.logp[rows].double() - lp).abs().max()) <= tol
+            if not grad:
+                continue
+            for at, p in ((6, 1 / S), (first - 1, 1 / S), (first, math.exp(-low) / S), (V - 1, math.exp(-low) / S)):
+                want = -f * p
+                err = abs(want) * (4 * tol + 1e-6 + 2.1 * HALF_ULP[dtype]) + TINY[dtype]
+                assert float((r.dlogits[rows, at].double() - want).abs().max()) <= err
+
+
+def test_equal_terms_far_out(sf):
+    """The same in a row that is computed by exact differences from its maximum: neighbours in 32 bits near -1e30."""
+    N, V, first = 2, 2000003, 8192
+    top = np.float32(-1.1e30)
+    low = np.nextafter(top, np.float32(-np.inf))
+    tau = float(np.float32(14.625 / (float(top) - float(low))))
+    z = torch.full((N, V), float(low), device="cuda")
+    z[:, :first] = float(top)
+    lp = -math.log(first + (V - first) * math.exp((float(low) - float(top)) * tau))
+    r, _ = loss_of_rows(sf, z, 5, lp, [0, 1], False, tau)
+    assert float((r.logp.double() - lp).abs().max()) <= 2.0 ** -24 * (SUM_UNITS + 4 * abs(lp))
