@@ -127,7 +127,8 @@ __device__ void zero_row(T* d, int64_t V) {
   for (int64_t i = head + nv * Pack<T>::kN + threadIdx.x; i < V; i += kThreads) d[i] = from_f32<T>(0.f);
 }
 
-// Exponentials of a row against a reference r near its largest logit, as powers
+// Exponentials of a row against a reference r near its largest logit (which is
+// at most kGrow powers of 2 above it, and is r itself if it stands out), as powers
 // of 2 with scale = tau log2(e).  f32: r is a logit and the difference is taken
 // first, which is exact near r.  16-bit types, two values of which come in the
 // bytes of one, take one multiply-add: r is a logit times scale, rounded, and z
@@ -166,14 +167,19 @@ struct Exponent {
 // a chunk adds is summed by itself (at most 16 terms to each of two sums), and
 // the chunks' sums with what each addition rounded off (Kahan): equal terms that
 // are small beside the sum round the same way every time, and a plain sum lost
-// 1.3e-5 of itself that way at 131072 entries and 1.8e-3 at 2^24.
+// 1.3e-5 of itself that way at 131072 entries and 1.8e-3 at 2^24.  The reference
+// follows a logit that exceeds it by more than kGrow powers of 2, not every larger
+// one: each rescaling errs by an exponential and a product, and in a row whose
+// logits rise all along there was one a chunk (more than 9e-6 of the sum at 2^24 entries).  Now what an
+// error counts falls to a 16th from one to the next.
+constexpr float kGrow = 4.f;
 template <typename T>
 struct MaxSum {
   float r = Reference<T>::floor();
   float s = 0.f, lost = 0.f;  // the sum, and what it is short of
   __device__ __forceinline__ void grow(float z, float scale) {
     const float to = Reference<T>::of(z, scale);
-    if (to > r) {
+    if (Reference<T>::between(to, r, scale) > kGrow) {
       const float f = exp2_fast(Reference<T>::between(r, to, scale));
       s *= f;
       lost *= f;

@@ -497,3 +497,20 @@ def test_equal_terms_far_out(sf):
     lp = -math.log(first + (V - first) * math.exp((float(low) - float(top)) * tau))
     r, _ = loss_of_rows(sf, z, 5, lp, [0, 1], False, tau)
     assert float((r.logp.double() - lp).abs().max()) <= 2.0 ** -24 * (SUM_UNITS + 4 * abs(lp))
+
+
+@pytest.mark.parametrize("N,V", [(40, 131072), (2, 2000003), (2, 1 << 24)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("grad", [False, True])
+def test_rising_rows(sf, N, V, dtype, grad):
+    """A maximum that rises from chunk to chunk, and what was summed is scaled
+    again and again: at most six times while the old part still counts, by an
+    exponential and a product of 5 units together."""
+    z = torch.zeros((N, V), dtype=TYPES[dtype], device="cuda")
+    rows = [0, N - 1]
+    for rise in (1.0, 6.0, 40.0):
+        z[rows] = torch.linspace(-rise, 0.0, V, dtype=torch.float64, device="cuda").to(TYPES[dtype])
+        x = z[0].double()
+        lp = float(x[V - 1] - x.logsumexp(0))
+        r, _ = loss_of_rows(sf, z, V - 1, lp, rows, grad)
+        assert float((r.logp[rows].double() - lp).abs().max()) <= 2.0 ** -24 * (SUM_UNITS + 30 + 4 * abs(lp)), rise
