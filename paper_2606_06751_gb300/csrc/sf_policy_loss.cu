@@ -139,10 +139,12 @@ template <typename T>
 struct Reference {
   static constexpr bool kScaled = sizeof(T) == 2;
   static __device__ __forceinline__ float of(float z, float scale) { return kScaled ? z * scale : z; }
-  // what a thread starts from: values far below add nothing, and a row without any other has sum 0
+  // what a thread starts from: values far below add nothing
   static __device__ __forceinline__ float floor() { return kScaled ? -1048576.f : -1e30f; }
+  // a sum has its largest term's 1 unless all logits are below the floor: there the smallest of them are lost,
+  // and a gradient's factor divided by it may not be finite
   static __device__ __forceinline__ bool sound(float r, float S) {
-    return S != 0.f && !(kScaled && r > 1048576.f);
+    return !(S < 0.5f) && !(kScaled && r > 1048576.f);
   }
   // the exponent of 2 of a logit, and of another reference
   static __device__ __forceinline__ float exponent(float z, float r, float scale) {
@@ -170,8 +172,8 @@ struct Exponent {
 // 1.3e-5 of itself that way at 131072 entries and 1.8e-3 at 2^24.  The reference
 // follows a logit that exceeds it by more than kGrow powers of 2, not every larger
 // one: each rescaling errs by an exponential and a product, and in a row whose
-// logits rise all along there was one a chunk (more than 9e-6 of the sum at 2^24 entries).  Now what an
-// error counts falls to a 16th from one to the next.
+// logits rise all along there was one a chunk (more than 9e-6 of the sum at 2^24
+// entries).  Now what an error counts falls to a 16th from one to the next.
 constexpr float kGrow = 4.f;
 template <typename T>
 struct MaxSum {

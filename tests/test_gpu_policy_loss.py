@@ -514,3 +514,31 @@ def test_rising_rows(sf, N, V, dtype, grad):
         lp = float(x[V - 1] - x.logsumexp(0))
         r, _ = loss_of_rows(sf, z, V - 1, lp, rows, grad)
         assert float((r.logp[rows].double() - lp).abs().max()) <= 2.0 ** -24 * (SUM_UNITS + 30 + 4 * abs(lp)), rise
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("N,V", [(3, 1000), (320, 1000), (2, 140000)])
+@pytest.mark.parametrize("below", [8, 100, 120, 125])
+def test_logits_just_below_the_reference(sf, dtype, N, V, below):
+    """A row whose largest logit times tau log2(e) lies a little below -2^20, the
+    least reference of 16-bit rows: no power of 2 there may stand for its sum."""
+    z = torch.zeros((N, V), dtype=TYPES[dtype], device="cuda")
+    z[0] = -2.0
+    z[0, 10:14] = -1.0
+    tau = float(np.float32((2.0 ** 20 + below) * math.log(2.0)))
+    lp = -math.log(4.0)
+    w = torch.zeros(N, device="cuda")
+    w[0] = 0.05
+    y, old = torch.full((N,), 11, device="cuda"), torch.full((N,), lp + 0.1, device="cuda")
+    st = sf.new_status("cuda")
+    r = sf.sf_policy_loss(z, y, old, torch.ones(N, device="cuda"), weight=w, clip=(LO, HI), inv_temperature=tau,
+                          grad=True, status=st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    assert abs(float(r.logp[0]) - lp) <= DLP
+    f = -math.exp(-0.1) * tau * 0.05
+    want = np.zeros(V)
+    want[10:14] = -f / 4
+    want[11] += f
+    err = np.abs(want) * (8 * DLP + 2.1 * HALF_ULP[dtype])
+    assert np.all(np.abs(r.dlogits[0].double().cpu().numpy() - want) <= err)
