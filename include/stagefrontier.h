@@ -484,7 +484,8 @@ typedef struct sf_policy_config {
  *   weight    [N] f32 (nullable: 1/N each)
  *   grad_out  f32 (device, nullable: 1), the upstream gradient g of the loss
  *   logp      [N] f32 (nullable), lp;  token_loss [N] f32 (nullable), loss
- *   stats     [4] f32: the sums over rows of w times loss, pg, kl, clipped
+ *   stats     [4] f32: the sums over rows of w times loss, pg, kl, clipped; a sum
+ *             beyond the largest f32 is infinite
  *   dlogits   [N] rows of V, ldd elements apart, of type dtype (nullable: no
  *             gradient); may be `logits` itself with ldd = ld, else the two
  *             must not overlap.  Rounded once, to nearest even.

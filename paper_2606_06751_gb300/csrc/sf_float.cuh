@@ -230,6 +230,8 @@ struct Sum2 {
     lo += (hi - (s - b)) + (v - b);
     hi = s;
   }
+  // rounded; lo is NaN once a sum has overflowed
+  __device__ __forceinline__ float value() const { return finite(hi) ? hi + lo : hi; }
 };
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll

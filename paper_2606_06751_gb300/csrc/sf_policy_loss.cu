@@ -702,9 +702,9 @@ __global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const PolicyJob
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (part != nullptr)
-        part[int64_t(blockIdx.x) * 4 + q] = make_float2(a[q].hi, a[q].lo);
+        part[int64_t(blockIdx.x) * 4 + q] = make_float2(a[q].hi, finite(a[q].hi) ? a[q].lo : 0.f);
       else
-        j.stats[q] = a[q].hi + a[q].lo;
+        j.stats[q] = a[q].value();
     }
   }
 }
@@ -719,7 +719,7 @@ __global__ void __launch_bounds__(128) policy_sum_parts_kernel(const float2* par
     s.add(p.y);
   }
   s = warp_sum(s);
-  if ((threadIdx.x & 31) == 0) stats[q] = s.hi + s.lo;
+  if ((threadIdx.x & 31) == 0) stats[q] = s.value();
 }
 
 template <typename T, int kThreads, int kPacks, int kPerSm, bool kGrad>

@@ -542,3 +542,21 @@ def test_logits_just_below_the_reference(sf, dtype, N, V, below):
     want[11] += f
     err = np.abs(want) * (8 * DLP + 2.1 * HALF_ULP[dtype])
     assert np.all(np.abs(r.dlogits[0].double().cpu().numpy() - want) <= err)
+
+
+@pytest.mark.parametrize("N", [3, 2000, 20000])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_sums_beyond_the_result_type(sf, N, sign):
+    """Finite rows whose sum is not: infinite, as one addition of 32 bits would be, whatever form adds up."""
+    z = torch.zeros((N, 4), device="cuda")
+    y = torch.zeros(N, dtype=torch.int64, device="cuda")
+    old = torch.full((N,), -math.log(4.0), device="cuda")
+    A = torch.full((N,), -sign * 2.5e38, device="cuda")
+    st = sf.new_status("cuda")
+    for want in (("logp", "token_loss"), ()):
+        r = sf.sf_policy_loss(z, y, old, A, ref_logp=old, weight=torch.ones(N, device="cuda"), status=st, want=want)
+        torch.cuda.synchronize()
+        stats = r.stats.tolist()
+        assert int(st.item()) == 0
+        assert stats[0] == stats[1] == sign * math.inf
+        assert 0 <= stats[2] <= 1e-6 * N and stats[3] == 0.0
