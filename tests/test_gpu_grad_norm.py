@@ -258,3 +258,41 @@ def test_refusals(sf):
         with pytest.raises(ValueError):
             sf.sf_grad_clip(g, 1.0, out=out)
     assert sf.launch_count() == before
+
+
+def ragged(n, total, seed):
+    """Sizes of n tensors (a few large ones, many small and empty ones, odd counts) and their types."""
+    rng = np.random.default_rng(seed)
+    share = rng.lognormal(0.0, 2.0, n)
+    sizes = [int(v) for v in share / share.sum() * total]
+    sizes[3::11] = [i % 3 for i in range(len(sizes[3::11]))]
+    return sizes, [["bf16", "f32", "f16"][int(v)] for v in rng.integers(0, 3, n)]
+
+
+@pytest.mark.parametrize("n,total", [(5, 150000001), (60, 140000001), (1100, 260000003)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_ranges_of_whole_ctas(sf, n, total, packed):
+    """Lists above 160 MB: a range is a CTA's and its warps take the blocks in
+    turn.  Random values of every type, ragged, in place and into results that
+    start elsewhere, with what lies around them; 1100 tensors are two lists."""
+    sizes, types = ragged(n, total, n)
+    grads, flat = tensors(sizes, types, n, packed)
+    # the first list's bytes: each of up to 152 * 4 * 8 warps' 2048 packs of 16
+    assert sum(g.numel() * g.element_size() for g in grads[:960]) > 160e6
+    check(sf, grads)
+    kept = {t: f.clone() for t, f in flat.items()}
+    for shift in (0, 1, 3):
+        full = {t: torch.full((sum(m + 8 for m, u in zip(sizes, types) if u == t),), 7.0, dtype=TYPES[t], device="cuda")
+                for t in flat}
+        guard = {t: torch.ones(f.numel(), dtype=torch.bool, device="cuda") for t, f in full.items()}
+        at, out = {t: 0 for t in flat}, []
+        for m, t in zip(sizes, types):
+            a = at[t] + 1 + shift
+            out.append(full[t][a:a + m])
+            guard[t][a:a + m] = False
+            at[t] += m + 8
+        check(sf, grads, 0.5, out)
+        for t in flat:
+            assert torch.equal(flat[t], kept[t]) and bool((full[t][guard[t]] == 7).all())
+        del full, guard, out
+    check(sf, grads, 0.5)
