@@ -1,5 +1,5 @@
 // sf_float.cuh - building blocks of the training-step kernels: 16-byte packs
-// of f32, bf16 or f16 values, rows that start at any element, and block sums.
+// of f32, bf16 or f16 values, rows that start at any element, and sums as pairs.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -243,7 +243,8 @@ __device__ __forceinline__ float warp_max(float v) {
   for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
   return v;
 }
-// In a fixed order; the same bits in every lane (two-sum does not depend on its terms' order).
+// In a fixed order.  hi has the same bits in every lane (two-sum does not depend on its terms' order), lo may
+// differ in its last ones: one lane's sum is the one to use.
 __device__ __forceinline__ Sum2 warp_sum(Sum2 s) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -251,20 +252,6 @@ __device__ __forceinline__ Sum2 warp_sum(Sum2 s) {
     s.add(h);
     s.lo += l;
   }
-  return s;
-}
-
-// Sum over the block in a fixed order; every thread gets it.  `buf` holds one
-// value per warp.  Callers that reuse buf synchronise in between.
-template <int kThreads, typename V>
-__device__ __forceinline__ V block_sum(V v, V* buf) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-  __syncthreads();
-  V s = buf[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) s += buf[w];
   return s;
 }
 

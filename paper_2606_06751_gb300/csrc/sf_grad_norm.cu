@@ -46,7 +46,7 @@ struct TensorList {
   double* total;    // of the CTAs
 };
 
-// The tensor that has pack `at` (at < off[count]).
+// The tensor that has pack `at` (at < off[count]): the last one that does not start after it, so never an empty one.
 template <int M>
 __device__ __forceinline__ int tensor_of(const TensorList<M>& list, int64_t at) {
   int lo = 0, hi = list.count;  // off[lo] <= at < off[hi]
@@ -57,7 +57,6 @@ __device__ __forceinline__ int tensor_of(const TensorList<M>& list, int64_t at) 
     else
       hi = mid;
   }
-  while (list.off[lo + 1] <= at) ++lo;  // past empty tensors
   return lo;
 }
 
@@ -66,7 +65,7 @@ struct Share {
   int lane, sub, group;
 };
 
-// Sum of squares of a warp's share of n values at p, in every lane.  A lane sums what
+// Sum of squares of a warp's share of n values at p; lane 0's counts.  A lane sums what
 // it has in flight in 32 bits (at most 16 squares to a sum) and adds that up
 // as a pair, so that equal values do not round the same way over and over.
 // Where the short sums overflow, or are so small that squares may have been
