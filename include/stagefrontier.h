@@ -602,7 +602,9 @@ sf_status sf_grad_clip(const void* const* data, void* const* out, const int64_t*
 size_t sf_grad_workspace_size(int64_t n);
 
 /* Whether sf_grad_norm and sf_grad_clip need a workspace for these tensors
-   (HOST arrays): 0 for up to 6 MB, which take one launch, and on bad arguments. */
+   (HOST arrays): 0 for up to 960 tensors of up to 393216 packs of 16 bytes (6 MB,
+   the last pack of each tensor counted whole), which take one launch and use no
+   workspace, and on bad arguments. */
 int32_t sf_grad_needs_workspace(const int64_t* numel, const int32_t* dtype, int64_t n);
 
 #ifdef __cplusplus

@@ -215,3 +215,21 @@ def test_host_validation_of_training_step_operators(sf):
     assert L.sf_grad_needs_workspace(sizes, types, 1) == 0 and L.sf_grad_needs_workspace(sizes, types, 2) == 1
     assert L.sf_grad_needs_workspace(None, None, 0) == 0
     assert sf.launch_count() == 0
+
+
+def test_which_gradient_lists_need_no_workspace(sf):
+    """As the header says: by tensors and by packs of 16 bytes, the last of each tensor counted whole."""
+    def needs(numel, dtype):
+        n = len(numel)
+        return sf.lib().sf_grad_needs_workspace((ctypes.c_int64 * n)(*numel), (ctypes.c_int32 * n)(*dtype), n)
+
+    packs = 393216
+    for dtype, per in ((sf.SF_F32, 4), (sf.SF_BF16, 8), (sf.SF_F16, 8)):
+        assert needs([packs * per], [dtype]) == 0 and needs([packs * per + 1], [dtype]) == 1
+        assert needs([(packs - 1) * per, 1], [dtype] * 2) == 0 and needs([(packs - 1) * per + 1, 1], [dtype] * 2) == 1
+    assert needs([1] * 960, [sf.SF_F32] * 960) == 0 and needs([1] * 961, [sf.SF_F32] * 961) == 1
+    assert needs([0] * 961, [sf.SF_F32] * 961) == 1
+    for n, dtype in ((961, sf.SF_F32), (1, 3)):  # a null workspace is refused there, bad arguments too
+        p, s, t = (ctypes.c_void_p * n)(*[FAKE] * n), (ctypes.c_int64 * n)(*[1] * n), (ctypes.c_int32 * n)(*[dtype] * n)
+        code = sf.lib().sf_grad_norm(p, s, t, n, FAKE, None, None, 0, None, None)
+        assert code == (sf.SF_EWORKSPACE if n == 961 else sf.SF_EINVAL)
