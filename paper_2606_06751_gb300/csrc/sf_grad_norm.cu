@@ -341,8 +341,10 @@ __global__ void __launch_bounds__(kThreads, kPerSm)
 
 // All of it by one cluster: each warp's sums of squares go to the first CTA's
 // shared memory, which adds them up, in the same order whatever came first, and
-// hands the coefficient back.  24 tensors of 4.8 MB: 12.3 us (two launches over
-// all SMs 10.3, but 4 to 7 us more of the host's time); 219 of 8435 values 12.
+// hands the coefficient back.  24 tensors of 4.8 MB: 12.2 us (two launches over
+// all SMs 10.3, but 4 to 7 us more of the host's time); 219 of 8435 values 12.  The
+// limit of 6 MB lies above that one comparison; many unaligned pieces are slow here
+// (317 packed tensors of 5 MB clipped 43 us).
 constexpr int kSmallCtas = 16, kSmallThreads = 512, kSmallWarps = kSmallCtas * kSmallThreads / 32;
 constexpr int64_t kSmallPacks = 6 << 16;  // 6 MB
 

@@ -307,7 +307,7 @@ __device__ __forceinline__ uint32_t active_rows(const PolicyJob& j, int64_t firs
 // read, the gradient) leaves L2 first: 716 -> 587 us at 6144 x 131072 bf16.
 // kThreads consumers take kPacks packs of a chunk each; kPerSm CTAs an SM.
 // 6144 x 131072 bf16 with gradients: 587 us, 5.5 TB/s in and out (82 % of the
-// copy rate; 71 % of the issue slots); 4095 x 50001 f32 without: 120 us (6.8 TB/s).
+// copy rate; 72 % of the issue slots); 4095 x 50001 f32 without: 122 us (6.7 TB/s).
 constexpr int kMaxSlots = 6, kRingBytes = 192 * 1024;  // of an SM's CTAs
 
 template <typename T, int kThreads, int kPacks, int kPerSm, bool kGrad>
@@ -763,7 +763,8 @@ cudaError_t launch_rows(const PolicyJob& j, cudaStream_t stream) {
   // As many CTAs an SM as leave their rows in L2 (129 MB) until the second read, a row each, with four 76 MB
   // in all, with two 84 (us with 4 / 2 / 1 an SM: 4096 x 32768 bf16, 40 MB with 4, 100 / 117 / 167; 4096 x
   // 65536, 80 MB, 209 / 197; 2048 x 50001 f32, 122 MB, 179 / 153 / 163; 6144 x 131072 bf16, 159 MB, 735 / 587 /
-  // 642; 2048 x 131072 f32, 319 MB, 491 / 489 / 389).  Without a second read always four.
+  // 642; 2048 x 131072 f32, 319 MB, 491 / 489 / 389).  With two an SM that is 80 MB as the last gain and 159 as
+  // the first loss: nothing between was measured, and 84 is the cautious end.  Without a second read always four.
   const double rows = double(j.V) * sizeof(T) * sm_count();  // bytes of a row on every SM
   if (!kGrad || rows * 4 <= 76e6) return launch_ring<T, 256, 4, 4, kGrad>(j, stream);
   if (rows * 2 <= 84e6) return launch_ring<T, 512, 2, 2, kGrad>(j, stream);
