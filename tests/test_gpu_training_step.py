@@ -1,7 +1,9 @@
 """The example's training step: its gradients against the same step in plain
 64-bit operations, and a run of it with its report."""
+import math
 import os
 import sys
+import threading
 
 import pytest
 import torch
@@ -77,3 +79,95 @@ def test_run_and_report(example):
     d = r["d"]
     assert d.shape == (12, 4, len(example.STAGES)) and bool((d >= 0).all())
     assert torch.equal(r["windows"].X.sum(1), r["windows"].D)  # increments add up to the makespan
+
+
+def step_operators(sf, N, V, T, E, seed):
+    """A call of every operator on inputs of its own and outputs that are kept: (call, refill, outputs)."""
+    dev = torch.device("cuda", torch.cuda.current_device())
+    f = lambda *s: torch.empty(s, device=dev)  # noqa: E731
+    z, old, ref, A = f(N, V), f(N), f(N), f(N)
+    router, dw = f(T, E), f(T, 4)
+    target = torch.zeros(N, dtype=torch.int64, device=dev)
+    grads = [f(5001), f(70).bfloat16(), f(12345)]
+
+    def refill(k):
+        g = torch.Generator(device=dev).manual_seed(seed * 100 + k)
+        for t in (z, old, ref, A, router, dw, *grads):
+            t.normal_(generator=g)
+        target.random_(0, V, generator=g)
+        old.sub_(math.log(V))
+        ref.sub_(math.log(V))
+
+    d, logp, loss, stats = torch.empty_like(z), f(N), f(N), f(4)
+    index, weight = torch.empty((T, 4), dtype=torch.int32, device=dev), f(T, 4)
+    load, droute = torch.empty(E, dtype=torch.int32, device=dev), torch.empty_like(router)
+    norm, coef, each, out = f(1), f(1), f(3), [torch.empty_like(t) for t in grads]
+    status = sf.new_status(dev)
+    ws = torch.empty(sf.lib().sf_policy_loss_workspace_size(N, V), dtype=torch.uint8, device=dev)
+
+    def call():
+        sf.sf_policy_loss(z, target, old, A, ref_logp=ref, kl_coef=0.1, logp=logp, token_loss=loss, stats=stats,
+                          dlogits=d, workspace=ws, status=status)
+        sf.sf_route_experts(router, 4, score="sigmoid", index=index, weight=weight, load=load, status=status)
+        sf.sf_route_experts_grad(router, index, dw, score="sigmoid", dlogits=droute, status=status)
+        sf.sf_grad_clip(grads, 1.0, out=out, norm=norm, coef=coef, tensor_norm=each, status=status)
+
+    return call, refill, [d, logp, loss, stats, index, weight, load, droute, norm, coef, each, *out, status]
+
+
+SHAPES = [(1, 4099, 3, 64), (3, 40000, 100, 64), (700, 1001, 5000, 160), (20000, 33, 700, 8)]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_operators_in_a_graph(example, shape):
+    """Captured once and replayed on new inputs: the bits of calls outside a graph."""
+    call, refill, outputs = step_operators(example.sf, *shape, 1)
+    refill(0)
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for k in (1, 2):
+        refill(k)
+        call()
+        want = [t.clone() for t in outputs]
+        for t in outputs[:-1]:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(outputs[-1].item()) == 0
+        for a, b in zip(outputs, want):
+            assert torch.equal(a, b)
+
+
+def test_operators_from_several_threads(example):
+    """Threads with streams and buffers of their own, at once: the bits of the same calls one after another."""
+    work = [step_operators(example.sf, *shape, 2 + i) for i, shape in enumerate(SHAPES)]
+    wants = []
+    for call, refill, outputs in work:
+        refill(0)
+        call()
+        wants.append([t.clone() for t in outputs])
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(i):
+        call, _, outputs = work[i]
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    for t in outputs[:-1]:
+                        t.zero_()
+                    call()
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(outputs, wants[i])):
+                        wrong.append(i)
+        except Exception as e:  # shown by the assertion
+            wrong.append(e)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(len(work))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and all(int(o[-1].item()) == 0 for _, _, o in work)
