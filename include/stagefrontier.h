@@ -607,6 +607,129 @@ size_t sf_grad_workspace_size(int64_t n);
    workspace, and on bad arguments. */
 int32_t sf_grad_needs_workspace(const int64_t* numel, const int32_t* dtype, int64_t n);
 
+/*
+ * The operators around a policy's layers: what its tokens pass between the
+ * router and the loss (the gated feed-forward product, dropout on the residual
+ * stream), and where the tokens that sf_policy_loss scores come from (drafted
+ * tokens verified against the policy).  The conventions of the training-step
+ * operators hold.
+ */
+#define SF_ACT_SILU 0      /* g / (1 + exp(-g)) */
+#define SF_ACT_GELU 1      /* g (1 + erf(g / sqrt 2)) / 2 */
+#define SF_ACT_GELU_TANH 2 /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+#define SF_ACT_RELU 3      /* max(g, 0), slope 0 at 0 */
+
+/*
+ * sf_gated_ffn - the gated feed-forward product: both projections, the
+ * activation and the product in one pass,
+ *   h = act(x Wg^T) * (x Wu^T)
+ *   x       [T] rows of H, ldx elements apart, of type dtype
+ *   w_gate, w_up [F] rows of H, ldw elements apart, of type dtype
+ *   h       [T] rows of F, ldh elements apart, of type dtype; must not overlap an input
+ *   workspace device, 16-byte aligned, sf_gated_ffn_workspace_size(...) bytes;
+ *             may be null where that is 0
+ * Products are summed in f32 and h is rounded once.  bf16 and f16 go by the
+ * tensor cores; rows of x or weights that do not all start on 16 bytes are
+ * copied to the workspace first.  NaN and infinities go where the formula takes
+ * them.  T, H, F < 2^31, and T H, T F, F H < 2^40.
+ */
+sf_status sf_gated_ffn(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t ldx, const void* w_gate,
+                       const void* w_up, int64_t F, int64_t ldw, int32_t act, void* h, int64_t ldh, void* workspace,
+                       size_t workspace_bytes, uint32_t* status, cudaStream_t stream);
+
+/*
+ * sf_gated_ffn_grad - its gradient from dh; both projections are computed
+ * again, so that nothing of the size of h is kept between the passes:
+ *   g = x Wg^T, u = x Wu^T, dg = dh u act'(g), du = dh act(g)
+ *   dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x
+ *   dh      [T] rows of F, lddh elements apart, of type dtype
+ *   dx      [T] rows of H, lddx elements apart, of type dtype (nullable)
+ *   dw_gate, dw_up [F] rows of H, lddw elements apart, of type dw_dtype, which is
+ *           dtype or SF_F32 (nullable, both or none)
+ *   h       [T] rows of F, ldh elements apart: the product itself once more, for
+ *           the projection behind it (nullable)
+ *   accumulate 1: the weights' gradients are added to their contents (the
+ *           micro-batches of a step), 0: they overwrite them
+ *   workspace device, 16-byte aligned, sf_gated_ffn_workspace_size(...) bytes
+ * At least one of dx, the weights' gradients and h.  dg and du are rounded once
+ * to dtype between the products, as the tensor cores take them.  Outputs must
+ * not overlap inputs or one another.  Without tokens (T = 0) the weights'
+ * gradients are 0, or stay as they are with accumulate.
+ */
+sf_status sf_gated_ffn_grad(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t ldx, const void* w_gate,
+                            const void* w_up, int64_t F, int64_t ldw, int32_t act, const void* dh, int64_t lddh,
+                            void* dx, int64_t lddx, void* dw_gate, void* dw_up, int32_t dw_dtype, int64_t lddw,
+                            int32_t accumulate, void* h, int64_t ldh, void* workspace, size_t workspace_bytes,
+                            uint32_t* status, cudaStream_t stream);
+
+/* Workspace bytes of sf_gated_ffn (grad = 0) and sf_gated_ffn_grad (grad = 1).
+   aligned: 1 if x, w_gate and w_up start on 16 bytes and ldx, ldw are multiples
+   of 16 bytes.  0 on bad arguments and for T = 0. */
+size_t sf_gated_ffn_workspace_size(int32_t dtype, int64_t T, int64_t H, int64_t F, int32_t aligned, int32_t grad);
+
+/*
+ * sf_dropout - out = residual + m x, m = 0 with probability p, else 1 / (1 - p),
+ * with a mask from counters that is never stored.  Element (n, j) is kept if
+ *   b >= t,  t = floor(65536 p + 1/2),
+ * with b the 16-bit number j mod 8 (low half of each word first) of the four
+ * words that Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC11) gives for the
+ * counter (floor(j / 8), n, offset mod 2^32, floor(offset / 2^32)) under the key
+ * (seed mod 2^32, floor(seed / 2^32)), and is then multiplied by 65536 / (65536 - t).
+ * The gradient of x is this call on out's gradient with the same key and
+ * without residual; the residual's is out's own.
+ *   x        [N] rows of D, ldx elements apart, of type dtype
+ *   key      [2] uint64, device: seed and offset, read when the kernel runs (a
+ *            replayed graph draws anew once the caller has moved the offset)
+ *   residual [N] rows of D, ldr elements apart, of type dtype (nullable)
+ *   out      [N] rows of D, ldo elements apart, of type dtype, rounded once; may
+ *            be x or residual itself (with its spacing), else must not overlap them
+ * A dropped element is not read into the sum: its NaN or infinity does not
+ * matter.  0 <= p <= 1; N, D < 2^31.
+ */
+sf_status sf_dropout(const void* x, int32_t dtype, int64_t N, int64_t D, int64_t ldx, float p, const uint64_t* key,
+                     const void* residual, int64_t ldr, void* out, int64_t ldo, cudaStream_t stream);
+
+#define SF_VERIFY_MAX_DRAFT 64
+
+/*
+ * sf_verify_draft - drafted tokens against the policy's rows, by given random
+ * numbers: what is kept is distributed as the policy's own samples are.  For
+ * sequence b with n drafted tokens y_i, p_i = softmax(tau target_i) and
+ * q_i = softmax(tau draft_i):
+ *   y_i is accepted while  uniform_i q_i(y_i) < p_i(y_i);  k is the first that is not
+ *   next token  the j of largest r_j / noise_j (equal values: the lowest), with
+ *               r = max(p_k - q_k, 0) if k < n (p_k if no r_j is above 0), r = p_n if k = n
+ * where noise holds draws of the exponential distribution of mean 1.  Without
+ * draft (tokens that were looked up) q_i is 1 at y_i.  Greedy (neither uniform
+ * nor noise): y_i is accepted while it is the first of the largest logits, which
+ * is also the next token.  n = 0 samples a token from each row.
+ *   target  [B (L + 1)] rows of V, ldt elements apart, of type dtype: row b (L + 1) + i
+ *           is the policy's before token i of sequence b
+ *   draft   [B L] rows of V, ldq elements apart, of type dtype (nullable)
+ *   token   [B][L] int64;  length [B] int32 (nullable: L each), drafted tokens of each sequence
+ *   uniform [B][L] f32 in [0, 1);  noise [B][V] f32 above 0; both or neither
+ *   out_token [B][L + 1] int64: the accepted tokens, the next one, then -1
+ *   accepted  [B] int32: k
+ *   logp    [B][L + 1] f32 (nullable): log p of the tokens of out_token, 0 behind
+ *           them: the old_logp of sf_policy_loss
+ *   workspace device, 16-byte aligned, sf_verify_draft_workspace_size(B, L, V) bytes
+ * Probabilities are held in 32 bits.  Rows behind a sequence's length are not
+ * read.  A token outside [0, V) is not accepted and the next one is drawn from p
+ * in its place, a length outside [0, L] is taken as the nearest one, both with
+ * SF_ST_INDEX.  Where a row that is needed has a NaN or +inf logit or none above
+ * -inf, or no entry can be drawn (its noise is not above 0), the sequence ends
+ * with next token -1, log-probability 0 and SF_ST_NONFINITE.
+ * B (L + 1) < 2^31, 0 <= L <= SF_VERIFY_MAX_DRAFT, 1 <= V <= 2^24, 0 < tau <= 1e6.
+ */
+sf_status sf_verify_draft(const void* target, int32_t dtype, int64_t B, int64_t L, int64_t V, int64_t ldt,
+                          const void* draft, int64_t ldq, const int64_t* token, const int32_t* length,
+                          const float* uniform, const float* noise, float inv_temperature, int64_t* out_token,
+                          int32_t* accepted, float* logp, void* workspace, size_t workspace_bytes, uint32_t* status,
+                          cudaStream_t stream);
+
+/* Workspace bytes of sf_verify_draft; 0 on bad arguments and for B = 0. */
+size_t sf_verify_draft_workspace_size(int64_t B, int64_t L, int64_t V);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,8 +2,9 @@
 // argument validation, output clearing, workspace carving and launch
 // sequencing.  Every computation happens in the kernels (sf_stream.cu,
 // sf_select.cu, sf_rank.cu, sf_group.cu, sf_ingest.cu; for the training-step
-// operators sf_policy_loss.cu, sf_route.cu, sf_grad_norm.cu); this file
-// performs no arithmetic on the data.
+// operators sf_policy_loss.cu, sf_route.cu, sf_grad_norm.cu; around a policy's
+// layers sf_ffn.cu, sf_dropout.cu, sf_verify.cu); this file performs no
+// arithmetic on the data.
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -658,6 +659,225 @@ sf_status sf_route_experts_grad(const void* logits, int32_t dtype, int64_t T, in
   j.ldd = ldd;
   j.status = status;
   return cuda_status(launch_route_grad(j, stream));
+}
+
+namespace {
+
+// The arguments that both passes of the gated product share.
+sf_status ffn_args_ok(const FfnJob& j) {
+  if (!dtype_ok(j.dtype) || !rows_ok(j.T, j.H, j.ldx) || !rows_ok(j.F, j.H, j.ldw) || j.F < 1 || j.act < SF_ACT_SILU ||
+      j.act > SF_ACT_RELU)
+    return SF_EINVAL;
+  constexpr int64_t kMost = int64_t(1) << 40;
+  if (j.F * j.H >= kMost || j.T * j.H >= kMost || j.T * j.F >= kMost) return SF_EUNSUPPORTED;
+  if ((j.T > 0 && !j.x) || !j.w_gate || !j.w_up) return SF_EINVAL;
+  const size_t size = dtype_size(j.dtype);
+  if (!aligned(j.x, size) || !aligned(j.w_gate, size) || !aligned(j.w_up, size) || !aligned(j.h, size) ||
+      !aligned(j.dh, size) || !aligned(j.dx, size) || !aligned(j.status, 4))
+    return SF_EINVAL_ALIGN;
+  return SF_OK;
+}
+
+bool ffn_inputs_on16(const FfnJob& j) {
+  return ffn_rows_on16(j.x, j.T > 1 ? j.ldx : 0, j.dtype) && ffn_rows_on16(j.w_gate, j.F > 1 ? j.ldw : 0, j.dtype) &&
+         ffn_rows_on16(j.w_up, j.F > 1 ? j.ldw : 0, j.dtype);
+}
+
+// Memory of `rows` rows of `len` elements, `ld` apart.
+struct Rows {
+  const void* p;
+  int64_t rows, len, ld;
+  size_t size;
+};
+// Whether two of them share memory: rows of one spacing and type may interleave.
+bool share(const Rows& a, const Rows& b) {
+  if (!a.p || !b.p || a.rows == 0 || b.rows == 0) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  const uintptr_t xn = size_t((a.rows - 1) * a.ld + a.len) * a.size, yn = size_t((b.rows - 1) * b.ld + b.len) * b.size;
+  if (x + xn <= y || y + yn <= x) return false;
+  if (a.ld * a.size != b.ld * b.size) return true;
+  const uintptr_t step = size_t(a.ld) * a.size, n = size_t(a.len) * a.size, m = size_t(b.len) * b.size;
+  const uintptr_t off = y > x ? (y - x) % step : (step - (x - y) % step) % step;  // of b's rows in a's
+  return off < n || step - off < m;
+}
+
+}  // namespace
+
+size_t sf_gated_ffn_workspace_size(int32_t dtype, int64_t T, int64_t H, int64_t F, int32_t on16, int32_t grad) {
+  if (!dtype_ok(dtype) || !rows_ok(T, H, H) || !rows_ok(F, H, H) || F < 1 || T == 0) return 0;
+  return ffn_workspace(dtype, T, H, F, on16 != 0, grad != 0);
+}
+
+sf_status sf_gated_ffn(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t ldx, const void* w_gate,
+                       const void* w_up, int64_t F, int64_t ldw, int32_t act, void* h, int64_t ldh, void* workspace,
+                       size_t workspace_bytes, uint32_t* status, cudaStream_t stream) {
+  FfnJob j;
+  j.x = x;
+  j.w_gate = w_gate;
+  j.w_up = w_up;
+  j.dtype = dtype;
+  j.act = act;
+  j.T = T;
+  j.H = H;
+  j.F = F;
+  j.ldx = ldx;
+  j.ldw = ldw;
+  j.h = h;
+  j.ldh = ldh;
+  j.status = status;
+  const sf_status st = ffn_args_ok(j);
+  if (st != SF_OK) return st;
+  if (!rows_ok(T, F, ldh) || (T > 0 && !h)) return SF_EINVAL;
+  if (T == 0) return SF_OK;
+  const size_t size = dtype_size(dtype);
+  const Rows out = {h, T, F, ldh, size};
+  if (share(out, {x, T, H, ldx, size}) || share(out, {w_gate, F, H, ldw, size}) || share(out, {w_up, F, H, ldw, size}))
+    return SF_EINVAL;
+  const size_t need = ffn_workspace(dtype, T, H, F, ffn_inputs_on16(j), false);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return SF_EWORKSPACE;
+  if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
+  return cuda_status(launch_ffn(j, false, workspace, stream));
+}
+
+sf_status sf_gated_ffn_grad(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t ldx, const void* w_gate,
+                            const void* w_up, int64_t F, int64_t ldw, int32_t act, const void* dh, int64_t lddh,
+                            void* dx, int64_t lddx, void* dw_gate, void* dw_up, int32_t dw_dtype, int64_t lddw,
+                            int32_t accumulate, void* h, int64_t ldh, void* workspace, size_t workspace_bytes,
+                            uint32_t* status, cudaStream_t stream) {
+  FfnJob j;
+  j.x = x;
+  j.w_gate = w_gate;
+  j.w_up = w_up;
+  j.dtype = dtype;
+  j.act = act;
+  j.T = T;
+  j.H = H;
+  j.F = F;
+  j.ldx = ldx;
+  j.ldw = ldw;
+  j.h = h;
+  j.ldh = ldh;
+  j.dh = dh;
+  j.lddh = lddh;
+  j.dx = dx;
+  j.lddx = lddx;
+  j.dw_gate = dw_gate;
+  j.dw_up = dw_up;
+  j.dw_dtype = dw_dtype;
+  j.lddw = lddw;
+  j.accumulate = accumulate != 0;
+  j.status = status;
+  const sf_status st = ffn_args_ok(j);
+  if (st != SF_OK) return st;
+  if ((accumulate != 0 && accumulate != 1) || !rows_ok(T, F, lddh) || (T > 0 && !dh) || (!dw_gate) != (!dw_up) ||
+      (!dx && !dw_gate && !h))
+    return SF_EINVAL;
+  if ((dx && !rows_ok(T, H, lddx)) || (h && !rows_ok(T, F, ldh))) return SF_EINVAL;
+  if (dw_gate && ((dw_dtype != dtype && dw_dtype != SF_F32) || !rows_ok(F, H, lddw))) return SF_EINVAL;
+  const size_t size = dtype_size(dtype), dw_size = dw_gate ? dtype_size(dw_dtype) : size;
+  if (!aligned(dw_gate, dw_size) || !aligned(dw_up, dw_size)) return SF_EINVAL_ALIGN;
+  const Rows out[4] = {{dx, T, H, lddx, size}, {h, T, F, ldh, size}, {dw_gate, F, H, lddw, dw_size},
+                       {dw_up, F, H, lddw, dw_size}};
+  const Rows in[4] = {{x, T, H, ldx, size}, {w_gate, F, H, ldw, size}, {w_up, F, H, ldw, size}, {dh, T, F, lddh, size}};
+  for (int a = 0; a < 4; ++a) {
+    for (int b = 0; b < 4; ++b)
+      if (share(out[a], in[b]) || (a < b && share(out[a], out[b]))) return SF_EINVAL;
+  }
+  if (T > 0) {
+    const size_t need = ffn_workspace(dtype, T, H, F, ffn_inputs_on16(j), true);
+    if (!workspace || workspace_bytes < need) return SF_EWORKSPACE;
+    if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
+  }
+  return cuda_status(launch_ffn(j, true, workspace, stream));
+}
+
+sf_status sf_dropout(const void* x, int32_t dtype, int64_t N, int64_t D, int64_t ldx, float p, const uint64_t* key,
+                     const void* residual, int64_t ldr, void* out, int64_t ldo, cudaStream_t stream) {
+  if (!dtype_ok(dtype) || !rows_ok(N, D, ldx) || !rows_ok(N, D, ldo) || (residual && !rows_ok(N, D, ldr)) ||
+      !(p >= 0.f && p <= 1.f))
+    return SF_EINVAL;
+  if (N > 0 && (!x || !key || !out)) return SF_EINVAL;
+  const size_t size = dtype_size(dtype);
+  if (!aligned(x, size) || !aligned(residual, size) || !aligned(out, size) || !aligned(key, 8)) return SF_EINVAL_ALIGN;
+  if (N == 0) return SF_OK;
+  const Rows to = {out, N, D, ldo, size};
+  if ((!(out == x && ldo == ldx) && share(to, {x, N, D, ldx, size})) ||
+      (!(out == residual && ldo == ldr) && share(to, {residual, N, D, ldr, size})) || share(to, {key, 1, 2, 2, 8}))
+    return SF_EINVAL;
+  DropoutJob j;
+  j.x = x;
+  j.dtype = dtype;
+  j.N = N;
+  j.D = D;
+  j.ldx = ldx;
+  j.threshold = static_cast<uint32_t>(std::floor(double(p) * 65536.0 + 0.5));
+  // all dropped: nothing is multiplied
+  j.scale = j.threshold < 65536u ? static_cast<float>(65536.0 / (65536u - j.threshold)) : 0.f;
+  j.key = key;
+  j.residual = residual;
+  j.ldr = ldr;
+  j.out = out;
+  j.ldo = ldo;
+  return cuda_status(launch_dropout(j, stream));
+}
+
+namespace {
+bool verify_sizes_ok(int64_t B, int64_t L, int64_t V) {
+  return B >= 0 && L >= 0 && L <= SF_VERIFY_MAX_DRAFT && B < (int64_t(1) << 31) / (L + 1) && V >= 1 &&
+         V <= (int64_t(1) << 24);
+}
+}  // namespace
+
+size_t sf_verify_draft_workspace_size(int64_t B, int64_t L, int64_t V) {
+  return !verify_sizes_ok(B, L, V) || B == 0 ? 0 : verify_workspace(B, L, V);
+}
+
+sf_status sf_verify_draft(const void* target, int32_t dtype, int64_t B, int64_t L, int64_t V, int64_t ldt,
+                          const void* draft, int64_t ldq, const int64_t* token, const int32_t* length,
+                          const float* uniform, const float* noise, float inv_temperature, int64_t* out_token,
+                          int32_t* accepted, float* logp, void* workspace, size_t workspace_bytes, uint32_t* status,
+                          cudaStream_t stream) {
+  if (!dtype_ok(dtype) || !verify_sizes_ok(B, L, V) || !rows_ok(B * (L + 1), V, ldt) ||
+      (draft && !rows_ok(B * L, V, ldq)) || !(inv_temperature > 0.f && inv_temperature <= 1e6f))
+    return SF_EINVAL;
+  if (B == 0) return SF_OK;
+  if (!target || !out_token || !accepted || (L > 0 && !token) || (uniform && !noise) || (L > 0 && noise && !uniform))
+    return SF_EINVAL;
+  const size_t size = dtype_size(dtype);
+  if (!aligned(target, size) || !aligned(draft, size) || !aligned(token, 8) || !aligned(length, 4) ||
+      !aligned(uniform, 4) || !aligned(noise, 4) || !aligned(out_token, 8) || !aligned(accepted, 4) ||
+      !aligned(logp, 4) || !aligned(status, 4))
+    return SF_EINVAL_ALIGN;
+  const Rows out[3] = {{out_token, B, L + 1, L + 1, 8}, {accepted, B, 1, 1, 4}, {logp, B, L + 1, L + 1, 4}};
+  const Rows in[6] = {{target, B * (L + 1), V, ldt, size}, {draft, B * L, V, ldq, size}, {token, B, L, L, 8},
+                      {length, B, 1, 1, 4}, {uniform, B, L, L, 4}, {noise, B, V, V, 4}};
+  for (int a = 0; a < 3; ++a) {
+    for (int b = 0; b < 6; ++b)
+      if (in[b].len > 0 && share(out[a], in[b])) return SF_EINVAL;
+    for (int b = a + 1; b < 3; ++b)
+      if (share(out[a], out[b])) return SF_EINVAL;
+  }
+  if (!workspace || workspace_bytes < verify_workspace(B, L, V)) return SF_EWORKSPACE;
+  if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
+  VerifyJob j;
+  j.target = target;
+  j.dtype = dtype;
+  j.B = B;
+  j.L = L;
+  j.V = V;
+  j.ldt = ldt;
+  j.draft = draft;
+  j.ldq = ldq;
+  j.token = token;
+  j.length = length;
+  j.uniform = uniform;
+  j.noise = noise;
+  j.tau = inv_temperature;
+  j.out_token = out_token;
+  j.accepted = accepted;
+  j.logp = logp;
+  j.status = status;
+  return cuda_status(launch_verify(j, workspace, stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,85 @@
+// sf_ffn_math.cuh - the activations of the gated feed-forward product and
+// their derivatives, in 32 bits.
+#pragma once
+
+#include <type_traits>
+
+#include "sf_float.cuh"
+
+namespace sf {
+
+// Results that are rounded to 16 bits take the hardware's exponential and
+// quotient (some 2^-21 of the value, under a tenth of a bf16 or f16 step).
+// A quotient by a number above 2^126, or by infinity, is 0 there.
+template <bool kFast>
+__device__ __forceinline__ float exp_of(float x) {
+  return kFast ? __expf(x) : expf(x);
+}
+template <bool kFast>
+__device__ __forceinline__ float quotient(float a, float b) {
+  return kFast ? __fdividef(a, b) : a / b;
+}
+
+// act(g) and, in both(), its derivative.
+template <int kAct, bool kFast>
+struct Activation;
+
+template <bool kFast>
+struct Activation<SF_ACT_SILU, kFast> {
+  static __device__ __forceinline__ float part(float g) { return quotient<kFast>(1.f, 1.f + exp_of<kFast>(-g)); }
+  static __device__ __forceinline__ float value(float g) { return g * part(g); }
+  static __device__ __forceinline__ void both(float g, float& a, float& slope) {
+    const float s = part(g);
+    a = g * s;
+    slope = s * (1.f + g * (1.f - s));
+  }
+};
+
+template <bool kFast>
+struct Activation<SF_ACT_GELU, kFast> {
+  // (1 + erf(g / sqrt 2)) / 2 = erfc(-g / sqrt 2) / 2, which does not cancel for negative g
+  static __device__ __forceinline__ float part(float g) { return 0.5f * erfcf(-0.70710678f * g); }
+  static __device__ __forceinline__ float value(float g) { return g * part(g); }
+  static __device__ __forceinline__ void both(float g, float& a, float& slope) {
+    const float c = part(g);
+    a = g * c;
+    slope = c + 0.39894228f * g * exp_of<kFast>(-0.5f * g * g);
+  }
+};
+
+template <bool kFast>
+struct Activation<SF_ACT_GELU_TANH, kFast> {
+  static constexpr float kTwo = 1.59576912f;  // 2 sqrt(2 / pi)
+  // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y))
+  static __device__ __forceinline__ float part(float g) {
+    return quotient<kFast>(1.f, 1.f + exp_of<kFast>(-kTwo * (g + 0.044715f * g * g * g)));
+  }
+  static __device__ __forceinline__ float value(float g) { return g * part(g); }
+  static __device__ __forceinline__ void both(float g, float& a, float& slope) {
+    const float s = part(g), bend = s * (1.f - s);
+    a = g * s;
+    slope = bend == 0.f ? s : s + g * bend * kTwo * (1.f + 0.134145f * g * g);  // g^2 may be infinite where bend is 0
+  }
+};
+
+template <bool kFast>
+struct Activation<SF_ACT_RELU, kFast> {
+  static __device__ __forceinline__ float value(float g) { return g < 0.f ? 0.f : g; }  // NaN stays
+  static __device__ __forceinline__ void both(float g, float& a, float& slope) {
+    a = value(g);
+    slope = g > 0.f ? 1.f : 0.f;
+  }
+};
+
+// Calls f with the activation's number as a constant.
+template <typename F>
+auto with_activation(int32_t act, F&& f) {
+  switch (act) {
+    case SF_ACT_GELU: return f(std::integral_constant<int, SF_ACT_GELU>());
+    case SF_ACT_GELU_TANH: return f(std::integral_constant<int, SF_ACT_GELU_TANH>());
+    case SF_ACT_RELU: return f(std::integral_constant<int, SF_ACT_RELU>());
+    default: return f(std::integral_constant<int, SF_ACT_SILU>());
+  }
+}
+
+}  // namespace sf

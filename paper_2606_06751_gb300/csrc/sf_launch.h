@@ -184,4 +184,69 @@ struct RouteGradJob {
 };
 cudaError_t launch_route_grad(const RouteGradJob& job, cudaStream_t stream);
 
+// ---- the operators around a policy's layers
+
+// What every kernel of the gated feed-forward product is given; `h` is the
+// forward pass's result or the gradient's second look at it.
+struct FfnJob {
+  const void *x, *w_gate, *w_up;
+  int32_t dtype, act;
+  int64_t T, H, F, ldx, ldw;
+  void* h = nullptr;
+  int64_t ldh = 0;
+  // the gradient
+  const void* dh = nullptr;
+  int64_t lddh = 0;
+  void* dx = nullptr;
+  int64_t lddx = 0;
+  void *dw_gate = nullptr, *dw_up = nullptr;
+  int32_t dw_dtype = 0;
+  int64_t lddw = 0;
+  bool accumulate = false;
+  // [T] rows of `ldg` in the workspace, of type dtype: the gradients of both projections
+  void *dg = nullptr, *du = nullptr;
+  int64_t ldg = 0;
+  uint32_t* status = nullptr;
+};
+// Rows that start on 16 bytes, as bulk tensor copies want them.
+bool ffn_rows_on16(const void* p, int64_t ld, int32_t dtype);
+size_t ffn_workspace(int32_t dtype, int64_t T, int64_t H, int64_t F, bool aligned, bool grad);
+cudaError_t launch_ffn(FfnJob job, bool grad, void* workspace, cudaStream_t stream);
+
+struct DropoutJob {
+  const void* x;
+  int32_t dtype;
+  int64_t N, D, ldx;
+  uint32_t threshold;  // of 65536
+  float scale;
+  const uint64_t* key;
+  const void* residual;
+  int64_t ldr;
+  void* out;
+  int64_t ldo;
+};
+cudaError_t launch_dropout(const DropoutJob& job, cudaStream_t stream);
+
+struct VerifyPiece;
+struct VerifyJob {
+  const void* target;
+  int32_t dtype;
+  int64_t B, L, V, ldt;
+  const void* draft;
+  int64_t ldq;
+  const int64_t* token;
+  const int32_t* length;
+  const float *uniform, *noise;
+  float tau;
+  int64_t* out_token;
+  int32_t* accepted;
+  float* logp;
+  uint32_t* status;
+  // set by launch_verify
+  VerifyPiece* pieces = nullptr;  // [rows][per_row]
+  int piece = 0, per_row = 0;     // logits of a piece, pieces of a row
+};
+size_t verify_workspace(int64_t B, int64_t L, int64_t V);
+cudaError_t launch_verify(VerifyJob job, void* workspace, cudaStream_t stream);
+
 }  // namespace sf

@@ -26,6 +26,8 @@ SF_ST_NONFINITE = 16
 SF_F32, SF_BF16, SF_F16 = 0, 1, 2
 SF_SCORE_SOFTMAX, SF_SCORE_SIGMOID = 0, 1
 SF_POLICY_DIRECT_ROWS = 1024
+SF_ACT_SILU, SF_ACT_GELU, SF_ACT_GELU_TANH, SF_ACT_RELU = 0, 1, 2, 3
+SF_VERIFY_MAX_DRAFT = 64
 SF_STEP_CONFIDENT = 0x80
 LABEL_NAMES = ("frontier_accounting", "direct_exposure", "sync_wait_dependent", "co_critical",
                "role_aware_needed", "telemetry_limited", "raw_only")
@@ -93,6 +95,11 @@ def _load():
         "sf_route_experts_grad": [P, I32, I, I, I, P, P, ctypes.POINTER(RouteConfig), P, I, P, S],
         "sf_grad_norm": [P, P, P, I, P, P, P, ctypes.c_size_t, P, S],
         "sf_grad_clip": [P, P, P, P, I, ctypes.c_float, ctypes.c_float, P, P, P, P, ctypes.c_size_t, P, S],
+        "sf_gated_ffn": [P, I32, I, I, I, P, P, I, I, I32, P, I, P, ctypes.c_size_t, P, S],
+        "sf_gated_ffn_grad": [P, I32, I, I, I, P, P, I, I, I32, P, I, P, I, P, P, I32, I, I32, P, I, P,
+                              ctypes.c_size_t, P, S],
+        "sf_dropout": [P, I32, I, I, I, ctypes.c_float, P, P, I, P, I, S],
+        "sf_verify_draft": [P, I32, I, I, I, I, P, I, P, P, P, P, ctypes.c_float, P, P, P, P, ctypes.c_size_t, P, S],
     }
     for name, argt in sigs.items():
         f = getattr(L, name)
@@ -118,6 +125,10 @@ def _load():
     L.sf_grad_workspace_size.restype = ctypes.c_size_t
     L.sf_policy_loss_workspace_size.argtypes = [I, I]
     L.sf_policy_loss_workspace_size.restype = ctypes.c_size_t
+    L.sf_gated_ffn_workspace_size.argtypes = [I32, I, I, I, I32, I32]
+    L.sf_gated_ffn_workspace_size.restype = ctypes.c_size_t
+    L.sf_verify_draft_workspace_size.argtypes = [I, I, I]
+    L.sf_verify_draft_workspace_size.restype = ctypes.c_size_t
     for name in ("sf_stream_windows_staging_size", "sf_stream_gathered_staging_size"):
         getattr(L, name).argtypes = [I, I, I, I]
         getattr(L, name).restype = ctypes.c_size_t
@@ -819,3 +830,212 @@ def sf_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, per_tensor
     in place, or into the tensors of `out`.  Where the norm is not finite, coef is
     NaN and the gradients stay as they are."""
     return _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, workspace, status, stream)
+
+
+# ---------------------------------------------------------------- the operators around a policy's layers
+
+_ACTS = {"silu": SF_ACT_SILU, "gelu": SF_ACT_GELU, "gelu_tanh": SF_ACT_GELU_TANH, "relu": SF_ACT_RELU}
+
+
+def _here(*tensors):
+    """The tensors given are on the current device, which the launches go to."""
+    d = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != d:
+            raise ValueError("tensors must be on the current CUDA device")
+
+
+def _like_rows(t, shape, dtypes, name: str):
+    """The row stride of an output matrix that has to be of this shape and type."""
+    n, m, ld = _rows(t, name)
+    if (n, m) != shape or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {list(shape)} of {' or '.join(map(str, dtypes))}")
+    return ld
+
+
+def _ffn_inputs(x, w_gate, w_up, act: str):
+    """(T, H, F, ldx, ldw, activation, whether all rows start on 16 bytes)"""
+    T, H, ldx = _rows(x, "x")
+    F, h, ldw = _rows(w_gate, "w_gate")
+    if h != H or w_gate.dtype != x.dtype:
+        raise ValueError("w_gate must be [F][H] of x's type")
+    if _like_rows(w_up, (F, H), (x.dtype,), "w_up") != ldw:
+        raise ValueError("w_gate and w_up must have one row spacing")
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {', '.join(_ACTS)}")
+    size = 4 if x.dtype == torch.float32 else 2
+    even = (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr() | (ldx * size if T > 1 else 0) |
+            (ldw * size if F > 1 else 0)) % 16 == 0
+    return T, H, F, ldx, ldw, _ACTS[act], even
+
+
+def _ffn_workspace(x, T, H, F, even, grad, made):
+    n = _lib.sf_gated_ffn_workspace_size(_DTYPES[x.dtype], T, H, F, 1 if even else 0, grad)
+    if n == 0:
+        return None
+    made.append(torch.empty(n, dtype=torch.uint8, device=x.device))
+    return made[-1]
+
+
+def sf_gated_ffn(x, w_gate, w_up, act: str = "silu", h=None, workspace=None, status=None, stream=None) -> torch.Tensor:
+    """The gated feed-forward product act(x w_gate^T) * (x w_up^T) [T][F] of x [T][H]
+    and weights [F][H], all of one type."""
+    T, H, F, ldx, ldw, number, even = _ffn_inputs(x, w_gate, w_up, act)
+    _here(x, w_gate, w_up, h, workspace, status)
+    made, ldh = [], F
+    if h is None:
+        h = _empty((T, F), x.dtype, x)
+        made.append(h)
+    else:
+        ldh = _like_rows(h, (T, F), (x.dtype,), "h")
+    if workspace is None:
+        workspace = _ffn_workspace(x, T, H, F, even, 0, made)
+    _hold(made, stream)
+    _check(_lib.sf_gated_ffn(_p(x), _DTYPES[x.dtype], T, H, ldx, _p(w_gate), _p(w_up), F, ldw, number, _p(h), ldh,
+                             _p(workspace), 0 if workspace is None else workspace.numel(), _p(status),
+                             _stream(stream)), "sf_gated_ffn")
+    return h
+
+
+@dataclass
+class GatedFfnGrad:
+    dx: Optional[torch.Tensor]
+    dw_gate: Optional[torch.Tensor]
+    dw_up: Optional[torch.Tensor]
+    h: Optional[torch.Tensor]
+
+
+def sf_gated_ffn_grad(x, w_gate, w_up, dh, act: str = "silu", dx=None, dw_gate=None, dw_up=None, h=None,
+                      accumulate: bool = False, want=("dx", "dw"), dw_dtype=None, workspace=None, status=None,
+                      stream=None) -> GatedFfnGrad:
+    """The gradients of sf_gated_ffn's inputs from that of its result, dh [T][F]: of
+    x, and of both weights (of x's type or float32; added to the tensors given with
+    `accumulate`).  With "h" in `want` the product itself once more."""
+    T, H, F, ldx, ldw, number, even = _ffn_inputs(x, w_gate, w_up, act)
+    lddh = _like_rows(dh, (T, F), (x.dtype,), "dh")
+    _here(x, w_gate, w_up, dh, dx, dw_gate, dw_up, h, workspace, status)
+    made = []
+
+    def out(t, name, wanted, shape, dtypes):
+        if t is not None:
+            return t, _like_rows(t, shape, dtypes, name)
+        if not wanted:
+            return None, shape[1]
+        made.append(_empty(shape, dtypes[0], x))
+        return made[-1], shape[1]
+
+    if (dw_gate is None) != (dw_up is None):
+        raise ValueError("dw_gate and dw_up go together")
+    if accumulate and dw_gate is None:
+        raise ValueError("accumulate adds to gradients that the caller gives")
+    types = (x.dtype, torch.float32)
+    if dw_gate is not None:
+        types = (dw_gate.dtype,) if dw_gate.dtype in types else types
+    elif dw_dtype is not None:
+        if dw_dtype not in types:
+            raise ValueError("dw_dtype must be x's type or float32")
+        types = (dw_dtype,)
+    dx, lddx = out(dx, "dx", "dx" in want, (T, H), (x.dtype,))
+    dw_gate, lddw = out(dw_gate, "dw_gate", "dw" in want, (F, H), types)
+    dw_up, other = out(dw_up, "dw_up", "dw" in want, (F, H), types)
+    if other != lddw:
+        raise ValueError("dw_gate and dw_up must have one row spacing")
+    h, ldh = out(h, "h", "h" in want, (T, F), (x.dtype,))
+    if workspace is None:
+        workspace = _ffn_workspace(x, T, H, F, even, 1, made)
+    _hold(made, stream)
+    _check(_lib.sf_gated_ffn_grad(_p(x), _DTYPES[x.dtype], T, H, ldx, _p(w_gate), _p(w_up), F, ldw, number, _p(dh), lddh,
+                                  _p(dx), lddx, _p(dw_gate), _p(dw_up),
+                                  SF_F32 if dw_gate is None else _DTYPES[dw_gate.dtype], lddw, 1 if accumulate else 0,
+                                  _p(h), ldh, _p(workspace), 0 if workspace is None else workspace.numel(), _p(status),
+                                  _stream(stream)), "sf_gated_ffn_grad")
+    return GatedFfnGrad(dx, dw_gate, dw_up, h)
+
+
+def sf_dropout(x, p: float, key, residual=None, out=None, stream=None) -> torch.Tensor:
+    """residual + x [N][D], each value of x kept with probability 1 - p and scaled.
+    The mask comes from `key` (int64 [2] on the device: seed and offset) and is not
+    stored; the same call on the gradient, without residual, is the backward pass.
+    `out` may be x or residual itself."""
+    N, D, ldx = _rows(x, "x")
+    _vec(key, 2, torch.int64, "key")
+    _here(x, key, residual, out)
+    ldr = ldo = D
+    if residual is not None:
+        ldr = _like_rows(residual, (N, D), (x.dtype,), "residual")
+    if out is None:
+        out = _empty((N, D), x.dtype, x)
+        _hold([out], stream)
+    else:
+        ldo = _like_rows(out, (N, D), (x.dtype,), "out")
+    _check(_lib.sf_dropout(_p(x), _DTYPES[x.dtype], N, D, ldx, p, _p(key), _p(residual), ldr, _p(out), ldo,
+                           _stream(stream)), "sf_dropout")
+    return out
+
+
+@dataclass
+class Verified:
+    token: torch.Tensor
+    accepted: torch.Tensor
+    logp: Optional[torch.Tensor]
+
+
+def _row_stack(t, shape, dtype, name: str):
+    """The row stride of a [B][n][V] tensor whose rows are evenly spaced."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or t.dim() != 3:
+        raise TypeError(f"{name} must be a CUDA tensor [B][rows][V] of float32, bfloat16 or float16")
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {list(shape)} of {dtype}")
+    B, n, V = shape
+    if V > 1 and t.stride(2) != 1:
+        raise TypeError(f"{name} must have contiguous rows")
+    if n > 1 and B > 1 and t.stride(0) != n * t.stride(1):
+        raise TypeError(f"{name}'s rows must be evenly spaced")
+    return t.stride(1) if n > 1 else t.stride(0) if B > 1 and n > 0 else V
+
+
+def sf_verify_draft(target, token, draft=None, lengths=None, uniform=None, noise=None, inv_temperature: float = 1.0,
+                    out_token=None, accepted=None, logp=None, want=("logp",), workspace=None, status=None,
+                    stream=None) -> Verified:
+    """Drafted tokens [B][L] against the policy's logits [B][L + 1][V]: the tokens
+    that are kept with the next one, then -1 ([B][L + 1]), how many drafted ones
+    were accepted [B], and the log-probabilities of the tokens (the old_logp of
+    sf_policy_loss).  `draft` [B][L][V] are the logits that the tokens were drawn
+    from (absent: they were looked up), `lengths` [B] the drafted tokens of each
+    sequence, `uniform` [B][L] and `noise` [B][V] (exponential) the random numbers;
+    without them the choice is greedy."""
+    _dev(token, torch.int64, "token")
+    if token.dim() != 2:
+        raise ValueError("token must be [B][L]")
+    B, L = token.shape
+    if not isinstance(target, torch.Tensor) or target.dim() != 3:
+        raise TypeError("target must be a CUDA tensor [B][L + 1][V]")
+    V = target.shape[2]
+    ldt = _row_stack(target, (B, L + 1, V), target.dtype, "target")
+    ldq = V if draft is None else _row_stack(draft, (B, L, V), target.dtype, "draft")
+    _vec(lengths, B, torch.int32, "lengths")
+    _vec(uniform, B * L, torch.float32, "uniform")
+    _vec(noise, B * V, torch.float32, "noise")
+    if (uniform is None) != (noise is None):
+        raise ValueError("uniform and noise go together")
+    _here(target, token, draft, lengths, uniform, noise, out_token, accepted, logp, workspace, status)
+    made = []
+
+    def new(shape, dtype):
+        made.append(torch.empty(shape, dtype=dtype, device=target.device))
+        return made[-1]
+
+    out_token = new((B, L + 1), torch.int64) if out_token is None else _vec(out_token, B * (L + 1), torch.int64,
+                                                                            "out_token")
+    accepted = new(B, torch.int32) if accepted is None else _vec(accepted, B, torch.int32, "accepted")
+    if logp is not None:
+        _vec(logp, B * (L + 1), torch.float32, "logp")
+    elif "logp" in want:
+        logp = new((B, L + 1), torch.float32)
+    if workspace is None:
+        workspace = new(_lib.sf_verify_draft_workspace_size(B, L, V), torch.uint8)
+    _hold(made, stream)
+    _check(_lib.sf_verify_draft(_p(target), _DTYPES[target.dtype], B, L, V, ldt, _p(draft), ldq, _p(token), _p(lengths),
+                                _p(uniform), _p(noise), inv_temperature, _p(out_token), _p(accepted), _p(logp),
+                                _p(workspace), workspace.numel(), _p(status), _stream(stream)), "sf_verify_draft")
+    return Verified(out_token, accepted, logp)
