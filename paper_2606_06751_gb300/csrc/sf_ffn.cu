@@ -1,5 +1,6 @@
 // sf_ffn.cu - the gated feed-forward product h = act(x Wg^T) * (x Wu^T) and its
-// gradient (sf_gated_ffn, sf_gated_ffn_grad), on the f32 units.
+// gradient (sf_gated_ffn, sf_gated_ffn_grad): what the call launches, and f32 on
+// the f32 units (bf16 and f16: sf_ffn_tensor.cu).
 //
 // Four products of one shape, rows x columns summed over k, by tiles of 128 x 128
 // in registers:
@@ -13,12 +14,12 @@
 #include <algorithm>
 
 #include "sf_ffn_math.cuh"
-#include "sf_launch.h"
+#include "sf_ffn_tensor.h"
 
 namespace sf {
 namespace {
 
-constexpr int kThreads = 256, kTile = 128, kDepth = 16, kHalf = kTile / 2;
+constexpr int kThreads = 256, kTile = 128, kDepth = 16, kHalf = kTile / 2, kRun = 128;
 enum Product { kForward, kInner, kDx, kDw };
 
 // Eight values along a row from p, `left` of which exist.
@@ -83,11 +84,13 @@ __global__ void __launch_bounds__(kThreads) ffn_tile_kernel(const FfnJob j) {
     }
   };
 
-  float sum[8][8];
+  // a run of kRun products is summed by itself and then added: the roundings of one long
+  // chain are twice the error of a sum in pieces
+  float sum[8][8], run[8][8];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sum[i][q] = 0.f;
+    for (int q = 0; q < 8; ++q) sum[i][q] = run[i][q] = 0.f;
   fetch(0);
   stage(0);
   __syncthreads();
@@ -105,7 +108,16 @@ __global__ void __launch_bounds__(kThreads) ffn_tile_kernel(const FfnJob j) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int q = 0; q < 8; ++q) sum[i][q] = fmaf(u[i], v[q], sum[i][q]);
+        for (int q = 0; q < 8; ++q) run[i][q] = fmaf(u[i], v[q], run[i][q]);
+    }
+    if ((step & (kRun / kDepth - 1)) == kRun / kDepth - 1 || step + 1 == all) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          sum[i][q] += run[i][q];
+          run[i][q] = 0.f;
+        }
     }
     if (step + 1 < all) stage(s ^ 1);
     __syncthreads();
@@ -187,6 +199,25 @@ cudaError_t launch_type(const FfnJob& j, bool grad, cudaStream_t stream) {
   return e;
 }
 
+// Rows of 16-bit values that start anywhere, copied to rows that start on 16 bytes.
+struct Spread {
+  const unsigned short* from[3];
+  uint4* to[3];
+  int64_t rows[3], ld[3];
+};
+__global__ void __launch_bounds__(kThreads) ffn_spread_kernel(const Spread s, int64_t len, int64_t packs) {
+  const int part = blockIdx.y;
+  const int64_t all = s.rows[part] * packs, step = int64_t(gridDim.x) * kThreads;
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < all; i += step) {
+    const int64_t r = i / packs, c = (i - r * packs) * 8;
+    const unsigned short* p = s.from[part] + r * s.ld[part] + c;
+    uint32_t v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = c + k < len ? p[k] : 0;
+    s.to[part][i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+  }
+}
+
 size_t value_size(int32_t dtype) { return dtype == SF_F32 ? 4 : 2; }
 size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 
@@ -197,9 +228,8 @@ bool ffn_rows_on16(const void* p, int64_t ld, int32_t dtype) {
 }
 
 size_t ffn_workspace(int32_t dtype, int64_t T, int64_t H, int64_t F, bool aligned, bool grad) {
-  (void)H;
-  (void)aligned;
-  return grad ? 2 * size_t(T) * round16(size_t(F) * value_size(dtype)) : 0;
+  const size_t inner = grad ? 2 * size_t(T) * round16(size_t(F) * value_size(dtype)) : 0;
+  return inner + (dtype == SF_F32 || aligned ? 0 : size_t(T + 2 * F) * round16(size_t(H) * 2));
 }
 
 cudaError_t launch_ffn(FfnJob j, bool grad, void* workspace, cudaStream_t stream) {
@@ -212,12 +242,36 @@ cudaError_t launch_ffn(FfnJob j, bool grad, void* workspace, cudaStream_t stream
     return cudaGetLastError();
   }
   const size_t size = value_size(j.dtype), row = round16(size_t(j.F) * size);
-  j.dg = workspace;
-  j.du = grad ? static_cast<char*>(workspace) + size_t(j.T) * row : nullptr;
-  j.ldg = int64_t(row / size);
-  return j.dtype == SF_F32    ? launch_type<float>(j, grad, stream)
-         : j.dtype == SF_BF16 ? launch_type<__nv_bfloat16>(j, grad, stream)
-                              : launch_type<__half>(j, grad, stream);
+  char* at = static_cast<char*>(workspace);
+  if (grad) {
+    j.dg = at;
+    j.du = at + size_t(j.T) * row;
+    j.ldg = int64_t(row / size);
+    at += 2 * size_t(j.T) * row;
+  }
+  if (j.dtype == SF_F32) return launch_type<float>(j, grad, stream);
+  if (!ffn_rows_on16(j.x, j.T > 1 ? j.ldx : 0, j.dtype) || !ffn_rows_on16(j.w_gate, j.F > 1 ? j.ldw : 0, j.dtype) ||
+      !ffn_rows_on16(j.w_up, j.F > 1 ? j.ldw : 0, j.dtype)) {
+    const int64_t packs = int64_t(round16(size_t(j.H) * 2) / 16);
+    Spread s;
+    const void** data[3] = {&j.x, &j.w_gate, &j.w_up};
+    for (int i = 0; i < 3; ++i) {
+      s.from[i] = static_cast<const unsigned short*>(*data[i]);
+      s.to[i] = reinterpret_cast<uint4*>(at);
+      s.rows[i] = i == 0 ? j.T : j.F;
+      s.ld[i] = i == 0 ? j.ldx : j.ldw;
+      *data[i] = at;
+      at += size_t(s.rows[i]) * packs * 16;
+    }
+    const int64_t most = (std::max(j.T, j.F) * packs + kThreads - 1) / kThreads;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(most, int64_t(sm_count()) * 8)), 3);
+    count_launch();
+    ffn_spread_kernel<<<grid, kThreads, 0, stream>>>(s, j.H, packs);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    j.ldx = j.ldw = packs * 8;
+  }
+  return launch_ffn_tensor(j, grad, stream);
 }
 
 }  // namespace sf

@@ -1,0 +1,558 @@
+// sf_ffn_tensor.cu - the products of the gated feed-forward operators on the
+// tensor cores (bf16 and f16).
+//
+// Every product is written as D[m][n] = sum_k A[m][k] B[n][k] with m along the
+// rows of what is stored, so that a warp's 32 lanes (rows of D in tensor memory)
+// store 32 neighbouring values, whatever the alignment of the output:
+//   forward, inner  m: 64 features of Wg and the same 64 of Wu, n: tokens, k: H
+//   dx              m: H, n: tokens, k: features of dg with Wg, then of du with Wu
+//   dW              m: H, n: features of dg, then of du, k: tokens
+// Weights under dx and both operands of dW lie with m or n along their rows; the
+// tensor cores take them as they are.
+#include <algorithm>
+
+#include "sf_ffn_math.cuh"
+#include "sf_ffn_tensor.h"
+#include "sf_tcgen05.cuh"
+
+namespace sf {
+namespace {
+
+enum Product { kForward, kInner, kDx, kDw };
+
+constexpr uint32_t kABytes = 128 * kDepthBytes;
+constexpr int kMaxStages = 12;
+
+struct Shape {
+  int64_t m_tiles, n_tiles;  // dW: n tiles of one of the two matrices
+  int N;                     // columns of D
+  int stages;
+  int blocks, half;          // blocks of 64 k; dx: those of the first half
+  uint32_t columns;          // of tensor memory
+};
+
+struct Maps {
+  CUtensorMap a0, a1, b0, b1;
+};
+
+template <int kProduct>
+struct Layout {
+  static constexpr bool kGated = kProduct == kForward || kProduct == kInner;
+  static constexpr bool kAAlongK = kGated, kBAlongK = kProduct != kDw;
+  static constexpr int kRows = kGated ? 64 : 128;  // of what is stored, in a CTA's 128 rows of D
+};
+
+// Copies block `kb` of the operands of a CTA's tile; `rows` is the tile's first m, `from` the first n it loads.
+template <int kProduct, int kCtas>
+__device__ __forceinline__ void copy_block(const Maps& maps, const Shape& s, int kb, int m, int n, int n_rows,
+                                           bool second, uint32_t a, uint32_t b, uint32_t bar) {
+  if constexpr (Layout<kProduct>::kGated) {
+    const int k = kb * kBox;
+    tensor_copy<kCtas>(a, &maps.a0, k, m, bar);
+    tensor_copy<kCtas>(a + kBoxBytes, &maps.a1, k, m, bar);
+    tensor_copy<kCtas>(b, &maps.b0, k, n, bar);
+  } else if constexpr (kProduct == kDx) {
+    const bool up = kb >= s.half;
+    const int k = (up ? kb - s.half : kb) * kBox;
+    const CUtensorMap* w = up ? &maps.a1 : &maps.a0;
+    tensor_copy<kCtas>(a, w, m, k, bar);
+    tensor_copy<kCtas>(a + kBoxBytes, w, m + kBox, k, bar);
+    tensor_copy<kCtas>(b, up ? &maps.b1 : &maps.b0, k, n, bar);
+  } else {
+    const int k = kb * kBox;
+    tensor_copy<kCtas>(a, &maps.a0, m, k, bar);
+    tensor_copy<kCtas>(a + kBoxBytes, &maps.a0, m + kBox, k, bar);
+    for (int i = 0; i < n_rows; i += kBox)
+      tensor_copy<kCtas>(b + uint32_t(i / kBox) * kBoxBytes, second ? &maps.b1 : &maps.b0, n + i, k, bar);
+  }
+}
+
+// The products of one block of 64 k.
+template <int kProduct, int kCtas>
+__device__ __forceinline__ void multiply_block(uint32_t d, uint32_t a, uint32_t b, uint32_t desc, bool first) {
+  using L = Layout<kProduct>;
+#pragma unroll
+  for (int k = 0; k < kBox / 16; ++k)
+    tensor_product<kCtas>(d, operand_of<L::kAAlongK>(a + k * kStepBytes<L::kAAlongK>),
+                          operand_of<L::kBAlongK>(b + k * kStepBytes<L::kBAlongK>), desc, !(first && k == 0));
+}
+
+// One value of h, or of dg and du (and h), from its g and u.
+template <typename T, int kProduct, int kAct>
+__device__ __forceinline__ void store_act(const FfnJob& j, int64_t t, int64_t f, float g, float u, float dh) {
+  using A = Activation<kAct, true>;
+  if constexpr (kProduct == kForward) {
+    static_cast<T*>(j.h)[t * j.ldh + f] = from_f32<T>(A::value(g) * u);
+  } else {
+    float a, slope;
+    A::both(g, a, slope);
+    if (j.h != nullptr) static_cast<T*>(j.h)[t * j.ldh + f] = from_f32<T>(a * u);
+    static_cast<T*>(j.dg)[t * j.ldg + f] = from_f32<T>(dh * u * slope);
+    static_cast<T*>(j.du)[t * j.ldg + f] = from_f32<T>(dh * a);
+  }
+}
+template <typename T, int kProduct>
+__device__ __forceinline__ void store_gated(const FfnJob& j, int64_t t, int64_t f, float g, float u, float dh) {
+  switch (j.act) {
+    case SF_ACT_GELU: return store_act<T, kProduct, SF_ACT_GELU>(j, t, f, g, u, dh);
+    case SF_ACT_GELU_TANH: return store_act<T, kProduct, SF_ACT_GELU_TANH>(j, t, f, g, u, dh);
+    case SF_ACT_RELU: return store_act<T, kProduct, SF_ACT_RELU>(j, t, f, g, u, dh);
+    default: return store_act<T, kProduct, SF_ACT_SILU>(j, t, f, g, u, dh);
+  }
+}
+
+// One value of dx or of a weight's gradient.
+template <typename T, int kProduct>
+__device__ __forceinline__ void store_plain(const FfnJob& j, bool second, int64_t m, int64_t n, float v) {
+  if constexpr (kProduct == kDx) {
+    static_cast<T*>(j.dx)[n * j.lddx + m] = from_f32<T>(v);
+  } else {
+    void* w = second ? j.dw_up : j.dw_gate;
+    if (j.dw_dtype == SF_F32) {
+      float* p = static_cast<float*>(w) + n * j.lddw + m;
+      *p = j.accumulate ? *p + v : v;
+    } else {
+      T* p = static_cast<T*>(w) + n * j.lddw + m;
+      *p = from_f32<T>(j.accumulate ? to_f32(*p) + v : v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- large products: a pair of SMs a tile
+
+constexpr int kPairThreads = 384, kStoreWarps = 8;
+constexpr int kSwapBytes = 2 * 2 * 4 * 8 * 32 * 4;  // groups, parities, quadrants, columns, lanes
+
+// Persistent pairs of CTAs: each pair multiplies 256 rows by N columns, the sums of
+// one tile being stored while the next is multiplied.  Warp 0 copies, warp 1 of the
+// pair's first CTA multiplies, warps 4 to 11 store.
+template <typename T, int kProduct>
+__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
+    ffn_pair_kernel(const __grid_constant__ Maps maps, const FfnJob j, const Shape s) {
+  using L = Layout<kProduct>;
+  extern __shared__ unsigned char raw[];
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], sums_full[2], sums_empty[2];
+  __shared__ uint32_t tensor_at;
+  __shared__ int abort;
+  unsigned char* base = align_1024(raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t rank = cluster_rank();
+  const int half_n = s.N / 2;
+  const uint32_t stage_bytes = kABytes + uint32_t(half_n) * kDepthBytes;
+  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
+  const int64_t pairs = gridDim.x / 2;
+
+  if (tid == 0) {
+    abort = 0;
+    for (int i = 0; i < s.stages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sums_full[i], 1);
+      mbar_init(&sums_empty[i], 2 * kStoreWarps);
+    }
+    fence_barrier_init();
+  }
+  if (warp == 2) tensor_alloc<2>(&tensor_at, 512);
+  tensor_fence_before();
+  cluster_sync();
+  tensor_fence_after();
+  const uint32_t sums = tensor_at;
+
+  // a tile's first m and n of the pair; n tiles in groups of 8 m tiles, whose operands stay in L2
+  const auto tile_of = [&](int64_t tile, int64_t& m, int64_t& n, bool& second) {
+    const int64_t all = s.n_tiles * (kProduct == kDw ? 2 : 1);
+    const int64_t group = tile / (8 * all), first = group * 8;
+    const int64_t in_group = s.m_tiles - first < 8 ? s.m_tiles - first : 8;
+    const int64_t at = tile - group * 8 * all;
+    m = (first + at % in_group) * (2 * L::kRows);
+    n = at / in_group;
+    second = kProduct == kDw && n >= s.n_tiles;
+    if (second) n -= s.n_tiles;
+    n *= s.N;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      prefetch_tensormap(&maps.a0);
+      prefetch_tensormap(&maps.a1);
+      prefetch_tensormap(&maps.b0);
+      prefetch_tensormap(&maps.b1);
+      int stage = 0;
+      uint32_t parity = 1;
+      bool ok = true;
+      for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += pairs) {
+        int64_t m, n;
+        bool second;
+        tile_of(tile, m, n, second);
+        for (int kb = 0; kb < s.blocks; ++kb) {
+          ok = mbar_wait_bounded(&empty[stage], parity, &abort);
+          if (!ok) break;
+          const uint32_t a = smem_u32(base) + stage * stage_bytes;
+          if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * stage_bytes);
+          copy_block<kProduct, 2>(maps, s, kb, static_cast<int>(m + rank * L::kRows), static_cast<int>(n + rank * half_n),
+                                  half_n, second, a, a + kABytes, at_rank(&full[stage], 0));
+          if (++stage == s.stages) {
+            stage = 0;
+            parity ^= 1;
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (rank == 0 && lane == 0) {
+      const uint32_t desc = product_of(j.dtype == SF_BF16, L::kAAlongK, L::kBAlongK, 256, s.N);
+      int stage = 0;
+      uint32_t parity = 0;
+      int64_t done = 0;
+      bool ok = true;
+      for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += pairs, ++done) {
+        const int buf = static_cast<int>(done & 1);
+        ok = mbar_wait_bounded(&sums_empty[buf], uint32_t(done >> 1 & 1) ^ 1u, &abort);
+        if (!ok) break;
+        tensor_fence_after();
+        for (int kb = 0; kb < s.blocks; ++kb) {
+          ok = mbar_wait_bounded(&full[stage], parity, &abort);
+          if (!ok) break;
+          tensor_fence_after();
+          const uint32_t a = smem_u32(base) + stage * stage_bytes;
+          multiply_block<kProduct, 2>(sums + buf * 256, a, a + kABytes, desc, kb == 0);
+          products_arrive<2>(&empty[stage]);
+          if (++stage == s.stages) {
+            stage = 0;
+            parity ^= 1;
+          }
+        }
+        if (ok) products_arrive<2>(&sums_full[buf]);
+      }
+    }
+  } else if (warp >= 4) {
+    // two groups of four warps take chunks of 16 columns in turn; a warp reads the 32 lanes of its quadrant
+    const int q = warp & 3, group = (warp - 4) >> 2;
+    float* swap = reinterpret_cast<float*>(base + s.stages * stage_bytes) + group * (2 * 4 * 8 * 32);
+    int64_t done = 0;
+    int turn = 0;
+    for (int64_t tile = blockIdx.x / 2; tile < tiles; tile += pairs, ++done) {
+      int64_t m, n;
+      bool second;
+      tile_of(tile, m, n, second);
+      m += rank * L::kRows;
+      const int buf = static_cast<int>(done & 1);
+      const bool ok = mbar_wait_bounded(&sums_full[buf], uint32_t(done >> 1 & 1), &abort);  // else garbage, and a status
+      tensor_fence_after();
+      const uint32_t at = sums + buf * 256 + (uint32_t(q) << 21);
+      for (int c = 16 * group; c < s.N; c += 32) {
+        uint32_t v[16];
+        if constexpr (L::kGated) {
+          // quadrants 0 and 1 hold g, 2 and 3 u of the same features: each keeps half of the columns
+          // and gets the other factor for them
+          const int mine = q < 2 ? 0 : 8;
+          const int64_t f = m + 32 * (q & 1) + lane, t0 = n + c + mine;
+          float dh[8];
+          if constexpr (kProduct == kInner) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              dh[i] = f < j.F && t0 + i < j.T ? to_f32(static_cast<const T*>(j.dh)[(t0 + i) * j.lddh + f]) : 0.f;
+          }
+          tensor_load16(at + c, v);
+          tensor_loaded();
+          float* out = swap + (turn * 4 + q) * 8 * 32 + lane;
+          const float* in = swap + (turn * 4 + (q ^ 2)) * 8 * 32 + lane;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) out[32 * i] = __uint_as_float(q < 2 ? v[8 + i] : v[i]);
+          named_barrier(1 + group * 2 + (q & 1), 64);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float own = __uint_as_float(q < 2 ? v[i] : v[8 + i]), other = in[32 * i];
+            if (f < j.F && t0 + i < j.T)
+              store_gated<T, kProduct>(j, t0 + i, f, q < 2 ? own : other, q < 2 ? other : own, dh[i]);
+          }
+          turn ^= 1;
+        } else {
+          tensor_load16(at + c, v);
+          tensor_loaded();
+          const int64_t row = m + 32 * q + lane, columns = kProduct == kDx ? j.T : j.F;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (row < j.H && n + c + i < columns)
+              store_plain<T, kProduct>(j, second, row, n + c + i, __uint_as_float(v[i]));
+        }
+      }
+      tensor_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_at(at_rank(&sums_empty[buf], 0));
+      if (!ok && lane == 0) report(j.status, SF_ST_TIMEOUT);
+    }
+  }
+  __syncwarp();
+  if (*static_cast<volatile int*>(&abort)) {  // let copies and products in flight end
+    if (tid == 0) report(j.status, SF_ST_TIMEOUT);
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 2000000u) {
+    }
+  }
+  cluster_sync();
+  if (warp == 2) tensor_free<2>(sums, 512);
+}
+
+// ---------------------------------------------------------------- small products: a tile a cluster, k split among its CTAs
+
+constexpr int kSplitThreads = 256;
+
+// Each CTA of a cluster sums its share of the blocks for the same 128 rows and N
+// columns; then CTA r adds up, in the CTAs' order, and stores a share of the columns.
+template <typename T, int kProduct>
+__global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_constant__ Maps maps, const FfnJob j,
+                                                                  const Shape s) {
+  using L = Layout<kProduct>;
+  extern __shared__ unsigned char raw[];
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], sums_full;
+  __shared__ uint32_t tensor_at;
+  __shared__ int abort;
+  unsigned char* base = align_1024(raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = static_cast<int>(cluster_rank()), C = static_cast<int>(cluster_size());
+  const uint32_t stage_bytes = kABytes + uint32_t(s.N) * kDepthBytes;
+  const int64_t tile = blockIdx.x / C;
+  const int64_t m = tile % s.m_tiles * L::kRows;
+  int64_t n = tile / s.m_tiles;
+  const bool second = kProduct == kDw && n >= s.n_tiles;
+  if (second) n -= s.n_tiles;
+  n *= s.N;
+  const int first = static_cast<int>(int64_t(s.blocks) * rank / C), last = static_cast<int>(int64_t(s.blocks) * (rank + 1) / C);
+
+  if (tid == 0) {
+    abort = 0;
+    for (int i = 0; i < s.stages; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    mbar_init(&sums_full, 1);
+    fence_barrier_init();
+  }
+  if (warp == 2) tensor_alloc<1>(&tensor_at, s.columns);
+  tensor_fence_before();
+  __syncthreads();
+  tensor_fence_after();
+  const uint32_t sums = tensor_at;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t parity = 1;
+      for (int kb = first; kb < last; ++kb) {
+        if (!mbar_wait_bounded(&empty[stage], parity, &abort)) break;
+        const uint32_t a = smem_u32(base) + stage * stage_bytes;
+        mbar_arrive_expect_tx(&full[stage], stage_bytes);
+        copy_block<kProduct, 1>(maps, s, kb, static_cast<int>(m), static_cast<int>(n), s.N, second, a, a + kABytes,
+                                smem_u32(&full[stage]));
+        if (++stage == s.stages) {
+          stage = 0;
+          parity ^= 1;
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t desc = product_of(j.dtype == SF_BF16, L::kAAlongK, L::kBAlongK, 128, s.N);
+      int stage = 0;
+      uint32_t parity = 0;
+      for (int kb = first; kb < last; ++kb) {
+        if (!mbar_wait_bounded(&full[stage], parity, &abort)) break;
+        tensor_fence_after();
+        const uint32_t a = smem_u32(base) + stage * stage_bytes;
+        multiply_block<kProduct, 1>(sums, a, a + kABytes, desc, kb == first);
+        products_arrive<1>(&empty[stage]);
+        if (++stage == s.stages) {
+          stage = 0;
+          parity ^= 1;
+        }
+      }
+      products_arrive<1>(&sums_full);
+    }
+    __syncwarp();
+  }
+  const bool ok = mbar_wait_bounded(&sums_full, 0, &abort);
+  tensor_fence_after();
+  if (!ok || *static_cast<volatile int*>(&abort)) {  // let copies in flight land
+    if (tid == 0) report(j.status, SF_ST_TIMEOUT);
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 2000000u) {
+    }
+  }
+  cluster_sync();  // the stages of every CTA are free
+
+  // partial sums: [source CTA][column of the share][128 rows] in the CTA that stores them
+  float* partial = reinterpret_cast<float*>(base);
+  const int share = (s.N + C - 1) / C;
+  const int q = warp & 3;
+  for (int c = 16 * (warp >> 2); c < s.N; c += 32) {
+    uint32_t v[16];
+    tensor_load16(sums + (uint32_t(q) << 21) + c, v);
+    tensor_loaded();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int to = (c + i) / share, at = (rank * share + (c + i) - to * share) * 128 + 32 * q + lane;
+      if (last > first) store_at(at_rank(partial + at, to), __uint_as_float(v[i]));
+      else store_at(at_rank(partial + at, to), 0.f);
+    }
+  }
+  tensor_fence_before();
+  cluster_sync();
+  if (warp == 2) tensor_free<1>(sums, s.columns);
+  const int from = rank * share, count = min(share, s.N - from);
+  for (int i = tid; i < count * L::kRows; i += kSplitThreads) {
+    const int r = i & (L::kRows - 1), c = i / L::kRows;
+    float v = 0.f, u = 0.f;
+    for (int k = 0; k < C; ++k) {
+      v += partial[(k * share + c) * 128 + r];
+      if (L::kGated) u += partial[(k * share + c) * 128 + 64 + r];
+    }
+    const int64_t row = m + r, column = n + from + c;
+    if constexpr (L::kGated) {
+      if (row >= j.F || column >= j.T) continue;
+      const float dh = kProduct == kInner ? to_f32(static_cast<const T*>(j.dh)[column * j.lddh + row]) : 0.f;
+      store_gated<T, kProduct>(j, column, row, v, u, dh);
+    } else {
+      if (row < j.H && column < (kProduct == kDx ? j.T : j.F)) store_plain<T, kProduct>(j, second, row, column, v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A matrix of `rows` rows of `len` values, `ld` apart, read in boxes of 64 x `box_rows`, 128-byte swizzle; what lies
+// outside is 0.
+bool make_map(CUtensorMap* map, const void* p, int32_t dtype, int64_t rows, int64_t len, int64_t ld, int box_rows) {
+  const EncodeFn encode = encode_fn();
+  if (encode == nullptr) return false;
+  const cuuint64_t dims[2] = {cuuint64_t(len), cuuint64_t(rows)};
+  const cuuint64_t strides[1] = {rows > 1 ? cuuint64_t(ld) * 2 : cuuint64_t((len * 2 + 15) / 16 * 16)};
+  const cuuint32_t box[2] = {kBox, cuuint32_t(box_rows)}, ones[2] = {1, 1};
+  return encode(map, dtype == SF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                const_cast<void*>(p), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int kProduct>
+bool make_maps(Maps& maps, const FfnJob& j, int n_rows) {
+  if (Layout<kProduct>::kGated) {
+    if (!make_map(&maps.a0, j.w_gate, j.dtype, j.F, j.H, j.ldw, kBox) ||
+        !make_map(&maps.a1, j.w_up, j.dtype, j.F, j.H, j.ldw, kBox) ||
+        !make_map(&maps.b0, j.x, j.dtype, j.T, j.H, j.ldx, n_rows))
+      return false;
+    maps.b1 = maps.b0;
+    return true;
+  }
+  const int rows = kProduct == kDx ? n_rows : kBox;
+  if (!make_map(&maps.b0, j.dg, j.dtype, j.T, j.F, j.ldg, rows) ||
+      !make_map(&maps.b1, j.du, j.dtype, j.T, j.F, j.ldg, rows))
+    return false;
+  if (kProduct == kDw) {
+    if (!make_map(&maps.a0, j.x, j.dtype, j.T, j.H, j.ldx, kBox)) return false;
+    maps.a1 = maps.a0;
+    return true;
+  }
+  return make_map(&maps.a0, j.w_gate, j.dtype, j.F, j.H, j.ldw, kBox) &&
+         make_map(&maps.a1, j.w_up, j.dtype, j.F, j.H, j.ldw, kBox);
+}
+
+constexpr size_t kSmemMost = 227 * 1024, kSmemFixed = 1024 + 1024;  // alignment; barriers
+
+template <typename T, int kProduct>
+cudaError_t launch_pairs(const FfnJob& j, Shape s, cudaStream_t stream) {
+  Maps maps;
+  if (!make_maps<kProduct>(maps, j, s.N / 2)) return cudaErrorUnknown;
+  const size_t stage = kABytes + size_t(s.N / 2) * kDepthBytes, swap = Layout<kProduct>::kGated ? kSwapBytes : 0;
+  s.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemMost - kSmemFixed - swap) / stage));
+  const size_t smem = 1024 + s.stages * stage + swap;
+  const auto kernel = ffn_pair_kernel<T, kProduct>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
+  const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, sm_count() / 2));
+  count_launch();
+  kernel<<<grid, kPairThreads, smem, stream>>>(maps, j, s);
+  return cudaGetLastError();
+}
+
+template <typename T, int kProduct>
+cudaError_t launch_split(const FfnJob& j, Shape s, int C, cudaStream_t stream) {
+  Maps maps;
+  if (!make_maps<kProduct>(maps, j, s.N)) return cudaErrorUnknown;
+  const size_t stage = kABytes + size_t(s.N) * kDepthBytes;
+  s.columns = 32;
+  while (s.columns < uint32_t(s.N)) s.columns *= 2;
+  // the sums of both partners of an SM fit tensor memory: shared memory allows no more CTAs than that
+  const size_t sums = size_t(ceil_div(s.N, C)) * C * 512;
+  const size_t least = std::max<size_t>(sums, kSmemMost * s.columns / 512);
+  const int most = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemMost - kSmemFixed) / stage));
+  s.stages = std::min<int>(most, std::max<int>(4, static_cast<int>(ceil_div(s.blocks, C))));
+  size_t smem = 1024 + std::max(least, s.stages * stage);
+  const auto kernel = ffn_split_kernel<T, kProduct>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
+  if (tiles * C >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles * C));
+  cfg.blockDim = dim3(kSplitThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, kernel, maps, j, s);
+}
+
+template <typename T, int kProduct>
+cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
+  using L = Layout<kProduct>;
+  const int64_t M = L::kGated ? j.F : j.H, Nall = kProduct == kDw ? j.F : j.T, two = kProduct == kDw ? 2 : 1;
+  Shape s = {};
+  const int64_t k = kProduct == kDx ? j.F : kProduct == kDw ? j.T : j.H;
+  s.half = static_cast<int>(ceil_div(k, kBox));
+  s.blocks = kProduct == kDx ? 2 * s.half : s.half;
+  const int granule = kProduct == kDw ? 128 : 32;  // of a pair's N
+  const int64_t n_tiles = ceil_div(Nall, 256);
+  const int64_t pair_tiles = ceil_div(M, 2 * L::kRows) * n_tiles * two;
+  if (pair_tiles >= sm_count() / 2) {
+    s.m_tiles = ceil_div(M, 2 * L::kRows);
+    s.n_tiles = n_tiles;
+    s.N = static_cast<int>(ceil_div(ceil_div(Nall, n_tiles), granule) * granule);
+    return launch_pairs<T, kProduct>(j, s, stream);
+  }
+  s.m_tiles = ceil_div(M, L::kRows);
+  const int fine = kProduct == kDw ? 64 : 16;
+  s.n_tiles = n_tiles;
+  s.N = static_cast<int>(ceil_div(ceil_div(Nall, n_tiles), fine) * fine);
+  const int64_t tiles = s.m_tiles * s.n_tiles * two;
+  int C = 1;
+  while (C < 8 && tiles * C * 2 <= 2 * sm_count() && s.blocks >= C * 4) C *= 2;
+  return launch_split<T, kProduct>(j, s, C, stream);
+}
+
+template <typename T>
+cudaError_t launch_type(const FfnJob& j, bool grad, cudaStream_t stream) {
+  if (!grad) return launch_product<T, kForward>(j, stream);
+  cudaError_t e = launch_product<T, kInner>(j, stream);
+  if (e == cudaSuccess && j.dx != nullptr) e = launch_product<T, kDx>(j, stream);
+  if (e == cudaSuccess && j.dw_gate != nullptr) e = launch_product<T, kDw>(j, stream);
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_ffn_tensor(const FfnJob& j, bool grad, cudaStream_t stream) {
+  return j.dtype == SF_BF16 ? launch_type<__nv_bfloat16>(j, grad, stream) : launch_type<__half>(j, grad, stream);
+}
+
+}  // namespace sf
