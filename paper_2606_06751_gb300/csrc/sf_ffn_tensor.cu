@@ -77,28 +77,60 @@ __device__ __forceinline__ void multiply_block(uint32_t d, uint32_t a, uint32_t 
                           operand_of<L::kBAlongK>(b + k * kStepBytes<L::kBAlongK>), desc, !(first && k == 0));
 }
 
-// One value of h, or of dg and du (and h), from its g and u.
-template <typename T, int kProduct, int kAct>
-__device__ __forceinline__ void store_act(const FfnJob& j, int64_t t, int64_t f, float g, float u, float dh) {
+// K values of h, or of dg and du (and h), from their g and u: feature f of tokens
+// t, t + step, ... before t + most and T.  One basic block, so that the K chains of exponential and quotient overlap.
+template <typename T, int kProduct, int kAct, int K>
+__device__ __forceinline__ void store_act(const FfnJob& j, int64_t t, int step, int64_t f, int most, const float (&g)[K],
+                                          const float (&u)[K], const float (&dh)[K]) {
   using A = Activation<kAct, true>;
-  if constexpr (kProduct == kForward) {
-    static_cast<T*>(j.h)[t * j.ldh + f] = from_f32<T>(A::value(g) * u);
-  } else {
-    float a, slope;
-    A::both(g, a, slope);
-    if (j.h != nullptr) static_cast<T*>(j.h)[t * j.ldh + f] = from_f32<T>(a * u);
-    static_cast<T*>(j.dg)[t * j.ldg + f] = from_f32<T>(dh * u * slope);
-    static_cast<T*>(j.du)[t * j.ldg + f] = from_f32<T>(dh * a);
+  T v[K], w[K], x[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    if constexpr (kProduct == kForward) {
+      v[i] = from_f32<T>(A::value(g[i]) * u[i]);
+    } else {
+      float a, slope;
+      A::both(g[i], a, slope);
+      v[i] = from_f32<T>(a * u[i]);
+      w[i] = from_f32<T>(dh[i] * u[i] * slope);
+      x[i] = from_f32<T>(dh[i] * a);
+    }
+  }
+  const int left = static_cast<int>(min(int64_t(most), j.T - t));
+  if (kProduct == kForward || j.h != nullptr) {
+    T* p = static_cast<T*>(j.h) + t * j.ldh + f;
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (i * step < left) p[i * step * j.ldh] = v[i];
+  }
+  if constexpr (kProduct == kInner) {
+    T *p = static_cast<T*>(j.dg) + t * j.ldg + f, *r = static_cast<T*>(j.du) + t * j.ldg + f;
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (i * step < left) {
+        p[i * step * j.ldg] = w[i];
+        r[i * step * j.ldg] = x[i];
+      }
   }
 }
-template <typename T, int kProduct>
-__device__ __forceinline__ void store_gated(const FfnJob& j, int64_t t, int64_t f, float g, float u, float dh) {
+template <typename T, int kProduct, int K>
+__device__ __forceinline__ void store_gated(const FfnJob& j, int64_t t, int step, int64_t f, int most, const float (&g)[K],
+                                            const float (&u)[K], const float (&dh)[K]) {
+  if (f >= j.F || t >= j.T) return;
   switch (j.act) {
-    case SF_ACT_GELU: return store_act<T, kProduct, SF_ACT_GELU>(j, t, f, g, u, dh);
-    case SF_ACT_GELU_TANH: return store_act<T, kProduct, SF_ACT_GELU_TANH>(j, t, f, g, u, dh);
-    case SF_ACT_RELU: return store_act<T, kProduct, SF_ACT_RELU>(j, t, f, g, u, dh);
-    default: return store_act<T, kProduct, SF_ACT_SILU>(j, t, f, g, u, dh);
+    case SF_ACT_GELU: return store_act<T, kProduct, SF_ACT_GELU>(j, t, step, f, most, g, u, dh);
+    case SF_ACT_GELU_TANH: return store_act<T, kProduct, SF_ACT_GELU_TANH>(j, t, step, f, most, g, u, dh);
+    case SF_ACT_RELU: return store_act<T, kProduct, SF_ACT_RELU>(j, t, step, f, most, g, u, dh);
+    default: return store_act<T, kProduct, SF_ACT_SILU>(j, t, step, f, most, g, u, dh);
   }
+}
+// Their upstream gradients.
+template <typename T, int K>
+__device__ __forceinline__ void load_dh(const FfnJob& j, int64_t t, int step, int64_t f, float (&dh)[K]) {
+  const T* p = static_cast<const T*>(j.dh) + t * j.lddh + f;
+  const int left = f < j.F && t < j.T ? static_cast<int>(min(int64_t(K) * step, j.T - t)) : 0;
+#pragma unroll
+  for (int i = 0; i < K; ++i) dh[i] = i * step < left ? to_f32(p[i * step * j.lddh]) : 0.f;
 }
 
 // One value of dx or of a weight's gradient.
@@ -249,12 +281,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
           // and gets the other factor for them
           const int mine = q < 2 ? 0 : 8;
           const int64_t f = m + 32 * (q & 1) + lane, t0 = n + c + mine;
-          float dh[8];
-          if constexpr (kProduct == kInner) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              dh[i] = f < j.F && t0 + i < j.T ? to_f32(static_cast<const T*>(j.dh)[(t0 + i) * j.lddh + f]) : 0.f;
-          }
+          float g[8], u[8], dh[8];
+          if constexpr (kProduct == kInner) load_dh<T>(j, t0, 1, f, dh);
           tensor_load16(at + c, v);
           tensor_loaded();
           float* out = swap + (turn * 4 + q) * 8 * 32 + lane;
@@ -265,9 +293,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float own = __uint_as_float(q < 2 ? v[i] : v[8 + i]), other = in[32 * i];
-            if (f < j.F && t0 + i < j.T)
-              store_gated<T, kProduct>(j, t0 + i, f, q < 2 ? own : other, q < 2 ? other : own, dh[i]);
+            g[i] = q < 2 ? own : other;
+            u[i] = q < 2 ? other : own;
           }
+          store_gated<T, kProduct>(j, t0, 1, f, 8, g, u, dh);
           turn ^= 1;
         } else {
           tensor_load16(at + c, v);
@@ -403,20 +432,33 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
   cluster_sync();
   if (warp == 2) tensor_free<1>(sums, s.columns);
   const int from = rank * share, count = min(share, s.N - from);
-  for (int i = tid; i < count * L::kRows; i += kSplitThreads) {
-    const int r = i & (L::kRows - 1), c = i / L::kRows;
-    float v = 0.f, u = 0.f;
+  // a thread a row, K columns at a time
+  constexpr int K = 4, kStep = kSplitThreads / L::kRows;
+  const int r = tid & (L::kRows - 1);
+  const int64_t row = m + r;
+  for (int c = tid / L::kRows; c < count; c += K * kStep) {
+    float v[K], u[K], dh[K];
+    if constexpr (kProduct == kInner) load_dh<T>(j, n + from + c, kStep, row, dh);
+#pragma unroll
+    for (int i = 0; i < K; ++i) v[i] = u[i] = 0.f;
     for (int k = 0; k < C; ++k) {
-      v += partial[(k * share + c) * 128 + r];
-      if (L::kGated) u += partial[(k * share + c) * 128 + 64 + r];
+      const float* p = partial + (k * share + c) * 128 + r;
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (c + i * kStep < count) {
+          v[i] += p[i * kStep * 128];
+          if (L::kGated) u[i] += p[i * kStep * 128 + 64];
+        }
     }
-    const int64_t row = m + r, column = n + from + c;
     if constexpr (L::kGated) {
-      if (row >= j.F || column >= j.T) continue;
-      const float dh = kProduct == kInner ? to_f32(static_cast<const T*>(j.dh)[column * j.lddh + row]) : 0.f;
-      store_gated<T, kProduct>(j, column, row, v, u, dh);
+      store_gated<T, kProduct>(j, n + from + c, kStep, row, min(count - c, K * kStep), v, u, dh);
     } else {
-      if (row < j.H && column < (kProduct == kDx ? j.T : j.F)) store_plain<T, kProduct>(j, second, row, column, v);
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const int64_t column = n + from + c + i * kStep;
+        if (c + i * kStep < count && row < j.H && column < (kProduct == kDx ? j.T : j.F))
+          store_plain<T, kProduct>(j, second, row, column, v[i]);
+      }
     }
   }
 }
