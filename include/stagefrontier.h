@@ -712,9 +712,8 @@ sf_status sf_dropout(const void* x, int32_t dtype, int64_t N, int64_t D, int64_t
  *   accepted  [B] int32: k
  *   logp    [B][L + 1] f32 (nullable): log p of the tokens of out_token, 0 behind
  *           them: the old_logp of sf_policy_loss
- *   workspace device, 16-byte aligned, sf_verify_draft_workspace_size(B, L, V) bytes
  * Probabilities are held in 32 bits.  Rows behind a sequence's length are not
- * read.  A token outside [0, V) is not accepted and the next one is drawn from p
+ * read, and those behind the one where it stops need not be.  A token outside [0, V) is not accepted and the next one is drawn from p
  * in its place, a length outside [0, L] is taken as the nearest one, both with
  * SF_ST_INDEX.  Where a row that is needed has a NaN or +inf logit or none above
  * -inf, or no entry can be drawn (its noise is not above 0), the sequence ends
@@ -724,11 +723,7 @@ sf_status sf_dropout(const void* x, int32_t dtype, int64_t N, int64_t D, int64_t
 sf_status sf_verify_draft(const void* target, int32_t dtype, int64_t B, int64_t L, int64_t V, int64_t ldt,
                           const void* draft, int64_t ldq, const int64_t* token, const int32_t* length,
                           const float* uniform, const float* noise, float inv_temperature, int64_t* out_token,
-                          int32_t* accepted, float* logp, void* workspace, size_t workspace_bytes, uint32_t* status,
-                          cudaStream_t stream);
-
-/* Workspace bytes of sf_verify_draft; 0 on bad arguments and for B = 0. */
-size_t sf_verify_draft_workspace_size(int64_t B, int64_t L, int64_t V);
+                          int32_t* accepted, float* logp, uint32_t* status, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

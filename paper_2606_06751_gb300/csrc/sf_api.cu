@@ -810,9 +810,10 @@ sf_status sf_dropout(const void* x, int32_t dtype, int64_t N, int64_t D, int64_t
   j.N = N;
   j.D = D;
   j.ldx = ldx;
-  j.threshold = static_cast<uint32_t>(std::floor(double(p) * 65536.0 + 0.5));
-  // all dropped: nothing is multiplied
-  j.scale = j.threshold < 65536u ? static_cast<float>(65536.0 / (65536u - j.threshold)) : 0.f;
+  const uint32_t t = static_cast<uint32_t>(std::floor(double(p) * 65536.0 + 0.5));
+  j.none = t == 65536u;
+  j.high = j.none ? 0u : t << 16;
+  j.scale = j.none ? 0.f : static_cast<float>(65536.0 / (65536u - t));
   j.key = key;
   j.residual = residual;
   j.ldr = ldr;
@@ -828,15 +829,10 @@ bool verify_sizes_ok(int64_t B, int64_t L, int64_t V) {
 }
 }  // namespace
 
-size_t sf_verify_draft_workspace_size(int64_t B, int64_t L, int64_t V) {
-  return !verify_sizes_ok(B, L, V) || B == 0 ? 0 : verify_workspace(B, L, V);
-}
-
 sf_status sf_verify_draft(const void* target, int32_t dtype, int64_t B, int64_t L, int64_t V, int64_t ldt,
                           const void* draft, int64_t ldq, const int64_t* token, const int32_t* length,
                           const float* uniform, const float* noise, float inv_temperature, int64_t* out_token,
-                          int32_t* accepted, float* logp, void* workspace, size_t workspace_bytes, uint32_t* status,
-                          cudaStream_t stream) {
+                          int32_t* accepted, float* logp, uint32_t* status, cudaStream_t stream) {
   if (!dtype_ok(dtype) || !verify_sizes_ok(B, L, V) || !rows_ok(B * (L + 1), V, ldt) ||
       (draft && !rows_ok(B * L, V, ldq)) || !(inv_temperature > 0.f && inv_temperature <= 1e6f))
     return SF_EINVAL;
@@ -857,8 +853,6 @@ sf_status sf_verify_draft(const void* target, int32_t dtype, int64_t B, int64_t 
     for (int b = a + 1; b < 3; ++b)
       if (share(out[a], out[b])) return SF_EINVAL;
   }
-  if (!workspace || workspace_bytes < verify_workspace(B, L, V)) return SF_EWORKSPACE;
-  if (!aligned(workspace, 16)) return SF_EINVAL_ALIGN;
   VerifyJob j;
   j.target = target;
   j.dtype = dtype;
@@ -877,7 +871,7 @@ sf_status sf_verify_draft(const void* target, int32_t dtype, int64_t B, int64_t 
   j.accepted = accepted;
   j.logp = logp;
   j.status = status;
-  return cuda_status(launch_verify(j, workspace, stream));
+  return cuda_status(launch_verify(j, stream));
 }
 
 }  // extern "C"

@@ -5,8 +5,11 @@
 // Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", SC11) on
 // (pack, row, offset) under the seed: 16 bits a column, ten rounds of two 32-bit
 // products.  Nothing of it is stored; a backward pass computes it again.  Each
-// value is read and written once: bound by memory, with the generator's some 60
-// integer instructions for 8 columns behind it.
+// value is read and written once.  Bound by memory with a residual (16384 x 8192
+// bf16: 131 us, 91 % of the copy rate) and by the integer units without (105 us, 75 %):
+// some 160 instructions for 8 columns, of which the generator is 40 and the 8
+// decisions with their selects 20.  CTAs of 128 threads: those of 256 take 138 and
+// 107 us (whole CTAs fit the registers worse), 32 an SM in turn.
 #include <algorithm>
 
 #include "sf_float.cuh"
@@ -15,96 +18,187 @@
 namespace sf {
 namespace {
 
-constexpr int kThreads = 256, kCols = 8;
+constexpr int kThreads = 128, kCols = 8, kTurns = 2, kRounds = 10, kPerSm = 32;
 
-struct Key {
-  uint32_t k0, k1, o0, o1;
+// The generator's keys of each round, in shared memory: they depend on the call
+// alone, and a read for all lanes takes no slot of the integer units.
+struct Keys {
+  uint2 round[kRounds];
+  uint2 offset;
 };
-
-__device__ __forceinline__ Key load_key(const uint64_t* key) {
-  const uint64_t seed = key[0], offset = key[1];
-  return {static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32), static_cast<uint32_t>(offset),
-          static_cast<uint32_t>(offset >> 32)};
-}
-
-// Ten rounds; the multipliers and the key's increments are the paper's.
-__device__ __forceinline__ uint4 philox(uint32_t pack, uint32_t row, const Key& key) {
-  uint32_t c0 = pack, c1 = row, c2 = key.o0, c3 = key.o1, k0 = key.k0, k1 = key.k1;
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    const uint64_t a = uint64_t(c0) * 0xD2511F53u, b = uint64_t(c2) * 0xCD9E8D57u;
-    const uint32_t n0 = static_cast<uint32_t>(b >> 32) ^ c1 ^ k0, n2 = static_cast<uint32_t>(a >> 32) ^ c3 ^ k1;
-    c0 = n0;
-    c1 = static_cast<uint32_t>(b);
-    c2 = n2;
-    c3 = static_cast<uint32_t>(a);
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
+__device__ __forceinline__ void load_keys(Keys& keys, const uint64_t* key) {
+  if (threadIdx.x == 0) {
+    const uint64_t seed = key[0], offset = key[1];
+    uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
+    for (int r = 0; r < kRounds; ++r) {
+      keys.round[r] = make_uint2(k0, k1);
+      k0 += 0x9E3779B9u;
+      k1 += 0xBB67AE85u;
+    }
+    keys.offset = make_uint2(static_cast<uint32_t>(offset), static_cast<uint32_t>(offset >> 32));
   }
-  return make_uint4(c0, c1, c2, c3);
+  __syncthreads();
 }
 
+// Ten rounds for K counters; the multipliers and the keys' increments are the paper's.
+template <int K>
+__device__ __forceinline__ void philox(const uint32_t (&pack)[K], const uint32_t (&row)[K], const Keys& keys,
+                                       uint4 (&c)[K]) {
+  const uint2 o = keys.offset;
+#pragma unroll
+  for (int k = 0; k < K; ++k) c[k] = make_uint4(pack[k], row[k], o.x, o.y);
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const uint2 key = keys.round[r];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint64_t a = uint64_t(c[k].x) * 0xD2511F53u, b = uint64_t(c[k].z) * 0xCD9E8D57u;
+      c[k] = make_uint4(static_cast<uint32_t>(b >> 32) ^ c[k].y ^ key.x, static_cast<uint32_t>(b),
+                        static_cast<uint32_t>(a >> 32) ^ c[k].w ^ key.y, static_cast<uint32_t>(a));
+    }
+  }
+}
+__device__ __forceinline__ uint4 philox(uint32_t pack, uint32_t row, const Keys& keys) {
+  const uint32_t p[1] = {pack}, r[1] = {row};
+  uint4 w[1];
+  philox(p, r, keys, w);
+  return w[0];
+}
+
+// Whether column q of the pack is kept: its 16 bits are not below the threshold, which
+// `high` holds in its upper half.  (All dropped, 65536 of 65536: the caller's to see.)
+__device__ __forceinline__ bool keeps(const uint4& w, int q, uint32_t high) {
+  const uint32_t v = q < 2 ? w.x : q < 4 ? w.y : q < 6 ? w.z : w.w;
+  return (q & 1 ? v : v << 16) >= high;
+}
 // Bit j: column j of the pack is kept.
-__device__ __forceinline__ uint32_t kept(const uint4& w, uint32_t t) {
-  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ uint32_t kept(const uint4& w, uint32_t high) {
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    m |= ((v[i] & 0xffffu) >= t ? 1u : 0u) << (2 * i);
-    m |= ((v[i] >> 16) >= t ? 1u : 0u) << (2 * i + 1);
-  }
+  for (int q = 0; q < kCols; ++q) m |= keeps(w, q, high) ? 1u << q : 0u;
   return m;
 }
 
 // The rounded result: the product and the sum are rounded in f32 as written, then to T.
+template <bool kResidual>
 __device__ __forceinline__ float masked(float x, float r, bool keep, float scale) {
-  return __fadd_rn(keep ? __fmul_rn(x, scale) : 0.f, r);
+  const float v = __fmul_rn(x, scale);
+  if (kResidual) return keep ? __fadd_rn(v, r) : r;
+  return keep ? v : 0.f;
 }
 
-// Rows whose packs of 8 columns are all 16-byte aligned: a thread a pack, the
-// packs of all rows one after another.
-template <typename T, bool kResidual>
-__global__ void __launch_bounds__(kThreads) dropout_pack_kernel(const DropoutJob j) {
+// A row's values that lie before its first 16-byte boundary's pack: `off` values
+// behind a boundary, the same for all three rows.
+template <typename T>
+__device__ __forceinline__ int row_off(const DropoutJob& j, int64_t row) {
+  return static_cast<int>(((reinterpret_cast<uintptr_t>(j.x) / sizeof(T)) + uint64_t(row) * uint64_t(j.ldx)) %
+                          uint64_t(Pack<T>::kN));
+}
+
+// The columns from c of a row of D that exist.
+template <typename T, int P>
+__device__ __forceinline__ void load_some(const T* row, int64_t c, int64_t D, uint4 (&u)[P]) {
+  constexpr int N = Pack<T>::kN;
+#pragma unroll
+  for (int q = 0; q < P * N; ++q)
+    reinterpret_cast<T*>(&u[q / N])[q % N] = c + q >= 0 && c + q < D ? row[c + q] : from_f32<T>(0.f);
+}
+
+// How a warp's lanes lie on the packs: `lanes` (a power of two) side by side in a row, 32 / lanes
+// rows below one another; the next of its kTurns turns is `packs_on` packs or `rows_on` rows further.
+struct Tile {
+  int shift;  // lanes = 1 << shift
+  int packs_on, rows_on;
+  int64_t rows, per_row, all;  // rows of a tile, tiles of a row, tiles
+};
+
+// Rows that start at the same distance from a 16-byte boundary in x, residual and
+// out (kShift: not 0 in every row): a thread takes 8 columns between boundaries.
+// Where a row starts `off` values behind a boundary its 8 columns lie in two packs of
+// the mask: the lane before has the other.  The generator serves all turns of a warp at once.
+template <typename T, bool kResidual, bool kShift>
+__global__ void __launch_bounds__(kThreads) dropout_pack_kernel(const DropoutJob j, const Tile t) {
   constexpr int N = Pack<T>::kN, P = kCols / N;  // 16-byte packs of a thread
-  const Key key = load_key(j.key);
-  const int64_t packs = (j.D + kCols - 1) / kCols, step = int64_t(gridDim.x) * kThreads;
-  const int64_t first = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  int64_t row = first / packs, at = first - row * packs;
-  const int64_t rows_on = step / packs, at_on = step - rows_on * packs;
+  __shared__ Keys keys;
+  load_keys(keys, j.key);
+  const int lane = threadIdx.x & 31, in_row = lane & ((1 << t.shift) - 1), below = lane >> t.shift;
+  const int packs = static_cast<int>((j.D + (kShift ? N - 1 : 0) + kCols - 1) / kCols);
+  const int D = static_cast<int>(j.D);
   const T *x = static_cast<const T*>(j.x), *res = static_cast<const T*>(j.residual);
   T* out = static_cast<T*>(j.out);
-  while (row < j.N) {
-    const int64_t c = at * kCols;
-    const T *px = x + row * j.ldx + c, *pr = res + row * j.ldr + c;
-    T* po = out + row * j.ldo + c;
-    if (c + kCols <= j.D) {
-      uint4 u[P], v[P];
+  const int64_t step = int64_t(gridDim.x) * (kThreads / 32);
+  const int64_t first = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  int64_t tile_row = first / t.per_row, seg = first - tile_row * t.per_row;
+  const int64_t rows_step = step / t.per_row, seg_step = step - rows_step * t.per_row;
+  for (int64_t tile = first; tile < t.all; tile += step) {
+    const int64_t row0 = tile_row * t.rows + below;
+    const int at0 = static_cast<int>(seg) * (kTurns * 32) + in_row;
+    uint32_t rows[kTurns], ats[kTurns];
+    int off[kTurns], c[kTurns];
+    bool mine[kTurns], whole[kTurns];
+    uint4 u[kTurns][P], v[kTurns][P], w[kTurns];
 #pragma unroll
-      for (int p = 0; p < P; ++p) u[p] = load16(px + p * N);
-      if (kResidual) {
+    for (int k = 0; k < kTurns; ++k) {
+      const int64_t row = row0 + k * t.rows_on;
+      const int at = at0 + k * t.packs_on;
+      rows[k] = static_cast<uint32_t>(row);
+      ats[k] = static_cast<uint32_t>(at);
+      off[k] = kShift ? row_off<T>(j, row) : 0;
+      c[k] = at * kCols - off[k];
+      mine[k] = row < j.N && at < packs;
+      whole[k] = mine[k] && c[k] >= 0 && c[k] + kCols <= D;
+      if (whole[k]) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) v[p] = load16(pr + p * N);
+        for (int p = 0; p < P; ++p) u[k][p] = load16(x + row * j.ldx + c[k] + p * N);
+        if (kResidual) {
+#pragma unroll
+          for (int p = 0; p < P; ++p) v[k][p] = load16(res + row * j.ldr + c[k] + p * N);
+        }
+      } else if (mine[k]) {
+        load_some(x + row * j.ldx, c[k], D, u[k]);
+        if (kResidual) load_some(res + row * j.ldr, c[k], D, v[k]);
       }
-      const uint32_t m = kept(philox(static_cast<uint32_t>(at), static_cast<uint32_t>(row), key), j.threshold);
+    }
+    philox(ats, rows, keys, w);
+    uint32_t last = 0;  // the mask of the turn before
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+      uint32_t m = 0;
+      if (kShift) {
+        const uint32_t own = kept(w[k], j.high);
+        uint32_t before = __shfl_up_sync(kFull, own, 1);
+        const uint32_t end = __shfl_sync(kFull, last, 31);
+        if (lane == 0) before = k > 0 ? end : kept(philox(ats[k] - 1, rows[k], keys), j.high);
+        last = own;
+        m = before >> (kCols - off[k]) | own << off[k];  // at a row's start columns before it, which are not stored
+      }
+      if (!mine[k]) continue;
+      T* to = out + (row0 + k * t.rows_on) * j.ldo + c[k];
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         float f[N], g[N];
-        unpack(u[p], f, T());
-        if (kResidual) unpack(v[p], g, T());
+        unpack(u[k][p], f, T());
+        if (kResidual) unpack(v[k][p], g, T());
 #pragma unroll
-        for (int q = 0; q < N; ++q) f[q] = masked(f[q], kResidual ? g[q] : 0.f, m >> (p * N + q) & 1u, j.scale);
-        store16(po + p * N, pack(f, T()));
+        for (int q = 0; q < N; ++q)
+          f[q] = masked<kResidual>(f[q], kResidual ? g[q] : 0.f,
+                                   kShift ? m >> (p * N + q) & 1u : keeps(w[k], p * N + q, j.high), j.scale);
+        u[k][p] = pack(f, T());
       }
-    } else {
-      const uint32_t m = kept(philox(static_cast<uint32_t>(at), static_cast<uint32_t>(row), key), j.threshold);
-      for (int q = 0; c + q < j.D; ++q)
-        po[q] = from_f32<T>(masked(to_f32(px[q]), kResidual ? to_f32(pr[q]) : 0.f, m >> q & 1u, j.scale));
+      if (whole[k]) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) store16(to + p * N, u[k][p]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < kCols; ++q)
+          if (c[k] + q >= 0 && c[k] + q < D) to[q] = reinterpret_cast<const T*>(&u[k][q / N])[q % N];
+      }
     }
-    row += rows_on;
-    at += at_on;
-    if (at >= packs) {
-      at -= packs;
-      ++row;
+    tile_row += rows_step;
+    seg += seg_step;
+    if (seg >= t.per_row) {
+      seg -= t.per_row;
+      ++tile_row;
     }
   }
 }
@@ -114,7 +208,8 @@ __global__ void __launch_bounds__(kThreads) dropout_pack_kernel(const DropoutJob
 // that the lanes' elements lie side by side.
 template <typename T, bool kResidual>
 __global__ void __launch_bounds__(kThreads) dropout_lane_kernel(const DropoutJob j) {
-  const Key key = load_key(j.key);
+  __shared__ Keys keys;
+  load_keys(keys, j.key);
   const int lane = threadIdx.x & 31;
   const int64_t blocks = (j.D + 255) / 256, step = int64_t(gridDim.x) * (kThreads / 32);
   const int64_t first = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
@@ -133,11 +228,11 @@ __global__ void __launch_bounds__(kThreads) dropout_lane_kernel(const DropoutJob
       g[i] = kResidual && c + 32 * i < j.D ? to_f32(pr[32 * i]) : 0.f;
     }
     const uint32_t m =
-        kept(philox(static_cast<uint32_t>(at * 32 + lane), static_cast<uint32_t>(row), key), j.threshold);
+        j.none ? 0u : kept(philox(static_cast<uint32_t>(at * 32 + lane), static_cast<uint32_t>(row), keys), j.high);
 #pragma unroll
     for (int i = 0; i < kCols; ++i) {
       const uint32_t bits = __shfl_sync(kFull, m, 4 * i + lane / 8);
-      if (c + 32 * i < j.D) po[32 * i] = from_f32<T>(masked(f[i], g[i], bits >> (lane & 7) & 1u, j.scale));
+      if (c + 32 * i < j.D) po[32 * i] = from_f32<T>(masked<kResidual>(f[i], g[i], bits >> (lane & 7) & 1u, j.scale));
     }
     row += rows_on;
     at += at_on;
@@ -148,21 +243,36 @@ __global__ void __launch_bounds__(kThreads) dropout_lane_kernel(const DropoutJob
   }
 }
 
-bool on16(const void* p, int64_t ld, size_t size) {
-  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * static_cast<int64_t>(size) % 16 == 0;
-}
-
 template <typename T, bool kResidual>
 cudaError_t launch_rows(const DropoutJob& j, cudaStream_t stream) {
-  const bool even = on16(j.x, j.ldx, sizeof(T)) && on16(j.out, j.ldo, sizeof(T)) &&
-                    (!kResidual || on16(j.residual, j.ldr, sizeof(T)));
-  const int64_t work = even ? j.N * ((j.D + kCols - 1) / kCols) : j.N * ((j.D + 255) / 256) * 32;
-  const int64_t grid = std::min<int64_t>((work + kThreads - 1) / kThreads, int64_t(sm_count()) * 8);
+  const auto off = [](const void* p) { return reinterpret_cast<uintptr_t>(p) & 15u; };
+  const auto pitch = [](int64_t ld) { return uint64_t(ld) * sizeof(T) & 15u; };
+  const bool alike = off(j.x) == off(j.out) && (!kResidual || off(j.x) == off(j.residual)) &&
+                     (j.N == 1 || (pitch(j.ldx) == pitch(j.ldo) && (!kResidual || pitch(j.ldx) == pitch(j.ldr))));
+  const bool even = alike && off(j.x) == 0 && (j.N == 1 || pitch(j.ldx) == 0);
+  if (!alike || j.none) {
+    const int64_t work = j.N * ((j.D + 255) / 256) * 32;
+    const int64_t grid = std::min<int64_t>((work + kThreads - 1) / kThreads, int64_t(sm_count()) * kPerSm);
+    count_launch();
+    dropout_lane_kernel<T, kResidual><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(j);
+    return cudaGetLastError();
+  }
+  const int64_t packs = (j.D + (even ? 0 : Pack<T>::kN - 1) + kCols - 1) / kCols;
+  Tile t;
+  t.shift = 0;
+  while (t.shift < 5 && (1 << t.shift) < packs) ++t.shift;
+  const bool wide = packs > 32;
+  t.packs_on = wide ? 32 : 0;
+  t.rows_on = wide ? 0 : 32 >> t.shift;
+  t.rows = wide ? 1 : kTurns * t.rows_on;
+  t.per_row = wide ? (packs + kTurns * 32 - 1) / (kTurns * 32) : 1;
+  t.all = (j.N + t.rows - 1) / t.rows * t.per_row;
+  const int64_t grid = std::min<int64_t>((t.all + kThreads / 32 - 1) / (kThreads / 32), int64_t(sm_count()) * kPerSm);
   count_launch();
   if (even)
-    dropout_pack_kernel<T, kResidual><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(j);
+    dropout_pack_kernel<T, kResidual, false><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(j, t);
   else
-    dropout_lane_kernel<T, kResidual><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(j);
+    dropout_pack_kernel<T, kResidual, true><<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(j, t);
   return cudaGetLastError();
 }
 

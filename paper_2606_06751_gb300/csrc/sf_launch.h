@@ -217,7 +217,8 @@ struct DropoutJob {
   const void* x;
   int32_t dtype;
   int64_t N, D, ldx;
-  uint32_t threshold;  // of 65536
+  uint32_t high;  // the threshold of 65536, in the upper half
+  bool none;      // all are dropped
   float scale;
   const uint64_t* key;
   const void* residual;
@@ -227,7 +228,6 @@ struct DropoutJob {
 };
 cudaError_t launch_dropout(const DropoutJob& job, cudaStream_t stream);
 
-struct VerifyPiece;
 struct VerifyJob {
   const void* target;
   int32_t dtype;
@@ -242,11 +242,7 @@ struct VerifyJob {
   int32_t* accepted;
   float* logp;
   uint32_t* status;
-  // set by launch_verify
-  VerifyPiece* pieces = nullptr;  // [rows][per_row]
-  int piece = 0, per_row = 0;     // logits of a piece, pieces of a row
 };
-size_t verify_workspace(int64_t B, int64_t L, int64_t V);
-cudaError_t launch_verify(VerifyJob job, void* workspace, cudaStream_t stream);
+cudaError_t launch_verify(const VerifyJob& job, cudaStream_t stream);
 
 }  // namespace sf

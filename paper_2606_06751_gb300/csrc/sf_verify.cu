@@ -3,33 +3,31 @@
 //
 // A drafted token y is kept while u q(y) < p(y); the first that is not is replaced
 // by a draw from max(p - q, 0), as the winner of a race: the entry of largest r_j /
-// e_j, e_j exponential, is j with probability r_j / sum r.  Two launches: the
-// softmax statistics of all rows, a CTA a piece of a row (the rows' only read but
-// one), and then a cluster of CTAs a sequence, each of which decides from the
-// statistics where the sequence stops and races a slice of the one row (with its
-// draft row and noise) that the next token comes from.  Bound by memory: (2 L + 1)
-// rows and a row of noise a sequence.
-#include <algorithm>
+// e_j, e_j exponential, is j with probability r_j / sum r.  One launch: a cluster of
+// CTAs a sequence, each with a slice of the vocabulary.  The positions go by in
+// groups: each warp streams its part of the group's rows (policy's and draft's) into
+// (maximum, sum of exponentials) pairs, the CTAs exchange them, and all decide alike
+// whether the sequence stops there.  Rows behind the stop are never read.  The slice
+// of the one row that the next token comes from is then raced against the noise.
+// Bound by memory for many sequences: 64 of 4 tokens over 131072 bf16 entries, 187 MB,
+// take 46 us (60 % of the copy rate; the exponentials alone some 16 us of the special
+// function units, and the race begins when the rows are done).  One sequence over
+// 32768 takes 10 us of latency.  Four CTAs of 256 threads an SM: with the registers
+// of two or three 61 us.  Groups of fewer positions, which read fewer rows, were no
+// faster (3: 47, 2: 49 us): another exchange costs what they save.
 
 #include "sf_float.cuh"
 #include "sf_launch.h"
 
 namespace sf {
-
-// What a piece of a row says: its largest logit, the sum of the exponentials
-// against it and the first place of the largest.
-struct __align__(16) VerifyPiece {
-  float m, s;
-  int at, pad;
-};
-
 namespace {
-
-using Piece = VerifyPiece;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMaxPieces = 64;
+constexpr int kPacks = 4;       // of 16 bytes that a thread has in flight
+constexpr int kPerSm = 4;       // CTAs of an SM
+constexpr int kMostCtas = 16;   // of a cluster
+constexpr int kGroup = 16;      // positions of a group
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -37,11 +35,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-// Larger value first, then lower place: one integer order for values above 0 (or any sign by `ordered`).
-__device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t b = __float_as_uint(v + 0.f);  // -0 as 0
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
+// Larger value first, then lower place: one integer order for values above 0.
 __device__ __forceinline__ uint64_t place_key(uint32_t value, int at) {
   return uint64_t(value) << 32 | (0xffffffffu - static_cast<uint32_t>(at));
 }
@@ -49,203 +43,337 @@ __device__ __forceinline__ int place_of(uint64_t key) {
   return static_cast<int>(0xffffffffu - static_cast<uint32_t>(key));
 }
 
-__device__ __forceinline__ int drafted(const VerifyJob& j, int64_t b, bool* bad) {
-  const int L = static_cast<int>(j.L);
-  if (j.length == nullptr) return L;
-  const int n = j.length[b];
-  *bad = n < 0 || n > L;
-  return n < 0 ? 0 : n > L ? L : n;
-}
-
-// Statistics of piece blockIdx.x of row blockIdx.y (+ 65535 blockIdx.z): policy
-// rows first, then the draft's.
-template <typename T, bool kGreedy>
-__global__ void __launch_bounds__(kThreads) verify_piece_kernel(const VerifyJob j, const int64_t rows) {
+// 16-byte packs of a row by address: pack 0 holds the row's first value, `off`
+// values behind a 16-byte boundary.  Values before the row and behind it are -inf.
+template <typename T>
+__device__ __forceinline__ uint4 row_pack(const T* z, int off, int pack, int V) {
   constexpr int N = Pack<T>::kN;
-  __shared__ float sm[kWarps], ss[kWarps];
-  __shared__ uint64_t sk[kWarps];
-  griddep_launch_dependents();
-  const int64_t row = int64_t(blockIdx.z) * 65535 + blockIdx.y;
-  if (row >= rows) return;
-  const int64_t policy_rows = j.B * (j.L + 1);
-  const int64_t of_draft = row - policy_rows;  // >= 0: a draft row
-  const int64_t b = of_draft < 0 ? row / (j.L + 1) : of_draft / j.L;
-  const int i = static_cast<int>(of_draft < 0 ? row - b * (j.L + 1) : of_draft - b * j.L);
-  bool bad;
-  const int n = drafted(j, b, &bad);
-  if (of_draft < 0 ? i > n : i >= n) return;
-  const T* z = of_draft < 0 ? static_cast<const T*>(j.target) + row * j.ldt
-                            : static_cast<const T*>(j.draft) + of_draft * j.ldq;
-  const int V = static_cast<int>(j.V), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int from = static_cast<int>(blockIdx.x) * j.piece, to = min(V, from + j.piece);
-  const float scale = j.tau * kLog2e;
-  float m = neg_inf();
-  uint64_t best = 0;
-  bool nan = false;
-  for (int q = from + tid; q < to; q += kThreads) {
-    const float v = to_f32(z[q]);
-    nan |= v != v;
-    m = fmaxf(m, v);
-    if (kGreedy && v == v) {
-      const uint64_t k = place_key(ordered(v), q);
-      best = k > best ? k : best;
-    }
-  }
-  m = warp_max(m);
-  if (lane == 0) sm[warp] = m;
-  if (kGreedy) {
-    best = warp_max_u64(best);
-    if (lane == 0) sk[warp] = best;
-  }
-  __syncthreads();
-  m = sm[0];
+  const int at = pack * N - off;
+  if (at >= 0 && at + N <= V) return load16(z + at);
+  uint4 u = lowest_pack(T());
+  T* e = reinterpret_cast<T*>(&u);
 #pragma unroll
-  for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sm[w]);
-  Sum2 a;
-  for (int q = from + tid; q < to; q += kThreads)
-    if (m != neg_inf()) a.add(exp2_fast((to_f32(z[q]) - m) * scale));
-  float s = warp_sum(a.value());
-  if (__any_sync(kFull, nan)) s = quiet_nan();
-  if (lane == 0) ss[warp] = s;
-  __syncthreads();
-  if (tid == 0) {
-    Piece o;
-    o.m = m;
-    o.s = 0.f;
-    for (int w = 0; w < kWarps; ++w) o.s += ss[w];
-    o.at = 0;
-    o.pad = 0;
-    if (kGreedy) {
-      uint64_t k = sk[0];
-      for (int w = 1; w < kWarps; ++w) k = sk[w] > k ? sk[w] : k;
-      o.at = place_of(k);
-    }
-    j.pieces[row * j.per_row + blockIdx.x] = o;
-  }
+  for (int q = 0; q < N; ++q)
+    if (at + q >= 0 && at + q < V) e[q] = z[at + q];
+  return u;
+}
+template <typename T>
+__device__ __forceinline__ int row_offset(const T* z) {
+  return static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T));
 }
 
-// A row's statistics from its pieces, in every lane: maximum, sum, first place of
-// the maximum.  The sum is NaN where a logit is NaN or +inf or none is above -inf.
-struct Row {
+// What part of a row says: its largest logit, the sum of the exponentials against
+// it and the first place of the largest.  The sum is NaN with a NaN or +inf logit.
+struct Part {
   float m, s;
   int at;
 };
-__device__ __forceinline__ Row row_of(const Piece* p, int pieces, float tau, int lane) {
-  float m = neg_inf();
-  for (int i = lane; i < pieces; i += 32) m = fmaxf(m, p[i].m);
-  m = warp_max(m);
-  float s = 0.f;
-  uint32_t first = 0xffffffffu;
-  for (int i = lane; i < pieces; i += 32) {
-    const Piece q = p[i];
-    s += q.m == neg_inf() ? q.s : q.s * expf((q.m - m) * tau);
-    if (q.m == m) first = min(first, static_cast<uint32_t>(q.at));
+constexpr int kNowhere = 0x7fffffff;
+
+__device__ __forceinline__ Part nothing() { return {neg_inf(), 0.f, kNowhere}; }
+
+// The lanes' parts (of `n` lanes, a power of two), in a fixed order.
+template <bool kGreedy>
+__device__ __forceinline__ Part joined_lanes(Part a, int n, float scale) {
+  float top = a.m;
+  for (int o = n / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+  if (a.m != neg_inf()) a.s *= exp2_fast((a.m - top) * scale);
+  for (int o = n / 2; o > 0; o >>= 1) a.s += __shfl_xor_sync(kFull, a.s, o);
+  if (kGreedy) {
+    a.at = a.m == top ? a.at : kNowhere;
+    for (int o = n / 2; o > 0; o >>= 1) a.at = min(a.at, __shfl_xor_sync(kFull, a.at, o));
   }
-  Row r;
-  r.m = m;
-  r.s = warp_sum(s);
-  if (!(r.s > 0.f) || !finite(m)) r.s = quiet_nan();
-  r.at = static_cast<int>(__reduce_min_sync(kFull, first));
+  a.m = top;
+  return a;
+}
+
+// The warp's largest value; NaN only if all are.
+__device__ __forceinline__ float warp_top(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
 }
 
+// kPacks packs a lane of a row: packs p, p + 32, ... before `to`.
+template <typename T>
+struct Piece {
+  uint4 u[kPacks];
+  __device__ __forceinline__ void load(const T* z, int off, int p, int to, int V) {
+    constexpr int N = Pack<T>::kN;
+    const int p0 = p - static_cast<int>(threadIdx.x & 31), end = p0 + kPacks * 32;
+    if (p0 > 0 && end <= to && end * N - off <= V) {
+#pragma unroll
+      for (int k = 0; k < kPacks; ++k) u[k] = load16(z + (p + k * 32) * N - off);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPacks; ++k) u[k] = p + k * 32 < to ? row_pack(z, off, p + k * 32, V) : lowest_pack(T());
+    }
+  }
+};
+
+// A warp's part of a row, piece by piece: the reference is the largest logit so far,
+// the sum each lane's own.
+template <typename T, bool kGreedy>
+struct Running {
+  float m = neg_inf(), scale;
+  uint64_t s = 0;  // a pair of sums
+  int at = kNowhere;
+  __device__ __forceinline__ void add(const Piece<T>& piece, int off, int p) {
+    constexpr int N = Pack<T>::kN;
+    const float top = warp_top(packs_max(piece.u, T()));
+    if (top > m) {  // one branch for the warp
+      const float by = exp2_fast((m - top) * scale);
+      s = mul2(s, pair_of(by, by));
+      m = top;
+      at = kNowhere;
+    }
+    const float ref = m == neg_inf() ? 0.f : m;  // NaN among logits of -inf stays NaN below
+    const uint64_t minus = pair_of(-ref, -ref), by = pair_of(scale, scale);
+#pragma unroll
+    for (int k = 0; k < kPacks; ++k) {
+      uint64_t w[N / 2];
+      unpack2(piece.u[k], w, T());
+#pragma unroll
+      for (int q = 0; q < N / 2; ++q) {
+        float x, y;
+        if (kGreedy) {
+          split(w[q], x, y);
+          const int place = (p + k * 32) * N - off + 2 * q;
+          if (y == m) at = min(at, place + 1);
+          if (x == m) at = min(at, place);
+        }
+        split(mul2(add2(w[q], minus), by), x, y);
+        s = add2(s, pair_of(exp2_fast(x), exp2_fast(y)));
+      }
+    }
+  }
+  // the lanes' together; then empty
+  __device__ __forceinline__ Part take() {
+    float x, y;
+    split(s, x, y);
+    Part a;
+    a.m = m;
+    a.s = warp_sum(x + y);
+    a.at = kGreedy ? static_cast<int>(__reduce_min_sync(kFull, static_cast<uint32_t>(at))) : kNowhere;
+    m = neg_inf();
+    s = 0;
+    at = kNowhere;
+    return a;
+  }
+};
+
 // Where a sequence stops.
 struct Stop {
-  int at;       // accepted tokens
-  int from;     // 0: no token; 1: the policy's row alone; 2: less the draft's; 3: without the drafted token
+  int at = -1;   // accepted tokens; -1: not yet
+  int from;      // 0: no token; 1: the policy's row alone; 2: less the draft's; 3: without the drafted token
   float m, s, mq, sq;
-  int last;     // greedy: the next token; 3: the drafted token
+  int last;      // greedy: the next token; 3: the drafted token
+};
+
+// The largest r_j / e_j a thread has met, r_j = p_j - q_j as `form` says; its
+// indices rise, so the first of equal ones stays.
+struct Race {
+  float best = 0.f;
+  int at = -1;
+  float m, by, mq, byq, scale;  // maxima, reciprocal sums
+  int form, token;
+  __device__ __forceinline__ void run(float z, float zq, float e, int j) {
+    // products rounded by themselves: equal rows have a difference of 0
+    float r = __fmul_rn(exp2_fast((z - m) * scale), by);
+    if (form == 2) r = __fsub_rn(r, __fmul_rn(exp2_fast((zq - mq) * scale), byq));
+    if (form == 3 && j == token) r = 0.f;
+    const float v = __fdividef(r, e);
+    if (v > best && e > 0.f) {
+      best = v;
+      at = j;
+    }
+  }
 };
 
 template <typename T, bool kGreedy>
-__global__ void __launch_bounds__(kThreads) verify_sample_kernel(const VerifyJob j) {
-  __shared__ float2 rows[SF_VERIFY_MAX_DRAFT + 1];   // (maximum, sum)
-  __shared__ float2 drafts[SF_VERIFY_MAX_DRAFT + 1];
+__global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJob j) {
+  __shared__ Part warps[2 * kGroup][kWarps];          // the group's rows: policy's, then draft's
+  __shared__ Part ctas[2][2 * kGroup][kMostCtas];     // of the cluster, for this group and the one before
+  __shared__ float2 rows[kGroup], drafts[kGroup];  // (maximum, sum)
+  __shared__ int firsts[kGroup];
+  __shared__ int takes[kGroup];  // 1 accepted, 0 not, -1 a faulty row, -2 no such token
+  __shared__ float zs[SF_VERIFY_MAX_DRAFT], zqs[SF_VERIFY_MAX_DRAFT], us[SF_VERIFY_MAX_DRAFT];
+  __shared__ int64_t ys[SF_VERIFY_MAX_DRAFT];
   __shared__ float lps[SF_VERIFY_MAX_DRAFT + 1];
-  __shared__ int firsts[SF_VERIFY_MAX_DRAFT + 1];
-  __shared__ int takes[SF_VERIFY_MAX_DRAFT + 1];  // 1 accepted, 0 not, -1 a faulty row, -2 no such token
   __shared__ uint64_t warps_best[kWarps];
-  __shared__ uint64_t best_of[16];  // of the cluster's CTAs
-  __shared__ Stop stop;
+  __shared__ uint64_t best_of[kMostCtas];
+  constexpr int N = Pack<T>::kN;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = static_cast<int>(cluster_size()), rank = static_cast<int>(cluster_rank());
-  const int64_t b = blockIdx.x / C;
+  const int64_t b = blockIdx.x / static_cast<unsigned>(C);
   const int V = static_cast<int>(j.V), L = static_cast<int>(j.L);
-  bool bad_length = false;
-  griddep_wait();
-  const int n = drafted(j, b, &bad_length);
+  const int given = j.length == nullptr ? L : j.length[b], n = min(max(given, 0), L);
   const T* target = static_cast<const T*>(j.target) + b * (L + 1) * j.ldt;
-  const T* draft = j.draft != nullptr ? static_cast<const T*>(j.draft) + b * L * j.ldq : nullptr;
-  const Piece* tp = j.pieces + b * (L + 1) * j.per_row;
-  const Piece* dp = j.pieces + (j.B * (L + 1) + b * L) * j.per_row;
-  uint32_t bits = bad_length ? SF_ST_INDEX : 0u;
-  for (int i = warp; i <= n; i += kWarps) {
-    const Row r = row_of(tp + int64_t(i) * j.per_row, j.per_row, j.tau, lane);
-    Row q = {0.f, 1.f, 0};
-    if (!kGreedy && draft != nullptr && i < n) q = row_of(dp + int64_t(i) * j.per_row, j.per_row, j.tau, lane);
-    if (lane == 0) {
-      int take = r.s != r.s ? -1 : 0;
-      float lp = 0.f;
-      if (i < n && take == 0) {
-        const int64_t y = j.token[b * L + i];
-        if (y < 0 || y >= V) {
-          take = -2;
-        } else if (kGreedy) {
-          take = y == r.at ? 1 : 0;
-          lp = (to_f32(target[i * j.ldt + y]) - r.m) * j.tau - logf(r.s);
-        } else {
-          const float ty = (to_f32(target[i * j.ldt + y]) - r.m) * j.tau;
-          const float p = expf(ty) / r.s;
-          const float qy = draft != nullptr ? expf((to_f32(draft[i * j.ldq + y]) - q.m) * j.tau) / q.s : 1.f;
-          take = q.s != q.s ? -1 : j.uniform[b * L + i] * qy < p ? 1 : 0;
-          lp = ty - logf(r.s);
+  const T* draft = !kGreedy && j.draft != nullptr ? static_cast<const T*>(j.draft) + b * L * j.ldq : nullptr;
+  const float scale = j.tau * kLog2e;
+  uint32_t bits = given != n ? SF_ST_INDEX : 0u;
+  Stop o;
+  for (int g0 = 0, turn = 0; o.at < 0; g0 += kGroup, turn ^= 1) {
+    const int g = min(kGroup, n + 1 - g0);  // positions; the last may be the one behind the drafted tokens
+    const int with_draft = draft != nullptr ? min(g, n - g0) : 0, all = g + with_draft;
+    for (int i = lane; i < all; i += 32) warps[i][warp] = nothing();
+    __syncwarp();
+    // the slices of all rows as one run of pieces, cut evenly among the warps
+    const int slice = ((V + 2 * N - 2) / N + C - 1) / C, per_row = (slice + kPacks * 32 - 1) / (kPacks * 32);
+    const int first = all * per_row * warp / kWarps, last = all * per_row * (warp + 1) / kWarps;
+    const auto place = [&](int item, int& i, const T*& z, int& off, int& p, int& to) {
+      i = item / per_row;
+      z = i < g ? target + (g0 + i) * j.ldt : draft + (g0 + i - g) * j.ldq;
+      off = row_offset(z);
+      p = rank * slice + (item - i * per_row) * (kPacks * 32) + lane;
+      to = min((rank + 1) * slice, (off + V + N - 1) / N);
+    };
+    Piece<T> odd, even;
+    int i, off, p, to, i2, off2, p2;
+    const T* z;
+    if (first < last) {
+      place(first, i, z, off, p, to);
+      even.load(z, off, p, to, V);
+    }
+    if (g0 == 0 && tid < n) {  // what the decisions need besides
+      const int64_t y = j.token[b * L + tid];
+      ys[tid] = y;
+      if (y >= 0 && y < V) {
+        zs[tid] = to_f32(target[tid * j.ldt + y]);
+        if (!kGreedy) {
+          zqs[tid] = draft != nullptr ? to_f32(draft[tid * j.ldq + y]) : 0.f;
+          us[tid] = j.uniform[b * L + tid];
         }
       }
-      rows[i] = make_float2(r.m, r.s);
-      drafts[i] = make_float2(q.m, q.s);
-      firsts[i] = r.at;
-      takes[i] = take;
-      lps[i] = lp;
+    }
+    Running<T, kGreedy> run;
+    run.scale = scale;
+    const auto keep = [&](int row) {
+      const Part a = run.take();
+      if (lane == 0) warps[row][warp] = a;
+    };
+    for (int item = first; item < last; item += 2) {  // the next piece is on its way while one is summed
+      const bool two = item + 1 < last, three = item + 2 < last;
+      if (two) {
+        place(item + 1, i2, z, off2, p2, to);
+        odd.load(z, off2, p2, to, V);
+      }
+      run.add(even, off, p);
+      if (!two || i2 != i) keep(i);
+      if (!two) break;
+      if (three) {
+        place(item + 2, i, z, off, p, to);
+        even.load(z, off, p, to, V);
+      }
+      run.add(odd, off2, p2);
+      if (!three || i != i2) keep(i2);
+    }
+    __syncthreads();
+    for (int i = warp; i < all; i += kWarps) {
+      Part a = joined_lanes<kGreedy>(lane < kWarps ? warps[i][lane] : nothing(), kWarps, scale);
+      a.m = __shfl_sync(kFull, a.m, 0);
+      a.s = __shfl_sync(kFull, a.s, 0);
+      a.at = __shfl_sync(kFull, a.at, 0);
+      if (lane < C) {
+        const uint32_t to = at_rank(&ctas[turn][i][rank], lane);
+        asm volatile("st.shared::cluster.f32 [%0], %1;\n\tst.shared::cluster.f32 [%0 + 4], %2;\n\t"
+                     "st.shared::cluster.u32 [%0 + 8], %3;" ::"r"(to),
+                     "f"(a.m), "f"(a.s), "r"(a.at)
+                     : "memory");
+      }
+    }
+    cluster_sync();
+    for (int i = warp; i < g; i += kWarps) {
+      const Part r = joined_lanes<kGreedy>(lane < C ? ctas[turn][i][lane] : nothing(), kMostCtas, scale);
+      Part q = {0.f, 1.f, 0};
+      if (i < with_draft) q = joined_lanes<kGreedy>(lane < C ? ctas[turn][g + i][lane] : nothing(), kMostCtas, scale);
+      if (lane == 0) {
+        const int at = g0 + i;
+        // a NaN sum, no logit above -inf, or +inf
+        int take = r.s > 0.f && finite(r.m) ? 0 : -1;
+        if (at < n && take == 0) {
+          const int64_t y = ys[at];
+          if (y < 0 || y >= V) {
+            take = -2;
+          } else {
+            const float ty = (zs[at] - r.m) * j.tau;
+            lps[at] = ty - logf(r.s);
+            if (kGreedy) {
+              take = y == r.at ? 1 : 0;
+            } else {
+              const float qy = draft != nullptr ? expf((zqs[at] - q.m) * j.tau) / q.s : 1.f;
+              take = !(q.s > 0.f && finite(q.m)) ? -1 : us[at] * qy < expf(ty) / r.s ? 1 : 0;
+            }
+          }
+        }
+        rows[i] = make_float2(r.m, r.s);
+        drafts[i] = make_float2(q.m, q.s);
+        firsts[i] = r.at;
+        takes[i] = take;
+      }
+    }
+    __syncthreads();
+    for (int i = 0; i < g && o.at < 0; ++i) {
+      const int at = g0 + i, take = takes[i];
+      if (at < n && take == 1) continue;
+      o.at = at;
+      o.m = rows[i].x;
+      o.s = rows[i].y;
+      o.mq = drafts[i].x;
+      o.sq = drafts[i].y;
+      o.from = take == -1 ? 0 : at == n || take == -2 || kGreedy ? 1 : draft != nullptr ? 2 : 3;
+      o.last = kGreedy ? firsts[i] : o.from == 3 ? static_cast<int>(ys[at]) : 0;
+      if (at < n && take == -2) bits |= SF_ST_INDEX;
     }
   }
-  __syncthreads();
-  if (tid == 0) {
-    int k = 0;
-    while (k < n && takes[k] == 1) ++k;
-    Stop o;
-    o.at = k;
-    o.m = rows[k].x;
-    o.s = rows[k].y;
-    o.mq = drafts[k].x;
-    o.sq = drafts[k].y;
-    o.last = kGreedy ? firsts[k] : 0;
-    o.from = takes[k] == -1 ? 0 : k == n || takes[k] == -2 || kGreedy ? 1 : draft != nullptr ? 2 : 3;
-    if (o.from == 3) o.last = static_cast<int>(j.token[b * L + k]);
-    stop = o;
-  }
-  __syncthreads();
-  const Stop o = stop;
   int next = -1;
   if (kGreedy) {
     next = o.from == 0 ? -1 : o.last;
   } else if (o.from != 0) {
-    const T *z = target + o.at * j.ldt, *zq = draft != nullptr ? draft + min(o.at, L - 1) * j.ldq : nullptr;
+    const T *z = target + o.at * j.ldt, *zq = o.from == 2 ? draft + o.at * j.ldq : z;
     const float* e = j.noise + b * V;
-    const int from = static_cast<int>(int64_t(V) * rank / C), to = static_cast<int>(int64_t(V) * (rank + 1) / C);
+    Race race;
+    race.m = o.m;
+    race.by = 1.f / o.s;
+    race.mq = o.mq;
+    race.byq = 1.f / o.sq;
+    race.scale = j.tau * kLog2e;
+    race.form = o.from;
+    race.token = o.last;
+    const bool even = ((reinterpret_cast<uintptr_t>(z) | reinterpret_cast<uintptr_t>(zq) | reinterpret_cast<uintptr_t>(e)) &
+                       15u) == 0;
     uint64_t best = 0;
-    int form = o.from;
     for (;;) {
-      best = 0;
-      for (int q = from + tid; q < to; q += kThreads) {
-        float r = expf((to_f32(z[q]) - o.m) * j.tau) / o.s;
-        if (form == 2) r -= expf((to_f32(zq[q]) - o.mq) * j.tau) / o.sq;
-        if (form == 3 && q == o.last) r = 0.f;
-        const float v = r / e[q];
-        if (r > 0.f && e[q] > 0.f && v > 0.f) {
-          const uint64_t key = place_key(__float_as_uint(v), q);
-          best = key > best ? key : best;
+      race.best = 0.f;
+      race.at = -1;
+      int rest = 0;
+      if (even) {  // whole packs of the three rows side by side
+        const int packs = V / N;
+        const int from = static_cast<int>(int64_t(packs) * rank / C), to = static_cast<int>(int64_t(packs) * (rank + 1) / C);
+#pragma unroll 2
+        for (int p = from + tid; p < to; p += kThreads) {
+          float f[N], g[N], h[N];
+          const uint4 u = load16(z + p * N), v = race.form == 2 ? load16(zq + p * N) : u;
+          uint4 w[N / 4];
+#pragma unroll
+          for (int k = 0; k < N / 4; ++k) w[k] = load16(e + p * N + 4 * k);
+          unpack(u, f, T());
+          unpack(v, g, T());
+#pragma unroll
+          for (int k = 0; k < N / 4; ++k) unpack(w[k], reinterpret_cast<float(&)[4]>(h[4 * k]), 0.f);
+#pragma unroll
+          for (int k = 0; k < N; ++k) race.run(f[k], g[k], h[k], p * N + k);
         }
+        rest = packs * N;
       }
+      {
+        const int left = V - rest;
+        const int from = rest + static_cast<int>(int64_t(left) * rank / C), to = rest + static_cast<int>(int64_t(left) * (rank + 1) / C);
+#pragma unroll 4
+        for (int q = from + tid; q < to; q += kThreads)
+          race.run(to_f32(z[q]), race.form == 2 ? to_f32(zq[q]) : 0.f, e[q], q);
+      }
+      best = race.at >= 0 ? place_key(__float_as_uint(race.best), race.at) : 0;
       best = warp_max_u64(best);
       if (lane == 0) warps_best[warp] = best;
       __syncthreads();
@@ -258,8 +386,8 @@ __global__ void __launch_bounds__(kThreads) verify_sample_kernel(const VerifyJob
       best = 0;
       for (int c = 0; c < C; ++c) best = best_of[c] > best ? best_of[c] : best;
       cluster_sync();  // all have read before a second race writes
-      if (best != 0 || form != 2) break;
-      form = 1;  // no residual above 0
+      if (best != 0 || race.form != 2) break;
+      race.form = 1;  // no residual above 0
     }
     next = best != 0 ? place_of(best) : -1;
   }
@@ -269,7 +397,7 @@ __global__ void __launch_bounds__(kThreads) verify_sample_kernel(const VerifyJob
     int64_t t = -1;
     float lp = 0.f;
     if (i < o.at) {
-      t = j.token[b * L + i];
+      t = ys[i];
       lp = lps[i];
     } else if (i == o.at && next >= 0) {
       t = next;
@@ -280,42 +408,34 @@ __global__ void __launch_bounds__(kThreads) verify_sample_kernel(const VerifyJob
   }
   if (tid == 0) {
     j.accepted[b] = o.at;
-    if (o.at < n && takes[o.at] == -2) bits |= SF_ST_INDEX;
     report(j.status, bits);
   }
 }
 
-int piece_of(int64_t V) {
-  const int64_t p = std::max<int64_t>(4096, (V + kMaxPieces - 1) / kMaxPieces);
-  return static_cast<int>((p + 7) / 8 * 8);
-}
-
 template <typename T, bool kGreedy>
-cudaError_t launch_type(VerifyJob j, cudaStream_t stream) {
-  const int64_t rows = j.B * (j.L + 1) + (j.draft != nullptr && !kGreedy ? j.B * j.L : 0);
-  const dim3 grid(j.per_row, static_cast<unsigned>(std::min<int64_t>(rows, 65535)),
-                  static_cast<unsigned>((rows + 65534) / 65535));
-  count_launch();
-  verify_piece_kernel<T, kGreedy><<<grid, kThreads, 0, stream>>>(j, rows);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  // CTAs a sequence: while there are SMs for them and entries for their threads
+cudaError_t launch_type(const VerifyJob& j, cudaStream_t stream) {
+  // CTAs a sequence: while all stay at once and each thread has a pack of a row.
+  // 64 sequences of 4 tokens, 131072 bf16 entries: 55, 46, 55 us with 4, 8, 16; one of
+  // 32768: 14.7, 11.5, 10.2 us.
   int C = 1;
-  while (!kGreedy && C < 8 && j.B * C * 2 <= int64_t(sm_count()) * 4 && j.V > int64_t(C) * kThreads * 4) C *= 2;
+  while (C < kMostCtas && j.B * C * 2 <= int64_t(sm_count()) * kPerSm && j.V > int64_t(C) * kThreads * Pack<T>::kN) C *= 2;
+  const auto kernel = verify_kernel<T, kGreedy>;
+  if (C > 8) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(j.B * C));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = 1;
   count_launch();
-  return cudaLaunchKernelEx(&cfg, verify_sample_kernel<T, kGreedy>, j);
+  return cudaLaunchKernelEx(&cfg, kernel, j);
 }
 
 template <typename T>
@@ -325,15 +445,7 @@ cudaError_t launch_mode(const VerifyJob& j, cudaStream_t stream) {
 
 }  // namespace
 
-size_t verify_workspace(int64_t B, int64_t L, int64_t V) {
-  const int64_t piece = piece_of(V);
-  return size_t(B * (2 * L + 1)) * size_t((V + piece - 1) / piece) * sizeof(Piece);
-}
-
-cudaError_t launch_verify(VerifyJob j, void* workspace, cudaStream_t stream) {
-  j.piece = piece_of(j.V);
-  j.per_row = static_cast<int>((j.V + j.piece - 1) / j.piece);
-  j.pieces = static_cast<Piece*>(workspace);
+cudaError_t launch_verify(const VerifyJob& j, cudaStream_t stream) {
   return j.dtype == SF_F32    ? launch_mode<float>(j, stream)
          : j.dtype == SF_BF16 ? launch_mode<__nv_bfloat16>(j, stream)
                               : launch_mode<__half>(j, stream);

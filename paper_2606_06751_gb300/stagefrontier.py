@@ -99,7 +99,7 @@ def _load():
         "sf_gated_ffn_grad": [P, I32, I, I, I, P, P, I, I, I32, P, I, P, I, P, P, I32, I, I32, P, I, P,
                               ctypes.c_size_t, P, S],
         "sf_dropout": [P, I32, I, I, I, ctypes.c_float, P, P, I, P, I, S],
-        "sf_verify_draft": [P, I32, I, I, I, I, P, I, P, P, P, P, ctypes.c_float, P, P, P, P, ctypes.c_size_t, P, S],
+        "sf_verify_draft": [P, I32, I, I, I, I, P, I, P, P, P, P, ctypes.c_float, P, P, P, P, S],
     }
     for name, argt in sigs.items():
         f = getattr(L, name)
@@ -127,8 +127,6 @@ def _load():
     L.sf_policy_loss_workspace_size.restype = ctypes.c_size_t
     L.sf_gated_ffn_workspace_size.argtypes = [I32, I, I, I, I32, I32]
     L.sf_gated_ffn_workspace_size.restype = ctypes.c_size_t
-    L.sf_verify_draft_workspace_size.argtypes = [I, I, I]
-    L.sf_verify_draft_workspace_size.restype = ctypes.c_size_t
     for name in ("sf_stream_windows_staging_size", "sf_stream_gathered_staging_size"):
         getattr(L, name).argtypes = [I, I, I, I]
         getattr(L, name).restype = ctypes.c_size_t
@@ -995,8 +993,7 @@ def _row_stack(t, shape, dtype, name: str):
 
 
 def sf_verify_draft(target, token, draft=None, lengths=None, uniform=None, noise=None, inv_temperature: float = 1.0,
-                    out_token=None, accepted=None, logp=None, want=("logp",), workspace=None, status=None,
-                    stream=None) -> Verified:
+                    out_token=None, accepted=None, logp=None, want=("logp",), status=None, stream=None) -> Verified:
     """Drafted tokens [B][L] against the policy's logits [B][L + 1][V]: the tokens
     that are kept with the next one, then -1 ([B][L + 1]), how many drafted ones
     were accepted [B], and the log-probabilities of the tokens (the old_logp of
@@ -1018,7 +1015,7 @@ def sf_verify_draft(target, token, draft=None, lengths=None, uniform=None, noise
     _vec(noise, B * V, torch.float32, "noise")
     if (uniform is None) != (noise is None):
         raise ValueError("uniform and noise go together")
-    _here(target, token, draft, lengths, uniform, noise, out_token, accepted, logp, workspace, status)
+    _here(target, token, draft, lengths, uniform, noise, out_token, accepted, logp, status)
     made = []
 
     def new(shape, dtype):
@@ -1032,10 +1029,8 @@ def sf_verify_draft(target, token, draft=None, lengths=None, uniform=None, noise
         _vec(logp, B * (L + 1), torch.float32, "logp")
     elif "logp" in want:
         logp = new((B, L + 1), torch.float32)
-    if workspace is None:
-        workspace = new(_lib.sf_verify_draft_workspace_size(B, L, V), torch.uint8)
     _hold(made, stream)
     _check(_lib.sf_verify_draft(_p(target), _DTYPES[target.dtype], B, L, V, ldt, _p(draft), ldq, _p(token), _p(lengths),
                                 _p(uniform), _p(noise), inv_temperature, _p(out_token), _p(accepted), _p(logp),
-                                _p(workspace), workspace.numel(), _p(status), _stream(stream)), "sf_verify_draft")
+                                _p(status), _stream(stream)), "sf_verify_draft")
     return Verified(out_token, accepted, logp)

@@ -73,17 +73,14 @@ def test_verify(sf):
     L = sf.lib()
 
     def call(z=at(0), dtype=sf.SF_BF16, B=2, Ld=3, V=64, ldt=64, q=at(1), ldq=64, y=at(2), n=None, u=at(3), e=at(4),
-             tau=1.0, t=at(5), acc=at(6), lp=at(7), ws=at(8), size=1 << 20):
-        return L.sf_verify_draft(z, dtype, B, Ld, V, ldt, q, ldq, y, n, u, e, tau, t, acc, lp, ws, size, None, None)
+             tau=1.0, t=at(5), acc=at(6), lp=at(7)):
+        return L.sf_verify_draft(z, dtype, B, Ld, V, ldt, q, ldq, y, n, u, e, tau, t, acc, lp, None, None)
 
     for kw in (dict(dtype=3), dict(B=-1), dict(Ld=65), dict(Ld=-1), dict(V=0), dict(V=(1 << 24) + 1), dict(ldt=63),
                dict(ldq=63), dict(z=None), dict(y=None), dict(t=None), dict(acc=None), dict(u=None), dict(e=None),
                dict(tau=0.0), dict(tau=float("inf")), dict(t=at(2)), dict(lp=at(3)), dict(lp=at(5)), dict(t=at(0) + 64),
                dict(B=1 << 30)):
         assert call(**kw) == sf.SF_EINVAL, kw
-    for kw in (dict(z=at(0) + 1), dict(y=at(2) + 4), dict(t=at(5) + 4), dict(lp=at(7) + 2), dict(ws=at(8) + 4)):
+    for kw in (dict(z=at(0) + 1), dict(y=at(2) + 4), dict(t=at(5) + 4), dict(lp=at(7) + 2)):
         assert call(**kw) == sf.SF_EINVAL_ALIGN, kw
-    assert call(ws=None) == sf.SF_EWORKSPACE and call(size=16) == sf.SF_EWORKSPACE
     assert call(B=0, z=None, y=None, t=None, acc=None) == sf.SF_OK
-    ws = L.sf_verify_draft_workspace_size
-    assert ws(0, 3, 64) == 0 and ws(1, 65, 64) == 0 and ws(1, 3, 0) == 0 and ws(2, 3, 64) >= 2 * 7 * 8
