@@ -205,16 +205,46 @@ struct Spread {
   uint4* to[3];
   int64_t rows[3], ld[3];
 };
-__global__ void __launch_bounds__(kThreads) ffn_spread_kernel(const Spread s, int64_t len, int64_t packs) {
-  const int part = blockIdx.y;
-  const int64_t all = s.rows[part] * packs, step = int64_t(gridDim.x) * kThreads;
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < all; i += step) {
-    const int64_t r = i / packs, c = (i - r * packs) * 8;
-    const unsigned short* p = s.from[part] + r * s.ld[part] + c;
-    uint32_t v[8];
+// A warp a run of 128 packs of a row.  A pack's 8 values lie in two of the source's
+// 16-byte words; the second is the next lane's first, read once more.
+__global__ void __launch_bounds__(kThreads) ffn_spread_kernel(const __grid_constant__ Spread s, int64_t len, int packs,
+                                                              int runs) {
+  griddep_launch_dependents();
+  const int part = blockIdx.y, lane = threadIdx.x & 31;
+  const int64_t all = s.rows[part] * runs, step = int64_t(gridDim.x) * (kThreads / 32);
+  const int64_t last = s.rows[part] * int64_t(s.ld[part]) - (s.ld[part] - len);  // values from the first to the last
+  for (int64_t i = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); i < all; i += step) {
+    const int64_t r = i / runs;
+    const int run = static_cast<int>(i - r * runs);
+    const unsigned short* row = s.from[part] + r * s.ld[part];
+    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 7u);
+    uint4* to = s.to[part] + r * packs;
+#pragma unroll 4
+    for (int p = run * 128 + lane; p < min(packs, run * 128 + 128); p += 32) {
+      const int64_t c = int64_t(p) * 8;
+      const int64_t at = r * s.ld[part] + c - off;  // of the first word
+      uint32_t w[9] = {0};
+      if (at >= 0 && at + 16 <= last) {
+        const uint4 a = load16(row + c - off), b = off != 0 ? load16(row + c - off + 8) : a;
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+        w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+        // by `off` values: whole words, then half a word
+        const int words = off >> 1;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = c + k < len ? p[k] : 0;
-    s.to[part][i] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+        for (int k = 0; k < 5; ++k) w[k] = words == 0 ? w[k] : words == 1 ? w[k + 1] : words == 2 ? w[k + 2] : w[min(k + 3, 8)];
+        if (off & 1) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t lo = c + 2 * k < len ? row[c + 2 * k] : 0u, hi = c + 2 * k + 1 < len ? row[c + 2 * k + 1] : 0u;
+          w[k] = lo | hi << 16;
+        }
+      }
+      to[p] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
 }
 
@@ -263,10 +293,10 @@ cudaError_t launch_ffn(FfnJob j, bool grad, void* workspace, cudaStream_t stream
       *data[i] = at;
       at += size_t(s.rows[i]) * packs * 16;
     }
-    const int64_t most = (std::max(j.T, j.F) * packs + kThreads - 1) / kThreads;
+    const int64_t runs = (packs + 127) / 128, most = (std::max(j.T, j.F) * runs + kThreads / 32 - 1) / (kThreads / 32);
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>(most, int64_t(sm_count()) * 8)), 3);
     count_launch();
-    ffn_spread_kernel<<<grid, kThreads, 0, stream>>>(s, j.H, packs);
+    ffn_spread_kernel<<<grid, kThreads, 0, stream>>>(s, j.H, static_cast<int>(packs), static_cast<int>(runs));
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     j.ldx = j.ldw = packs * 8;

@@ -42,6 +42,13 @@ struct Layout {
   static constexpr int kRows = kGated ? 64 : 128;  // of what is stored, in a CTA's 128 rows of D
 };
 
+__device__ __forceinline__ void prefetch_maps(const Maps& maps) {
+  prefetch_tensormap(&maps.a0);
+  prefetch_tensormap(&maps.a1);
+  prefetch_tensormap(&maps.b0);
+  prefetch_tensormap(&maps.b1);
+}
+
 // Copies block `kb` of the operands of a CTA's tile; `rows` is the tile's first m, `from` the first n it loads.
 template <int kProduct, int kCtas>
 __device__ __forceinline__ void copy_block(const Maps& maps, const Shape& s, int kb, int m, int n, int n_rows,
@@ -77,11 +84,24 @@ __device__ __forceinline__ void multiply_block(uint32_t d, uint32_t a, uint32_t 
                           operand_of<L::kBAlongK>(b + k * kStepBytes<L::kBAlongK>), desc, !(first && k == 0));
 }
 
+// K values to addresses `ld` apart: those of rows i * step < left.
+template <typename T, int K>
+__device__ __forceinline__ void store_down(T* p, int64_t ld, int step, int left, const T (&v)[K]) {
+  if ((K - 1) * step < left) {
+#pragma unroll
+    for (int i = 0; i < K; ++i, p += ld) *p = v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < K; ++i, p += ld)
+      if (i * step < left) *p = v[i];
+  }
+}
+
 // K values of h, or of dg and du (and h), from their g and u: feature f of tokens
 // t, t + step, ... before t + most and T.  One basic block, so that the K chains of exponential and quotient overlap.
 template <typename T, int kProduct, int kAct, int K>
 __device__ __forceinline__ void store_act(const FfnJob& j, int64_t t, int step, int64_t f, int most, const float (&g)[K],
-                                          const float (&u)[K], const float (&dh)[K]) {
+                                          const float (&u)[K], const T (&dh)[K]) {
   using A = Activation<kAct, true>;
   T v[K], w[K], x[K];
 #pragma unroll
@@ -92,30 +112,21 @@ __device__ __forceinline__ void store_act(const FfnJob& j, int64_t t, int step, 
       float a, slope;
       A::both(g[i], a, slope);
       v[i] = from_f32<T>(a * u[i]);
-      w[i] = from_f32<T>(dh[i] * u[i] * slope);
-      x[i] = from_f32<T>(dh[i] * a);
+      const float d = to_f32(dh[i]);
+      w[i] = from_f32<T>(d * u[i] * slope);
+      x[i] = from_f32<T>(d * a);
     }
   }
   const int left = static_cast<int>(min(int64_t(most), j.T - t));
-  if (kProduct == kForward || j.h != nullptr) {
-    T* p = static_cast<T*>(j.h) + t * j.ldh + f;
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-      if (i * step < left) p[i * step * j.ldh] = v[i];
-  }
+  if (kProduct == kForward || j.h != nullptr) store_down(static_cast<T*>(j.h) + t * j.ldh + f, step * j.ldh, step, left, v);
   if constexpr (kProduct == kInner) {
-    T *p = static_cast<T*>(j.dg) + t * j.ldg + f, *r = static_cast<T*>(j.du) + t * j.ldg + f;
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-      if (i * step < left) {
-        p[i * step * j.ldg] = w[i];
-        r[i * step * j.ldg] = x[i];
-      }
+    store_down(static_cast<T*>(j.dg) + t * j.ldg + f, step * j.ldg, step, left, w);
+    store_down(static_cast<T*>(j.du) + t * j.ldg + f, step * j.ldg, step, left, x);
   }
 }
 template <typename T, int kProduct, int K>
 __device__ __forceinline__ void store_gated(const FfnJob& j, int64_t t, int step, int64_t f, int most, const float (&g)[K],
-                                            const float (&u)[K], const float (&dh)[K]) {
+                                            const float (&u)[K], const T (&dh)[K]) {
   if (f >= j.F || t >= j.T) return;
   switch (j.act) {
     case SF_ACT_GELU: return store_act<T, kProduct, SF_ACT_GELU>(j, t, step, f, most, g, u, dh);
@@ -124,40 +135,59 @@ __device__ __forceinline__ void store_gated(const FfnJob& j, int64_t t, int step
     default: return store_act<T, kProduct, SF_ACT_SILU>(j, t, step, f, most, g, u, dh);
   }
 }
-// Their upstream gradients.
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
+// Their upstream gradients, as they are: a conversion would wait for them.
 template <typename T, int K>
-__device__ __forceinline__ void load_dh(const FfnJob& j, int64_t t, int step, int64_t f, float (&dh)[K]) {
+__device__ __forceinline__ void load_dh(const FfnJob& j, int64_t t, int step, int64_t f, T (&dh)[K]) {
   const T* p = static_cast<const T*>(j.dh) + t * j.lddh + f;
   const int left = f < j.F && t < j.T ? static_cast<int>(min(int64_t(K) * step, j.T - t)) : 0;
 #pragma unroll
-  for (int i = 0; i < K; ++i) dh[i] = i * step < left ? to_f32(p[i * step * j.lddh]) : 0.f;
+  for (int i = 0; i < K; ++i, p += step * j.lddh) dh[i] = i * step < left ? *p : from_f32<T>(0.f);
 }
 
-// One value of dx or of a weight's gradient.
-template <typename T, int kProduct>
-__device__ __forceinline__ void store_plain(const FfnJob& j, bool second, int64_t m, int64_t n, float v) {
-  if constexpr (kProduct == kDx) {
-    static_cast<T*>(j.dx)[n * j.lddx + m] = from_f32<T>(v);
-  } else {
-    void* w = second ? j.dw_up : j.dw_gate;
-    if (j.dw_dtype == SF_F32) {
-      float* p = static_cast<float*>(w) + n * j.lddw + m;
-      *p = j.accumulate ? *p + v : v;
-    } else {
-      T* p = static_cast<T*>(w) + n * j.lddw + m;
-      *p = from_f32<T>(j.accumulate ? to_f32(*p) + v : v);
+// K values of dx or of a weight's gradient: column m of rows n, n + step, ... before n + most and the last.
+template <typename T, int kProduct, int K>
+__device__ __forceinline__ void store_plain(const FfnJob& j, bool second, int64_t m, int64_t n, int step, int most,
+                                            const float (&v)[K]) {
+  const int64_t rows = kProduct == kDx ? j.T : j.F;
+  if (m >= j.H || n >= rows) return;
+  const int left = static_cast<int>(min(int64_t(most), rows - n));
+  void* w = kProduct == kDx ? j.dx : second ? j.dw_up : j.dw_gate;
+  const int64_t ld = kProduct == kDx ? j.lddx : j.lddw;
+  if (kProduct == kDw && j.dw_dtype == SF_F32) {
+    float* p = static_cast<float*>(w) + n * ld + m;
+    float x[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) x[i] = v[i];
+    if (j.accumulate) {
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (i * step < left) x[i] += p[i * step * ld];
     }
+    store_down(p, step * ld, step, left, x);
+  } else {
+    T* p = static_cast<T*>(w) + n * ld + m;
+    T x[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) x[i] = from_f32<T>(v[i]);
+    if (kProduct == kDw && j.accumulate) {
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (i * step < left) x[i] = from_f32<T>(to_f32(p[i * step * ld]) + v[i]);
+    }
+    store_down(p, step * ld, step, left, x);
   }
 }
 
 // ---------------------------------------------------------------- large products: a pair of SMs a tile
 
-constexpr int kPairThreads = 384, kStoreWarps = 8;
-constexpr int kSwapBytes = 2 * 2 * 4 * 8 * 32 * 4;  // groups, parities, quadrants, columns, lanes
+constexpr int kGroups = 3, kStoreWarps = 4 * kGroups, kPairThreads = 128 + 32 * kStoreWarps;
+constexpr int kSwapBytes = kGroups * 2 * 4 * 8 * 32 * 4;  // groups, parities, quadrants, columns, lanes
 
 // Persistent pairs of CTAs: each pair multiplies 256 rows by N columns, the sums of
 // one tile being stored while the next is multiplied.  Warp 0 copies, warp 1 of the
-// pair's first CTA multiplies, warps 4 to 11 store.
+// pair's first CTA multiplies, warps from 4 store.
 template <typename T, int kProduct>
 __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     ffn_pair_kernel(const __grid_constant__ Maps maps, const FfnJob j, const Shape s) {
@@ -175,6 +205,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
   const int64_t pairs = gridDim.x / 2;
 
   if (tid == 0) {
+    prefetch_maps(maps);
     abort = 0;
     for (int i = 0; i < s.stages; ++i) {
       mbar_init(&full[i], 1);
@@ -187,9 +218,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     fence_barrier_init();
   }
   if (warp == 2) tensor_alloc<2>(&tensor_at, 512);
+  griddep_launch_dependents();
   tensor_fence_before();
   cluster_sync();
   tensor_fence_after();
+  griddep_wait();
   const uint32_t sums = tensor_at;
 
   // a tile's first m and n of the pair; n tiles in groups of 8 m tiles, whose operands stay in L2
@@ -207,10 +240,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
 
   if (warp == 0) {
     if (lane == 0) {
-      prefetch_tensormap(&maps.a0);
-      prefetch_tensormap(&maps.a1);
-      prefetch_tensormap(&maps.b0);
-      prefetch_tensormap(&maps.b1);
       int stage = 0;
       uint32_t parity = 1;
       bool ok = true;
@@ -259,8 +288,29 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
         if (ok) products_arrive<2>(&sums_full[buf]);
       }
     }
+  } else if (kProduct == kInner && warp == 3) {
+    // the upstream gradients of the next tile, into L2: their loads come while the copies fill every queue
+    const auto fetch = [&](int64_t tile) {
+      if (tile >= tiles) return;
+      int64_t m, n;
+      bool second;
+      tile_of(tile, m, n, second);
+      m += rank * L::kRows;
+      if (m >= j.F) return;
+      for (int64_t t = n + lane; t < n + s.N && t < j.T; t += 32) {
+        const T* p = static_cast<const T*>(j.dh) + t * j.lddh + m;
+        prefetch_l2(p);
+        prefetch_l2(p + min(int64_t(L::kRows), j.F - m) - 1);
+      }
+    };
+    int64_t done = 0;
+    fetch(blockIdx.x / 2);
+    for (int64_t tile = blockIdx.x / 2; tile < tiles; tile += pairs, ++done) {
+      fetch(tile + pairs);
+      if (!mbar_wait_bounded(&sums_full[done & 1], uint32_t(done >> 1 & 1), &abort)) break;
+    }
   } else if (warp >= 4) {
-    // two groups of four warps take chunks of 16 columns in turn; a warp reads the 32 lanes of its quadrant
+    // groups of four warps take chunks of 16 columns in turn; a warp reads the 32 lanes of its quadrant
     const int q = warp & 3, group = (warp - 4) >> 2;
     float* swap = reinterpret_cast<float*>(base + s.stages * stage_bytes) + group * (2 * 4 * 8 * 32);
     int64_t done = 0;
@@ -271,20 +321,34 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       tile_of(tile, m, n, second);
       m += rank * L::kRows;
       const int buf = static_cast<int>(done & 1);
+      T dh_next[8];
+      if constexpr (kProduct == kInner)
+        load_dh<T>(j, n + 16 * group + (q < 2 ? 0 : 8), 1, m + 32 * (q & 1) + lane, dh_next);
       const bool ok = mbar_wait_bounded(&sums_full[buf], uint32_t(done >> 1 & 1), &abort);  // else garbage, and a status
       tensor_fence_after();
       const uint32_t at = sums + buf * 256 + (uint32_t(q) << 21);
-      for (int c = 16 * group; c < s.N; c += 32) {
+      const auto give_back = [&] {  // this warp has read its last columns of the tile
+        tensor_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_at(at_rank(&sums_empty[buf], 0));
+      };
+      for (int c = 16 * group; c < s.N; c += 16 * kGroups) {
         uint32_t v[16];
         if constexpr (L::kGated) {
           // quadrants 0 and 1 hold g, 2 and 3 u of the same features: each keeps half of the columns
           // and gets the other factor for them
           const int mine = q < 2 ? 0 : 8;
           const int64_t f = m + 32 * (q & 1) + lane, t0 = n + c + mine;
-          float g[8], u[8], dh[8];
-          if constexpr (kProduct == kInner) load_dh<T>(j, t0, 1, f, dh);
+          float g[8], u[8];
+          T dh[8];
+          if constexpr (kProduct == kInner) {  // on their way since the chunk before
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dh[i] = dh_next[i];
+            if (c + 16 * kGroups < s.N) load_dh<T>(j, t0 + 16 * kGroups, 1, f, dh_next);
+          }
           tensor_load16(at + c, v);
           tensor_loaded();
+          if (c + 16 * kGroups >= s.N) give_back();
           float* out = swap + (turn * 4 + q) * 8 * 32 + lane;
           const float* in = swap + (turn * 4 + (q ^ 2)) * 8 * 32 + lane;
 #pragma unroll
@@ -301,16 +365,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
         } else {
           tensor_load16(at + c, v);
           tensor_loaded();
-          const int64_t row = m + 32 * q + lane, columns = kProduct == kDx ? j.T : j.F;
+          if (c + 16 * kGroups >= s.N) give_back();
+          float x[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (row < j.H && n + c + i < columns)
-              store_plain<T, kProduct>(j, second, row, n + c + i, __uint_as_float(v[i]));
+          for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(v[i]);
+          store_plain<T, kProduct>(j, second, m + 32 * q + lane, n + c, 1, 16, x);
         }
       }
-      tensor_fence_before();
-      __syncwarp();
-      if (lane == 0) arrive_at(at_rank(&sums_empty[buf], 0));
+      if (16 * group >= s.N) give_back();  // no chunk of its own
       if (!ok && lane == 0) report(j.status, SF_ST_TIMEOUT);
     }
   }
@@ -352,6 +414,7 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
   const int first = static_cast<int>(int64_t(s.blocks) * rank / C), last = static_cast<int>(int64_t(s.blocks) * (rank + 1) / C);
 
   if (tid == 0) {
+    prefetch_maps(maps);
     abort = 0;
     for (int i = 0; i < s.stages; ++i) {
       mbar_init(&full[i], 1);
@@ -360,10 +423,12 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
     mbar_init(&sums_full, 1);
     fence_barrier_init();
   }
+  griddep_launch_dependents();
   if (warp == 2) tensor_alloc<1>(&tensor_at, s.columns);
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();
+  griddep_wait();
   const uint32_t sums = tensor_at;
 
   if (warp == 0) {
@@ -413,19 +478,39 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
   }
   cluster_sync();  // the stages of every CTA are free
 
+  const int q = warp & 3;
+  const uint32_t mine = sums + (uint32_t(q) << 21);
+  if (!L::kGated && C == 1) {  // nothing to add up or exchange
+    for (int c = 16 * (warp >> 2); c < s.N; c += 32) {
+      uint32_t v[16];
+      float x[16];
+      tensor_load16(mine + c, v);
+      tensor_loaded();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(v[i]);
+      if constexpr (!L::kGated) store_plain<T, kProduct>(j, second, m + 32 * q + lane, n + c, 1, 16, x);
+    }
+    tensor_fence_before();
+    __syncthreads();
+    if (warp == 2) tensor_free<1>(sums, s.columns);
+    return;
+  }
   // partial sums: [source CTA][column of the share][128 rows] in the CTA that stores them
   float* partial = reinterpret_cast<float*>(base);
   const int share = (s.N + C - 1) / C;
-  const int q = warp & 3;
   for (int c = 16 * (warp >> 2); c < s.N; c += 32) {
     uint32_t v[16];
-    tensor_load16(sums + (uint32_t(q) << 21) + c, v);
+    tensor_load16(mine + c, v);
     tensor_loaded();
+    int to = c / share, left = (to + 1) * share - c;
+    uint32_t at = at_rank(partial + (rank * share + c - to * share) * 128 + 32 * q + lane, to);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int to = (c + i) / share, at = (rank * share + (c + i) - to * share) * 128 + 32 * q + lane;
-      if (last > first) store_at(at_rank(partial + at, to), __uint_as_float(v[i]));
-      else store_at(at_rank(partial + at, to), 0.f);
+    for (int i = 0; i < 16; ++i, at += 512) {
+      if (left-- == 0) {
+        left = share - 1;
+        at = at_rank(partial + rank * share * 128 + 32 * q + lane, ++to);
+      }
+      store_at(at, __uint_as_float(v[i]));
     }
   }
   tensor_fence_before();
@@ -437,7 +522,8 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
   const int r = tid & (L::kRows - 1);
   const int64_t row = m + r;
   for (int c = tid / L::kRows; c < count; c += K * kStep) {
-    float v[K], u[K], dh[K];
+    float v[K], u[K];
+    T dh[K];
     if constexpr (kProduct == kInner) load_dh<T>(j, n + from + c, kStep, row, dh);
 #pragma unroll
     for (int i = 0; i < K; ++i) v[i] = u[i] = 0.f;
@@ -450,20 +536,16 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
           if (L::kGated) u[i] += p[i * kStep * 128 + 64];
         }
     }
-    if constexpr (L::kGated) {
-      store_gated<T, kProduct>(j, n + from + c, kStep, row, min(count - c, K * kStep), v, u, dh);
-    } else {
-#pragma unroll
-      for (int i = 0; i < K; ++i) {
-        const int64_t column = n + from + c + i * kStep;
-        if (c + i * kStep < count && row < j.H && column < (kProduct == kDx ? j.T : j.F))
-          store_plain<T, kProduct>(j, second, row, column, v[i]);
-      }
-    }
+    const int most = min(count - c, K * kStep);
+    if constexpr (L::kGated)
+      store_gated<T, kProduct>(j, n + from + c, kStep, row, most, v, u, dh);
+    else
+      store_plain<T, kProduct>(j, second, row, n + from + c, kStep, most, v);
   }
 }
 
 // ---------------------------------------------------------------- host
+
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -505,6 +587,25 @@ bool make_maps(Maps& maps, const FfnJob& j, int n_rows) {
 
 constexpr size_t kSmemMost = 227 * 1024, kSmemFixed = 1024 + 1024;  // alignment; barriers
 
+// The split kernel's shared memory.
+uint32_t columns_of(int N) {
+  uint32_t c = 32;
+  while (c < uint32_t(N)) c *= 2;
+  return c;
+}
+int split_stages(int N, int C, int blocks) {
+  const size_t stage = kABytes + size_t(N) * kDepthBytes;
+  const int most = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemMost - kSmemFixed) / stage));
+  // four blocks on their way: more CTAs an SM do better than more blocks of one
+  return std::min(most, std::min<int>(4, static_cast<int>(ceil_div(blocks, C))));
+}
+size_t split_smem(int N, int C, int blocks) {
+  const size_t sums = size_t(ceil_div(N, C)) * C * 512;
+  // CTAs that share an SM must find room in tensor memory: shared memory allows no more of them than that
+  const size_t room = kSmemMost * columns_of(N) / 512;
+  return 1024 + std::max({sums, room, split_stages(N, C, blocks) * (kABytes + size_t(N) * kDepthBytes)});
+}
+
 template <typename T, int kProduct>
 cudaError_t launch_pairs(const FfnJob& j, Shape s, cudaStream_t stream) {
   Maps maps;
@@ -517,24 +618,27 @@ cudaError_t launch_pairs(const FfnJob& j, Shape s, cudaStream_t stream) {
   if (e != cudaSuccess) return e;
   const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
   const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, sm_count() / 2));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
   count_launch();
-  kernel<<<grid, kPairThreads, smem, stream>>>(maps, j, s);
-  return cudaGetLastError();
+  return cudaLaunchKernelEx(&cfg, kernel, maps, j, s);
 }
 
 template <typename T, int kProduct>
 cudaError_t launch_split(const FfnJob& j, Shape s, int C, cudaStream_t stream) {
   Maps maps;
   if (!make_maps<kProduct>(maps, j, s.N)) return cudaErrorUnknown;
-  const size_t stage = kABytes + size_t(s.N) * kDepthBytes;
-  s.columns = 32;
-  while (s.columns < uint32_t(s.N)) s.columns *= 2;
-  // the sums of both partners of an SM fit tensor memory: shared memory allows no more CTAs than that
-  const size_t sums = size_t(ceil_div(s.N, C)) * C * 512;
-  const size_t least = std::max<size_t>(sums, kSmemMost * s.columns / 512);
-  const int most = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemMost - kSmemFixed) / stage));
-  s.stages = std::min<int>(most, std::max<int>(4, static_cast<int>(ceil_div(s.blocks, C))));
-  size_t smem = 1024 + std::max(least, s.stages * stage);
+  s.columns = columns_of(s.N);
+  s.stages = split_stages(s.N, C, s.blocks);
+  const size_t smem = split_smem(s.N, C, s.blocks);
   const auto kernel = ffn_split_kernel<T, kProduct>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
@@ -545,41 +649,78 @@ cudaError_t launch_split(const FfnJob& j, Shape s, int C, cudaStream_t stream) {
   cfg.blockDim = dim3(kSplitThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   count_launch();
   return cudaLaunchKernelEx(&cfg, kernel, maps, j, s);
+}
+
+// How a product is cut.  The candidates' times are estimated, in microseconds, from
+// what was measured: an SM takes 48 bytes a clock from L2, a launch with its first
+// copies and its last sums costs 5 us, a tile's stores what `stores` says.
+struct Choice {
+  bool pairs;
+  int N, n_tiles, C;
+  double us;
+};
+double block_us(int rows_n) { return (kABytes + double(rows_n) * kDepthBytes) / 91200.0; }
+
+template <int kProduct>
+Choice choose(int64_t M, int64_t Nall, int blocks, int64_t bytes) {
+  using L = Layout<kProduct>;
+  const int two = kProduct == kDw ? 2 : 1, sms = sm_count();
+  const auto stores = [](int N) { return kProduct == kInner ? 1.2 + 0.012 * N : 0.8 + 0.006 * N; };
+  const double least = double(bytes) / 6.5e6;
+  const int64_t few = ceil_div(Nall, 256), most = std::min<int64_t>(ceil_div(Nall, 32), few + 8);
+  Choice best = {};
+  best.us = 1e30;
+  for (int64_t nt = few; nt <= most; ++nt) {
+    const auto width = [&](int granule) { return static_cast<int>(ceil_div(ceil_div(Nall, nt), granule) * granule); };
+    {
+      const int N = width(kProduct == kDw ? 128 : 32);
+      const int64_t n_tiles = ceil_div(Nall, N), tiles = ceil_div(M, 2 * L::kRows) * n_tiles * two;
+      const double rounds = double(ceil_div(tiles, sms / 2));
+      const double us = 5.5 + std::max(least, rounds * std::max(blocks * block_us(N / 2), stores(N))) + stores(N);
+      if (us < best.us) best = {true, N, static_cast<int>(n_tiles), 1, us};
+    }
+    const int N = width(kProduct == kDw ? 64 : 16);
+    const int64_t n_tiles = ceil_div(Nall, N), tiles = ceil_div(M, L::kRows) * n_tiles * two;
+    for (int C = 1; C <= 8 && (C == 1 || blocks >= 2 * C); C *= 2) {
+      const int per_sm = std::max<int>(1, static_cast<int>(kSmemMost / (split_smem(N, C, blocks) + 2048)));
+      // clusters of four and eight do not fill every group of SMs
+      const double slots = per_sm * (C == 8 ? 120 : C == 4 ? 144 : sms), ctas = double(tiles * C);
+      const double at_once = std::min<double>(per_sm, std::ceil(ctas / sms));
+      const double sum = double(ceil_div(blocks, C)) * block_us(N) * at_once;
+      // bytes on their way: 2.3 us of them make the rate of memory
+      const double way = std::min(ctas, slots) * split_stages(N, C, blocks) * (kABytes + double(N) * kDepthBytes);
+      const double reads = std::max(least, double(bytes) / (way / 2.3));
+      const double us = 4.5 + std::max(reads, std::ceil(ctas / slots) * (sum + 1.0 + (C > 1 ? 0.015 : 0.008) * N));
+      if (us < best.us) best = {false, N, static_cast<int>(n_tiles), C, us};
+    }
+  }
+  return best;
 }
 
 template <typename T, int kProduct>
 cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
   using L = Layout<kProduct>;
-  const int64_t M = L::kGated ? j.F : j.H, Nall = kProduct == kDw ? j.F : j.T, two = kProduct == kDw ? 2 : 1;
-  Shape s = {};
+  const int64_t M = L::kGated ? j.F : j.H, Nall = kProduct == kDw ? j.F : j.T;
   const int64_t k = kProduct == kDx ? j.F : kProduct == kDw ? j.T : j.H;
+  Shape s = {};
   s.half = static_cast<int>(ceil_div(k, kBox));
   s.blocks = kProduct == kDx ? 2 * s.half : s.half;
-  const int granule = kProduct == kDw ? 128 : 32;  // of a pair's N
-  const int64_t n_tiles = ceil_div(Nall, 256);
-  const int64_t pair_tiles = ceil_div(M, 2 * L::kRows) * n_tiles * two;
-  if (pair_tiles >= sm_count() / 2) {
-    s.m_tiles = ceil_div(M, 2 * L::kRows);
-    s.n_tiles = n_tiles;
-    s.N = static_cast<int>(ceil_div(ceil_div(Nall, n_tiles), granule) * granule);
-    return launch_pairs<T, kProduct>(j, s, stream);
-  }
-  s.m_tiles = ceil_div(M, L::kRows);
-  const int fine = kProduct == kDw ? 64 : 16;
-  s.n_tiles = n_tiles;
-  s.N = static_cast<int>(ceil_div(ceil_div(Nall, n_tiles), fine) * fine);
-  const int64_t tiles = s.m_tiles * s.n_tiles * two;
-  int C = 1;
-  while (C < 8 && tiles * C * 2 <= 2 * sm_count() && s.blocks >= C * 4) C *= 2;
-  return launch_split<T, kProduct>(j, s, C, stream);
+  const int64_t bytes = 2 * (j.T * j.H + 2 * j.F * j.H + (kProduct == kForward ? 1 : 2) * j.T * j.F);
+  const Choice c = choose<kProduct>(M, Nall, s.blocks, bytes);
+  s.N = c.N;
+  s.n_tiles = c.n_tiles;
+  s.m_tiles = ceil_div(M, c.pairs ? 2 * L::kRows : L::kRows);
+  return c.pairs ? launch_pairs<T, kProduct>(j, s, stream) : launch_split<T, kProduct>(j, s, c.C, stream);
 }
 
 template <typename T>

@@ -114,8 +114,10 @@ __device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map
         : "memory");
 }
 
+// Relaxed: what it orders is reads of tensor memory that have completed.  A release
+// would also wait for the warp's stores to global memory.
 __device__ __forceinline__ void arrive_at(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void store_at(uint32_t at, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
