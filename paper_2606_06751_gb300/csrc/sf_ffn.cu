@@ -1,203 +1,22 @@
 // sf_ffn.cu - the gated feed-forward product h = act(x Wg^T) * (x Wu^T) and its
-// gradient (sf_gated_ffn, sf_gated_ffn_grad): what the call launches, and f32 on
-// the f32 units (bf16 and f16: sf_ffn_tensor.cu).
-//
-// Four products of one shape, rows x columns summed over k, by tiles of 128 x 128
-// in registers:
-//   forward   tokens x features over H; a tile's columns are 64 features of Wg
-//             and the same 64 of Wu, so that a thread holds both factors of a
-//             value of h
-//   inner     the same, turned into dg = dh u act'(g) and du = dh act(g)
-//   dx        tokens x H over the features of dg with Wg, then of du with Wu
-//   dW        features of dg, then of du, x H over the tokens
-// Bound by the multiply-adds: 128 an SM and clock.
+// gradient (sf_gated_ffn, sf_gated_ffn_grad): which form a call takes, and the copy of
+// rows that tensor copies cannot read.
+//   bf16, f16          the tensor cores (sf_ffn_tensor.cu); rows that do not start
+//                      on 16 bytes are copied first, but for a few tokens
+//   f32                the tensor cores by parts (sf_ffn_parts.cu), but for a few
+//                      tokens' product
+//   a few tokens       one read of the weights on the f32 units (sf_ffn_few.cu)
 #include <algorithm>
 
-#include "sf_ffn_math.cuh"
+#include "sf_float.cuh"
 #include "sf_ffn_tensor.h"
 
 namespace sf {
 namespace {
 
-constexpr int kThreads = 256, kTile = 128, kDepth = 16, kHalf = kTile / 2, kRun = 128;
-enum Product { kForward, kInner, kDx, kDw };
+constexpr int kThreads = 256;
 
-// Eight values along a row from p, `left` of which exist.
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int64_t left, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < left ? to_f32(p[i]) : 0.f;
-}
-
-template <typename T, int kProduct, int kAct>
-__global__ void __launch_bounds__(kThreads) ffn_tile_kernel(const FfnJob j) {
-  constexpr bool kGated = kProduct == kForward || kProduct == kInner;
-  __shared__ float sa[2][kDepth][kTile + 4], sb[2][kDepth][kTile + 4];
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const T *x = static_cast<const T*>(j.x), *wg = static_cast<const T*>(j.w_gate), *wu = static_cast<const T*>(j.w_up);
-  T *dg = static_cast<T*>(j.dg), *du = static_cast<T*>(j.du);
-  const int64_t feature_tiles = (j.F + kTile - 1) / kTile;
-  // the tile's first row and column; dW: which of the two matrices
-  const bool second = kProduct == kDw && blockIdx.x >= feature_tiles;
-  const int64_t r0 = (int64_t(blockIdx.x) - (second ? feature_tiles : 0)) * kTile;
-  const int64_t c0 = (int64_t(blockIdx.z) * 65535 + blockIdx.y) * (kGated ? kHalf : kTile);
-  const int64_t rows = kProduct == kDw ? j.F : j.T, columns = kGated ? j.F : j.H;
-  if (c0 >= columns) return;
-  const int64_t per = kProduct == kDx ? j.F : kProduct == kDw ? j.T : j.H;  // the sum's length, for dx of each half
-  const int64_t steps = (per + kDepth - 1) / kDepth, all = kProduct == kDx ? 2 * steps : steps;
-
-  // the thread's eight values of each operand: along k of one row, or along the rows of one k
-  const int lr = tid >> 1, lk = (tid & 1) * 8, tr = (tid & 15) * 8, tk = tid >> 4;
-  float a[8], b[8];
-  auto fetch = [&](int64_t step) {
-    const bool up = kProduct == kDx && step >= steps;
-    const int64_t k = (up ? step - steps : step) * kDepth;
-    if constexpr (kProduct == kDw) {
-      const int64_t t = k + tk;
-      const T* g = second ? du : dg;
-      load8(g + t * j.ldg + r0 + tr, t < per ? rows - r0 - tr : 0, a);
-      load8(x + t * j.ldx + c0 + tr, t < per ? columns - c0 - tr : 0, b);
-    } else {
-      const int64_t r = r0 + lr;
-      const T* p = kProduct == kDx ? (up ? du : dg) + r * j.ldg : x + r * j.ldx;
-      load8(p + k + lk, r < rows ? per - k - lk : 0, a);
-      if constexpr (kProduct == kDx) {
-        const int64_t f = k + tk;
-        load8((up ? wu : wg) + f * j.ldw + c0 + tr, f < per ? columns - c0 - tr : 0, b);
-      } else {
-        const int64_t f = c0 + (lr & (kHalf - 1));
-        load8((lr < kHalf ? wg : wu) + f * j.ldw + k + lk, f < columns ? per - k - lk : 0, b);
-      }
-    }
-  };
-  auto stage = [&](int s) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (kProduct == kDw)
-        sa[s][tk][tr + i] = a[i];
-      else
-        sa[s][lk + i][lr] = a[i];
-      if (kGated)
-        sb[s][lk + i][lr] = b[i];
-      else
-        sb[s][tk][tr + i] = b[i];
-    }
-  };
-
-  // a run of kRun products is summed by itself and then added: the roundings of one long
-  // chain are twice the error of a sum in pieces
-  float sum[8][8], run[8][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int q = 0; q < 8; ++q) sum[i][q] = run[i][q] = 0.f;
-  fetch(0);
-  stage(0);
-  __syncthreads();
-  for (int64_t step = 0; step < all; ++step) {
-    const int s = static_cast<int>(step & 1);
-    if (step + 1 < all) fetch(step + 1);
-#pragma unroll
-    for (int k = 0; k < kDepth; ++k) {
-      float u[8], v[8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        *reinterpret_cast<float4*>(u + 4 * h) = *reinterpret_cast<const float4*>(&sa[s][k][kHalf * h + 4 * ty]);
-        *reinterpret_cast<float4*>(v + 4 * h) = *reinterpret_cast<const float4*>(&sb[s][k][kHalf * h + 4 * tx]);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int q = 0; q < 8; ++q) run[i][q] = fmaf(u[i], v[q], run[i][q]);
-    }
-    if ((step & (kRun / kDepth - 1)) == kRun / kDepth - 1 || step + 1 == all) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          sum[i][q] += run[i][q];
-          run[i][q] = 0.f;
-        }
-    }
-    if (step + 1 < all) stage(s ^ 1);
-    __syncthreads();
-  }
-
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t r = r0 + kHalf * (i >> 2) + 4 * ty + (i & 3);
-    if (r >= rows) continue;
-    if constexpr (kGated) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {  // columns q of both halves are one feature's g and u
-        const int64_t f = c0 + 4 * tx + q;
-        if (f >= columns) continue;
-        const float g = sum[i][q], u = sum[i][q + 4];
-        using A = Activation<kAct, sizeof(T) == 2>;
-        if constexpr (kProduct == kForward) {
-          static_cast<T*>(j.h)[r * j.ldh + f] = from_f32<T>(A::value(g) * u);
-        } else {
-          float act, slope;
-          A::both(g, act, slope);
-          const float d = to_f32(static_cast<const T*>(j.dh)[r * j.lddh + f]);
-          if (j.h != nullptr) static_cast<T*>(j.h)[r * j.ldh + f] = from_f32<T>(act * u);
-          dg[r * j.ldg + f] = from_f32<T>(d * u * slope);
-          du[r * j.ldg + f] = from_f32<T>(d * act);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int64_t c = c0 + kHalf * (q >> 2) + 4 * tx + (q & 3);
-        if (c >= columns) continue;
-        float v = sum[i][q];
-        if (kProduct == kDx) {
-          static_cast<T*>(j.dx)[r * j.lddx + c] = from_f32<T>(v);
-        } else if (j.dw_dtype == SF_F32) {
-          float* p = static_cast<float*>(second ? j.dw_up : j.dw_gate) + r * j.lddw + c;
-          *p = j.accumulate ? *p + v : v;
-        } else {
-          T* p = static_cast<T*>(second ? j.dw_up : j.dw_gate) + r * j.lddw + c;
-          *p = from_f32<T>(j.accumulate ? to_f32(*p) + v : v);
-        }
-      }
-    }
-  }
-}
-
-// Rows of nothing, for weights without tokens.
-__global__ void __launch_bounds__(kThreads) ffn_clear_kernel(char* gate, char* up, int64_t rows, int64_t bytes,
-                                                             int64_t pitch) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (int64_t i = threadIdx.x * int64_t(2); i < bytes; i += kThreads * 2) {
-      *reinterpret_cast<unsigned short*>(gate + r * pitch + i) = 0;
-      *reinterpret_cast<unsigned short*>(up + r * pitch + i) = 0;
-    }
-}
-
-template <typename T, int kProduct>
-cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
-  constexpr bool kGated = kProduct == kForward || kProduct == kInner;
-  const int64_t row_tiles = kProduct == kDw ? 2 * ((j.F + kTile - 1) / kTile) : (j.T + kTile - 1) / kTile;
-  const int64_t columns = kGated ? (j.F + kHalf - 1) / kHalf : (j.H + kTile - 1) / kTile;
-  const dim3 grid(static_cast<unsigned>(row_tiles), static_cast<unsigned>(std::min<int64_t>(columns, 65535)),
-                  static_cast<unsigned>((columns + 65534) / 65535));
-  count_launch();
-  if constexpr (kGated)
-    with_activation(j.act, [&](auto act) { ffn_tile_kernel<T, kProduct, act.value><<<grid, kThreads, 0, stream>>>(j); });
-  else
-    ffn_tile_kernel<T, kProduct, 0><<<grid, kThreads, 0, stream>>>(j);
-  return cudaGetLastError();
-}
-
-template <typename T>
-cudaError_t launch_type(const FfnJob& j, bool grad, cudaStream_t stream) {
-  if (!grad) return launch_product<T, kForward>(j, stream);
-  cudaError_t e = launch_product<T, kInner>(j, stream);
-  if (e == cudaSuccess && j.dx != nullptr) e = launch_product<T, kDx>(j, stream);
-  if (e == cudaSuccess && j.dw_gate != nullptr) e = launch_product<T, kDw>(j, stream);
-  return e;
-}
+// ---------------------------------------------------------------- rows for tensor copies
 
 // Rows of 16-bit values that start anywhere, copied to rows that start on 16 bytes.
 struct Spread {
@@ -248,8 +67,34 @@ __global__ void __launch_bounds__(kThreads) ffn_spread_kernel(const __grid_const
   }
 }
 
+// ---------------------------------------------------------------- host
+
+// Rows of nothing, for weights without tokens.
+__global__ void __launch_bounds__(kThreads) ffn_clear_kernel(char* gate, char* up, int64_t rows, int64_t bytes,
+                                                             int64_t pitch) {
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int64_t i = threadIdx.x * int64_t(2); i < bytes; i += kThreads * 2) {
+      *reinterpret_cast<unsigned short*>(gate + r * pitch + i) = 0;
+      *reinterpret_cast<unsigned short*>(up + r * pitch + i) = 0;
+    }
+}
+
 size_t value_size(int32_t dtype) { return dtype == SF_F32 ? 4 : 2; }
 size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
+
+// Whether a call takes the form for a few tokens.  Products, us here against the tensor cores:
+//   f32          16 tokens through 2048 x 4096  32 / 57, 8 through 4096 x 12288  88 / 296, 64 through
+//                1024 x 4096  60 / 29; gradients have this form up to 8 tokens
+//   16 bits      one token through 4096 x 12288  33.8 / 35.2, two 37.0 / 34.7; through 1024 x 2048
+//                one 3.7 / 5.4, four 4.4 / 5.4
+//   uneven rows  one token through 4097 x 12288  55 / 131 (with the copy of the weights), two 90 / 132,
+//                four 304 / 132
+bool few_tokens(int32_t dtype, int64_t T, int64_t H, int64_t F, bool aligned, bool grad) {
+  if (F > kFewMostFeatures) return false;
+  if (dtype == SF_F32) return T <= (grad ? kFewGradTokens : 32);
+  if (grad) return false;
+  return aligned ? T == 1 || (T <= 4 && F * H <= int64_t(1) << 22) : T <= 2;
+}
 
 }  // namespace
 
@@ -258,8 +103,10 @@ bool ffn_rows_on16(const void* p, int64_t ld, int32_t dtype) {
 }
 
 size_t ffn_workspace(int32_t dtype, int64_t T, int64_t H, int64_t F, bool aligned, bool grad) {
-  const size_t inner = grad ? 2 * size_t(T) * round16(size_t(F) * value_size(dtype)) : 0;
-  return inner + (dtype == SF_F32 || aligned ? 0 : size_t(T + 2 * F) * round16(size_t(H) * 2));
+  if (few_tokens(dtype, T, H, F, aligned, grad)) return grad ? ffn_few_workspace(T, H, F) : 0;
+  if (dtype == SF_F32) return ffn_parts_workspace(T, H, F, grad);
+  const size_t inner = grad ? 2 * size_t(T) * round16(size_t(F) * 2) : 0;
+  return inner + (aligned ? 0 : size_t(T + 2 * F) * round16(size_t(H) * 2));
 }
 
 cudaError_t launch_ffn(FfnJob j, bool grad, void* workspace, cudaStream_t stream) {
@@ -271,17 +118,21 @@ cudaError_t launch_ffn(FfnJob j, bool grad, void* workspace, cudaStream_t stream
         static_cast<char*>(j.dw_gate), static_cast<char*>(j.dw_up), j.F, j.H * size, j.lddw * size);
     return cudaGetLastError();
   }
-  const size_t size = value_size(j.dtype), row = round16(size_t(j.F) * size);
+  const bool even = ffn_rows_on16(j.x, j.T > 1 ? j.ldx : 0, j.dtype) &&
+                    ffn_rows_on16(j.w_gate, j.F > 1 ? j.ldw : 0, j.dtype) &&
+                    ffn_rows_on16(j.w_up, j.F > 1 ? j.ldw : 0, j.dtype);
+  if (few_tokens(j.dtype, j.T, j.H, j.F, even, grad))
+    return grad ? launch_ffn_few_grad(j, workspace, stream) : launch_ffn_few(j, even, stream);
+  if (j.dtype == SF_F32) return launch_ffn_parts(j, grad, workspace, stream);
   char* at = static_cast<char*>(workspace);
   if (grad) {
+    const size_t row = round16(size_t(j.F) * 2);
     j.dg = at;
     j.du = at + size_t(j.T) * row;
-    j.ldg = int64_t(row / size);
+    j.ldg = int64_t(row / 2);
     at += 2 * size_t(j.T) * row;
   }
-  if (j.dtype == SF_F32) return launch_type<float>(j, grad, stream);
-  if (!ffn_rows_on16(j.x, j.T > 1 ? j.ldx : 0, j.dtype) || !ffn_rows_on16(j.w_gate, j.F > 1 ? j.ldw : 0, j.dtype) ||
-      !ffn_rows_on16(j.w_up, j.F > 1 ? j.ldw : 0, j.dtype)) {
+  if (!even) {
     const int64_t packs = int64_t(round16(size_t(j.H) * 2) / 16);
     Spread s;
     const void** data[3] = {&j.x, &j.w_gate, &j.w_up};

@@ -2,8 +2,6 @@
 // their derivatives, in 32 bits.
 #pragma once
 
-#include <type_traits>
-
 #include "sf_float.cuh"
 
 namespace sf {
@@ -70,16 +68,5 @@ struct Activation<SF_ACT_RELU, kFast> {
     slope = g > 0.f ? 1.f : 0.f;
   }
 };
-
-// Calls f with the activation's number as a constant.
-template <typename F>
-auto with_activation(int32_t act, F&& f) {
-  switch (act) {
-    case SF_ACT_GELU: return f(std::integral_constant<int, SF_ACT_GELU>());
-    case SF_ACT_GELU_TANH: return f(std::integral_constant<int, SF_ACT_GELU_TANH>());
-    case SF_ACT_RELU: return f(std::integral_constant<int, SF_ACT_RELU>());
-    default: return f(std::integral_constant<int, SF_ACT_SILU>());
-  }
-}
 
 }  // namespace sf

@@ -11,16 +11,12 @@
 // tensor cores take them as they are.
 #include <algorithm>
 
-#include "sf_ffn_math.cuh"
 #include "sf_ffn_tensor.h"
-#include "sf_tcgen05.cuh"
+#include "sf_ffn_tiles.cuh"
 
 namespace sf {
 namespace {
 
-enum Product { kForward, kInner, kDx, kDw };
-
-constexpr uint32_t kABytes = 128 * kDepthBytes;
 constexpr int kMaxStages = 12;
 
 struct Shape {
@@ -33,13 +29,6 @@ struct Shape {
 
 struct Maps {
   CUtensorMap a0, a1, b0, b1;
-};
-
-template <int kProduct>
-struct Layout {
-  static constexpr bool kGated = kProduct == kForward || kProduct == kInner;
-  static constexpr bool kAAlongK = kGated, kBAlongK = kProduct != kDw;
-  static constexpr int kRows = kGated ? 64 : 128;  // of what is stored, in a CTA's 128 rows of D
 };
 
 __device__ __forceinline__ void prefetch_maps(const Maps& maps) {
@@ -82,102 +71,6 @@ __device__ __forceinline__ void multiply_block(uint32_t d, uint32_t a, uint32_t 
   for (int k = 0; k < kBox / 16; ++k)
     tensor_product<kCtas>(d, operand_of<L::kAAlongK>(a + k * kStepBytes<L::kAAlongK>),
                           operand_of<L::kBAlongK>(b + k * kStepBytes<L::kBAlongK>), desc, !(first && k == 0));
-}
-
-// K values to addresses `ld` apart: those of rows i * step < left.
-template <typename T, int K>
-__device__ __forceinline__ void store_down(T* p, int64_t ld, int step, int left, const T (&v)[K]) {
-  if ((K - 1) * step < left) {
-#pragma unroll
-    for (int i = 0; i < K; ++i, p += ld) *p = v[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < K; ++i, p += ld)
-      if (i * step < left) *p = v[i];
-  }
-}
-
-// K values of h, or of dg and du (and h), from their g and u: feature f of tokens
-// t, t + step, ... before t + most and T.  One basic block, so that the K chains of exponential and quotient overlap.
-template <typename T, int kProduct, int kAct, int K>
-__device__ __forceinline__ void store_act(const FfnJob& j, int64_t t, int step, int64_t f, int most, const float (&g)[K],
-                                          const float (&u)[K], const T (&dh)[K]) {
-  using A = Activation<kAct, true>;
-  T v[K], w[K], x[K];
-#pragma unroll
-  for (int i = 0; i < K; ++i) {
-    if constexpr (kProduct == kForward) {
-      v[i] = from_f32<T>(A::value(g[i]) * u[i]);
-    } else {
-      float a, slope;
-      A::both(g[i], a, slope);
-      v[i] = from_f32<T>(a * u[i]);
-      const float d = to_f32(dh[i]);
-      w[i] = from_f32<T>(d * u[i] * slope);
-      x[i] = from_f32<T>(d * a);
-    }
-  }
-  const int left = static_cast<int>(min(int64_t(most), j.T - t));
-  if (kProduct == kForward || j.h != nullptr) store_down(static_cast<T*>(j.h) + t * j.ldh + f, step * j.ldh, step, left, v);
-  if constexpr (kProduct == kInner) {
-    store_down(static_cast<T*>(j.dg) + t * j.ldg + f, step * j.ldg, step, left, w);
-    store_down(static_cast<T*>(j.du) + t * j.ldg + f, step * j.ldg, step, left, x);
-  }
-}
-template <typename T, int kProduct, int K>
-__device__ __forceinline__ void store_gated(const FfnJob& j, int64_t t, int step, int64_t f, int most, const float (&g)[K],
-                                            const float (&u)[K], const T (&dh)[K]) {
-  if (f >= j.F || t >= j.T) return;
-  switch (j.act) {
-    case SF_ACT_GELU: return store_act<T, kProduct, SF_ACT_GELU>(j, t, step, f, most, g, u, dh);
-    case SF_ACT_GELU_TANH: return store_act<T, kProduct, SF_ACT_GELU_TANH>(j, t, step, f, most, g, u, dh);
-    case SF_ACT_RELU: return store_act<T, kProduct, SF_ACT_RELU>(j, t, step, f, most, g, u, dh);
-    default: return store_act<T, kProduct, SF_ACT_SILU>(j, t, step, f, most, g, u, dh);
-  }
-}
-__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-
-// Their upstream gradients, as they are: a conversion would wait for them.
-template <typename T, int K>
-__device__ __forceinline__ void load_dh(const FfnJob& j, int64_t t, int step, int64_t f, T (&dh)[K]) {
-  const T* p = static_cast<const T*>(j.dh) + t * j.lddh + f;
-  const int left = f < j.F && t < j.T ? static_cast<int>(min(int64_t(K) * step, j.T - t)) : 0;
-#pragma unroll
-  for (int i = 0; i < K; ++i, p += step * j.lddh) dh[i] = i * step < left ? *p : from_f32<T>(0.f);
-}
-
-// K values of dx or of a weight's gradient: column m of rows n, n + step, ... before n + most and the last.
-template <typename T, int kProduct, int K>
-__device__ __forceinline__ void store_plain(const FfnJob& j, bool second, int64_t m, int64_t n, int step, int most,
-                                            const float (&v)[K]) {
-  const int64_t rows = kProduct == kDx ? j.T : j.F;
-  if (m >= j.H || n >= rows) return;
-  const int left = static_cast<int>(min(int64_t(most), rows - n));
-  void* w = kProduct == kDx ? j.dx : second ? j.dw_up : j.dw_gate;
-  const int64_t ld = kProduct == kDx ? j.lddx : j.lddw;
-  if (kProduct == kDw && j.dw_dtype == SF_F32) {
-    float* p = static_cast<float*>(w) + n * ld + m;
-    float x[K];
-#pragma unroll
-    for (int i = 0; i < K; ++i) x[i] = v[i];
-    if (j.accumulate) {
-#pragma unroll
-      for (int i = 0; i < K; ++i)
-        if (i * step < left) x[i] += p[i * step * ld];
-    }
-    store_down(p, step * ld, step, left, x);
-  } else {
-    T* p = static_cast<T*>(w) + n * ld + m;
-    T x[K];
-#pragma unroll
-    for (int i = 0; i < K; ++i) x[i] = from_f32<T>(v[i]);
-    if (kProduct == kDw && j.accumulate) {
-#pragma unroll
-      for (int i = 0; i < K; ++i)
-        if (i * step < left) x[i] = from_f32<T>(to_f32(p[i * step * ld]) + v[i]);
-    }
-    store_down(p, step * ld, step, left, x);
-  }
 }
 
 // ---------------------------------------------------------------- large products: a pair of SMs a tile
@@ -225,19 +118,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
   griddep_wait();
   const uint32_t sums = tensor_at;
 
-  // a tile's first m and n of the pair; n tiles in groups of 8 m tiles, whose operands stay in L2
-  const auto tile_of = [&](int64_t tile, int64_t& m, int64_t& n, bool& second) {
-    const int64_t all = s.n_tiles * (kProduct == kDw ? 2 : 1);
-    const int64_t group = tile / (8 * all), first = group * 8;
-    const int64_t in_group = s.m_tiles - first < 8 ? s.m_tiles - first : 8;
-    const int64_t at = tile - group * 8 * all;
-    m = (first + at % in_group) * (2 * L::kRows);
-    n = at / in_group;
-    second = kProduct == kDw && n >= s.n_tiles;
-    if (second) n -= s.n_tiles;
-    n *= s.N;
-  };
-
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0;
@@ -246,7 +126,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += pairs) {
         int64_t m, n;
         bool second;
-        tile_of(tile, m, n, second);
+        tile_of<kProduct>(tile, s.m_tiles, s.n_tiles, s.N, m, n, second);
         for (int kb = 0; kb < s.blocks; ++kb) {
           ok = mbar_wait_bounded(&empty[stage], parity, &abort);
           if (!ok) break;
@@ -294,7 +174,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       if (tile >= tiles) return;
       int64_t m, n;
       bool second;
-      tile_of(tile, m, n, second);
+      tile_of<kProduct>(tile, s.m_tiles, s.n_tiles, s.N, m, n, second);
       m += rank * L::kRows;
       if (m >= j.F) return;
       for (int64_t t = n + lane; t < n + s.N && t < j.T; t += 32) {
@@ -318,7 +198,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     for (int64_t tile = blockIdx.x / 2; tile < tiles; tile += pairs, ++done) {
       int64_t m, n;
       bool second;
-      tile_of(tile, m, n, second);
+      tile_of<kProduct>(tile, s.m_tiles, s.n_tiles, s.N, m, n, second);
       m += rank * L::kRows;
       const int buf = static_cast<int>(done & 1);
       T dh_next[8];
@@ -546,8 +426,6 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
 
 // ---------------------------------------------------------------- host
 
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // A matrix of `rows` rows of `len` values, `ld` apart, read in boxes of 64 x `box_rows`, 128-byte swizzle; what lies
 // outside is 0.

@@ -171,8 +171,8 @@ def test_spacing_and_surroundings(sf, T, pad, offset, dtype):
     within(first, ref["h"], "h")
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("T", [5, 600])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [1, 5, 600])
 def test_accumulate_and_f32_weights(sf, T, dtype):
     H, F = 320, 264
     x, wg, wu, dh = inputs(T, H, F, dtype, 21, grad=True)
@@ -225,7 +225,7 @@ def test_differences(sf, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("T", [3, 40, 400])
+@pytest.mark.parametrize("T", [3, 8, 40, 400])
 def test_infinite_and_nan_tokens(sf, T, dtype):
     """A token's NaN or infinity goes to its own rows and to the weights' gradients, nowhere else."""
     x, wg, wu, dh = inputs(T, 96, 130, dtype, 41, grad=True)
@@ -241,6 +241,9 @@ def test_infinite_and_nan_tokens(sf, T, dtype):
     x[1, 5] = float("inf")
     h = sf.sf_gated_ffn(x, wg, wu, act="relu")
     g, u = wg[:, 5].double(), wu[:, 5].double()
+    if dtype == "f32" and T > 32:  # products by parts: an infinity meets parts that are 0
+        assert not bool(h[1].isfinite().any()) and bool(h[keep].isfinite().all())
+        return
     assert bool((h[1][(g > 0) & (u > 0)] == float("inf")).all())
     assert bool((h[1][(g > 0) & (u < 0)] == float("-inf")).all())
 
