@@ -152,7 +152,7 @@ cudaError_t launch_few(const FfnJob& j, bool even, cudaStream_t stream) {
 // ---------------------------------------------------------------- the gradient, f32
 
 constexpr int kColumns = 4, kBlock = kThreads * kColumns;  // of a thread, of a CTA
-constexpr int kSlab = 128;                                   // features of a CTA
+constexpr int kSlab = 128;                                   // features of a CTA, at most
 
 // A thread's columns: four side by side (kEven), or every 256th.
 template <bool kEven>
@@ -181,11 +181,11 @@ __device__ __forceinline__ void store_columns(float* row, int64_t c0, int64_t H,
 
 // The slab's dg and du, [feature][token].
 template <int kTokens>
-__device__ __forceinline__ void load_slab(const FfnJob& j, int64_t f0, float (&dg)[kSlab][kTokens],
+__device__ __forceinline__ void load_slab(const FfnJob& j, int64_t f0, int n, float (&dg)[kSlab][kTokens],
                                           float (&du)[kSlab][kTokens]) {
   for (int i = threadIdx.x; i < kSlab * kTokens; i += kThreads) {
     const int f = i % kSlab, t = i / kSlab;
-    const bool in = f0 + f < j.F && t < j.T;
+    const bool in = f < n && t < j.T;
     dg[f][t] = in ? static_cast<const float*>(j.dg)[t * j.ldg + f0 + f] : 0.f;
     du[f][t] = in ? static_cast<const float*>(j.du)[t * j.ldg + f0 + f] : 0.f;
   }
@@ -202,11 +202,11 @@ __device__ __forceinline__ void store_part(float* row, int64_t c0, int64_t H, co
 
 // A slab's part of dx, [slab][T][H]: the weights' rows go by once.
 template <int kTokens, bool kEven>
-__global__ void __launch_bounds__(kThreads) ffn_few_dx_kernel(const FfnJob j, float* parts) {
+__global__ void __launch_bounds__(kThreads) ffn_few_dx_kernel(const FfnJob j, float* parts, int slab) {
   __shared__ __align__(16) float dg[kSlab][kTokens], du[kSlab][kTokens];
-  const int64_t f0 = int64_t(blockIdx.y) * kSlab, c0 = int64_t(blockIdx.x) * kBlock;
-  load_slab<kTokens>(j, f0, dg, du);
-  const int n = static_cast<int>(min(int64_t(kSlab), j.F - f0));
+  const int64_t f0 = int64_t(blockIdx.y) * slab, c0 = int64_t(blockIdx.x) * kBlock;
+  const int n = static_cast<int>(min(int64_t(slab), j.F - f0));
+  load_slab<kTokens>(j, f0, n, dg, du);
   const float *wg = static_cast<const float*>(j.w_gate) + f0 * j.ldw, *wu = static_cast<const float*>(j.w_up) + f0 * j.ldw;
   float sum[kTokens][kColumns] = {};
 #pragma unroll 4
@@ -238,15 +238,15 @@ __global__ void __launch_bounds__(kThreads) ffn_few_sum_kernel(const FfnJob j, c
 
 // A slab's rows of both weights' gradients; the tokens stay in registers.
 template <int kTokens, bool kEven>
-__global__ void __launch_bounds__(kThreads) ffn_few_dw_kernel(const FfnJob j) {
+__global__ void __launch_bounds__(kThreads) ffn_few_dw_kernel(const FfnJob j, int slab) {
   __shared__ __align__(16) float dg[kSlab][kTokens], du[kSlab][kTokens];
-  const int64_t f0 = int64_t(blockIdx.y) * kSlab, c0 = int64_t(blockIdx.x) * kBlock;
-  load_slab<kTokens>(j, f0, dg, du);
+  const int64_t f0 = int64_t(blockIdx.y) * slab, c0 = int64_t(blockIdx.x) * kBlock;
+  const int n = static_cast<int>(min(int64_t(slab), j.F - f0));
+  load_slab<kTokens>(j, f0, n, dg, du);
   float x[kTokens][kColumns];
 #pragma unroll
   for (int t = 0; t < kTokens; ++t)
     load_columns<kEven>(static_cast<const float*>(j.x) + min(int64_t(t), j.T - 1) * j.ldx, c0, j.H, x[t]);
-  const int n = static_cast<int>(min(int64_t(kSlab), j.F - f0));
   float *og = static_cast<float*>(j.dw_gate) + f0 * j.lddw, *ou = static_cast<float*>(j.dw_up) + f0 * j.lddw;
 #pragma unroll 2
   for (int f = 0; f < n; ++f) {
@@ -275,7 +275,12 @@ __global__ void __launch_bounds__(kThreads) ffn_few_dw_kernel(const FfnJob j) {
   }
 }
 
-int64_t slabs_of(int64_t F) { return (F + kSlab - 1) / kSlab; }
+// Features of a CTA: so many that two CTAs an SM have some, for a short sum over slabs.
+int slab_of(int64_t H, int64_t F) {
+  int slab = kSlab;
+  while (slab > 16 && (F + slab - 1) / slab * ((H + kBlock - 1) / kBlock) < int64_t(2) * sm_count()) slab /= 2;
+  return slab;
+}
 int64_t padded(int64_t F) { return (F + 3) / 4 * 4; }
 
 template <int kTokens>
@@ -283,14 +288,15 @@ cudaError_t launch_grad(const FfnJob& j, float* parts, cudaStream_t stream) {
   const auto even = [](const void* p, int64_t rows, int64_t ld) { return ffn_rows_on16(p, rows > 1 ? ld : 0, SF_F32); };
   const bool weights = even(j.w_gate, j.F, j.ldw) && even(j.w_up, j.F, j.ldw), tokens = even(j.x, j.T, j.ldx);
   cudaError_t e = launch_rows<float, kTokens, true>(j, weights && tokens, stream);
-  const int64_t slabs = slabs_of(j.F);
+  const int slab = slab_of(j.H, j.F);
+  const int64_t slabs = (j.F + slab - 1) / slab;
   const dim3 grid(static_cast<unsigned>((j.H + kBlock - 1) / kBlock), static_cast<unsigned>(slabs));
   if (e == cudaSuccess && j.dx != nullptr) {
     count_launch(2);
     if (weights)
-      ffn_few_dx_kernel<kTokens, true><<<grid, kThreads, 0, stream>>>(j, parts);
+      ffn_few_dx_kernel<kTokens, true><<<grid, kThreads, 0, stream>>>(j, parts, slab);
     else
-      ffn_few_dx_kernel<kTokens, false><<<grid, kThreads, 0, stream>>>(j, parts);
+      ffn_few_dx_kernel<kTokens, false><<<grid, kThreads, 0, stream>>>(j, parts, slab);
     const int64_t blocks = (j.T * j.H + kThreads - 1) / kThreads;
     ffn_few_sum_kernel<<<static_cast<unsigned>(std::min<int64_t>(blocks, int64_t(sm_count()) * 8)), kThreads, 0, stream>>>(
         j, parts, static_cast<int>(slabs));
@@ -299,9 +305,9 @@ cudaError_t launch_grad(const FfnJob& j, float* parts, cudaStream_t stream) {
   if (e == cudaSuccess && j.dw_gate != nullptr) {
     count_launch();
     if (tokens && even(j.dw_gate, j.F, j.lddw) && even(j.dw_up, j.F, j.lddw))
-      ffn_few_dw_kernel<kTokens, true><<<grid, kThreads, 0, stream>>>(j);
+      ffn_few_dw_kernel<kTokens, true><<<grid, kThreads, 0, stream>>>(j, slab);
     else
-      ffn_few_dw_kernel<kTokens, false><<<grid, kThreads, 0, stream>>>(j);
+      ffn_few_dw_kernel<kTokens, false><<<grid, kThreads, 0, stream>>>(j, slab);
     e = cudaGetLastError();
   }
   return e;
@@ -316,7 +322,8 @@ cudaError_t launch_ffn_few(const FfnJob& j, bool even, cudaStream_t stream) {
 }
 
 size_t ffn_few_workspace(int64_t T, int64_t H, int64_t F) {
-  return 4 * (2 * size_t(T) * size_t(padded(F)) + size_t(slabs_of(F)) * size_t(T) * size_t(H));
+  const int slab = slab_of(H, F);
+  return 4 * (2 * size_t(T) * size_t(padded(F)) + size_t((F + slab - 1) / slab) * size_t(T) * size_t(H));
 }
 
 cudaError_t launch_ffn_few_grad(FfnJob j, void* workspace, cudaStream_t stream) {

@@ -5,7 +5,7 @@
 // six products of bf16 at 16 times the f32 units' rate or more.  The tensor cores
 // cut their f32 sums off instead of rounding them, by up to 2^-23 each time: a1 b1 and
 // the rest are summed apart, so that the small terms lose nothing to the large ones, and
-// runs of 512 k are summed there and the runs' sums in registers, rounded to nearest.
+// runs of 256 k are summed there and the runs' sums in registers, rounded to nearest.
 // The error is below that of one f32 chain over k.  An infinite input has parts
 // (inf, 0, 0) and makes NaN where it meets a part that is 0.
 //
@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kGroups = 2, kStoreWarps = 4 * kGroups, kPairThreads = 128 + 32 * kStoreWarps;
-constexpr int kMostN = 128, kRun = 8, kMaxStages = 6;  // kRun blocks of 64 k are summed at once
+constexpr int kMostN = 128, kRun = 4, kMaxStages = 6;  // kRun blocks of 64 k are summed at once
 constexpr int kSwapBytes = kGroups * 4 * 8 * 32 * 4;    // groups, quadrants, columns, lanes
 
 // ---------------------------------------------------------------- the parts

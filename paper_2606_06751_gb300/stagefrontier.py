@@ -610,12 +610,17 @@ _DTYPES = {torch.float32: SF_F32, torch.bfloat16: SF_BF16, torch.float16: SF_F16
 
 def _rows(t: torch.Tensor, name: str):
     """(rows, columns, row stride) of a CUDA matrix whose rows are contiguous."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or t.dim() != 2:
+    try:
+        n, m = t.shape
+        fine = t.is_cuda and t.dtype in _DTYPES
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
         raise TypeError(f"{name} must be a CUDA matrix of float32, bfloat16 or float16")
-    n, m = t.shape
-    if m > 1 and t.stride(1) != 1:
+    ld, one = t.stride()
+    if m > 1 and one != 1:
         raise TypeError(f"{name} must have contiguous rows")
-    return n, m, (t.stride(0) if n > 1 else m)
+    return n, m, (ld if n > 1 else m)
 
 
 def _vec(t: Optional[torch.Tensor], n: int, dtype, name: str):
@@ -835,12 +840,21 @@ def sf_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, per_tensor
 _ACTS = {"silu": SF_ACT_SILU, "gelu": SF_ACT_GELU, "gelu_tanh": SF_ACT_GELU_TANH, "relu": SF_ACT_RELU}
 
 
-def _here(*tensors):
-    """The tensors given are on the current device, which the launches go to."""
-    d = torch.cuda.current_device()
+# the current device without torch's initialisation around it, where torch has that
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _here(tensors) -> int:
+    """The current device, which the launches go to and the tensors given have to be on."""
+    d = _device()
     for t in tensors:
         if t is not None and t.get_device() != d:
             raise ValueError("tensors must be on the current CUDA device")
+    return d
+
+
+def _on(stream, d: int) -> int:
+    return _raw_stream(d) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _like_rows(t, shape, dtypes, name: str):
@@ -852,46 +866,42 @@ def _like_rows(t, shape, dtypes, name: str):
 
 
 def _ffn_inputs(x, w_gate, w_up, act: str):
-    """(T, H, F, ldx, ldw, activation, whether all rows start on 16 bytes)"""
+    """(T, H, F, ldx, ldw, activation, whether all rows start on 16 bytes, the three pointers)"""
     T, H, ldx = _rows(x, "x")
     F, h, ldw = _rows(w_gate, "w_gate")
     if h != H or w_gate.dtype != x.dtype:
         raise ValueError("w_gate must be [F][H] of x's type")
     if _like_rows(w_up, (F, H), (x.dtype,), "w_up") != ldw:
         raise ValueError("w_gate and w_up must have one row spacing")
-    if act not in _ACTS:
+    number = _ACTS.get(act)
+    if number is None:
         raise ValueError(f"act must be one of {', '.join(_ACTS)}")
     size = 4 if x.dtype == torch.float32 else 2
-    even = (x.data_ptr() | w_gate.data_ptr() | w_up.data_ptr() | (ldx * size if T > 1 else 0) |
-            (ldw * size if F > 1 else 0)) % 16 == 0
-    return T, H, F, ldx, ldw, _ACTS[act], even
+    px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
+    even = (px | pg | pu | (ldx * size if T > 1 else 0) | (ldw * size if F > 1 else 0)) % 16 == 0
+    return T, H, F, ldx, ldw, number, even, px, pg, pu
 
 
-def _ffn_workspace(x, T, H, F, even, grad, made):
+def _ffn_workspace(x, T, H, F, even, grad):
     n = _lib.sf_gated_ffn_workspace_size(_DTYPES[x.dtype], T, H, F, 1 if even else 0, grad)
-    if n == 0:
-        return None
-    made.append(torch.empty(n, dtype=torch.uint8, device=x.device))
-    return made[-1]
+    return None if n == 0 else torch.empty(n, dtype=torch.uint8, device=x.device)
 
 
 def sf_gated_ffn(x, w_gate, w_up, act: str = "silu", h=None, workspace=None, status=None, stream=None) -> torch.Tensor:
     """The gated feed-forward product act(x w_gate^T) * (x w_up^T) [T][F] of x [T][H]
     and weights [F][H], all of one type."""
-    T, H, F, ldx, ldw, number, even = _ffn_inputs(x, w_gate, w_up, act)
-    _here(x, w_gate, w_up, h, workspace, status)
-    made, ldh = [], F
+    T, H, F, ldx, ldw, number, even, px, pg, pu = _ffn_inputs(x, w_gate, w_up, act)
+    d = _here((x, w_gate, w_up, h, workspace, status))
     if h is None:
-        h = _empty((T, F), x.dtype, x)
-        made.append(h)
+        h, ldh = torch.empty((T, F), dtype=x.dtype, device=x.device), F
     else:
         ldh = _like_rows(h, (T, F), (x.dtype,), "h")
     if workspace is None:
-        workspace = _ffn_workspace(x, T, H, F, even, 0, made)
-    _hold(made, stream)
-    _check(_lib.sf_gated_ffn(_p(x), _DTYPES[x.dtype], T, H, ldx, _p(w_gate), _p(w_up), F, ldw, number, _p(h), ldh,
-                             _p(workspace), 0 if workspace is None else workspace.numel(), _p(status),
-                             _stream(stream)), "sf_gated_ffn")
+        workspace = _ffn_workspace(x, T, H, F, even, 0)
+    if stream is not None:
+        _hold((h, workspace), stream)
+    _check(_lib.sf_gated_ffn(px, _DTYPES[x.dtype], T, H, ldx, pg, pu, F, ldw, number, h.data_ptr(), ldh, _p(workspace),
+                             0 if workspace is None else workspace.numel(), _p(status), _on(stream, d)), "sf_gated_ffn")
     return h
 
 
@@ -909,44 +919,43 @@ def sf_gated_ffn_grad(x, w_gate, w_up, dh, act: str = "silu", dx=None, dw_gate=N
     """The gradients of sf_gated_ffn's inputs from that of its result, dh [T][F]: of
     x, and of both weights (of x's type or float32; added to the tensors given with
     `accumulate`).  With "h" in `want` the product itself once more."""
-    T, H, F, ldx, ldw, number, even = _ffn_inputs(x, w_gate, w_up, act)
-    lddh = _like_rows(dh, (T, F), (x.dtype,), "dh")
-    _here(x, w_gate, w_up, dh, dx, dw_gate, dw_up, h, workspace, status)
-    made = []
-
-    def out(t, name, wanted, shape, dtypes):
-        if t is not None:
-            return t, _like_rows(t, shape, dtypes, name)
-        if not wanted:
-            return None, shape[1]
-        made.append(_empty(shape, dtypes[0], x))
-        return made[-1], shape[1]
-
+    T, H, F, ldx, ldw, number, even, px, pg, pu = _ffn_inputs(x, w_gate, w_up, act)
+    dtype, device = x.dtype, x.device
+    lddh = _like_rows(dh, (T, F), (dtype,), "dh")
+    d = _here((x, w_gate, w_up, dh, dx, dw_gate, dw_up, h, workspace, status))
     if (dw_gate is None) != (dw_up is None):
         raise ValueError("dw_gate and dw_up go together")
-    if accumulate and dw_gate is None:
-        raise ValueError("accumulate adds to gradients that the caller gives")
-    types = (x.dtype, torch.float32)
+    lddx, lddw, ldh = H, H, F
+    if dx is not None:
+        lddx = _like_rows(dx, (T, H), (dtype,), "dx")
+    elif "dx" in want:
+        dx = torch.empty((T, H), dtype=dtype, device=device)
     if dw_gate is not None:
-        types = (dw_gate.dtype,) if dw_gate.dtype in types else types
-    elif dw_dtype is not None:
-        if dw_dtype not in types:
+        lddw = _like_rows(dw_gate, (F, H), (dtype, torch.float32), "dw_gate")
+        if _like_rows(dw_up, (F, H), (dw_gate.dtype,), "dw_up") != lddw:
+            raise ValueError("dw_gate and dw_up must have one row spacing")
+    elif accumulate:
+        raise ValueError("accumulate adds to gradients that the caller gives")
+    elif "dw" in want:
+        if dw_dtype is None:
+            dw_dtype = dtype
+        elif dw_dtype is not dtype and dw_dtype is not torch.float32:
             raise ValueError("dw_dtype must be x's type or float32")
-        types = (dw_dtype,)
-    dx, lddx = out(dx, "dx", "dx" in want, (T, H), (x.dtype,))
-    dw_gate, lddw = out(dw_gate, "dw_gate", "dw" in want, (F, H), types)
-    dw_up, other = out(dw_up, "dw_up", "dw" in want, (F, H), types)
-    if other != lddw:
-        raise ValueError("dw_gate and dw_up must have one row spacing")
-    h, ldh = out(h, "h", "h" in want, (T, F), (x.dtype,))
+        dw_gate = torch.empty((F, H), dtype=dw_dtype, device=device)
+        dw_up = torch.empty((F, H), dtype=dw_dtype, device=device)
+    if h is not None:
+        ldh = _like_rows(h, (T, F), (dtype,), "h")
+    elif "h" in want:
+        h = torch.empty((T, F), dtype=dtype, device=device)
     if workspace is None:
-        workspace = _ffn_workspace(x, T, H, F, even, 1, made)
-    _hold(made, stream)
-    _check(_lib.sf_gated_ffn_grad(_p(x), _DTYPES[x.dtype], T, H, ldx, _p(w_gate), _p(w_up), F, ldw, number, _p(dh), lddh,
-                                  _p(dx), lddx, _p(dw_gate), _p(dw_up),
-                                  SF_F32 if dw_gate is None else _DTYPES[dw_gate.dtype], lddw, 1 if accumulate else 0,
-                                  _p(h), ldh, _p(workspace), 0 if workspace is None else workspace.numel(), _p(status),
-                                  _stream(stream)), "sf_gated_ffn_grad")
+        workspace = _ffn_workspace(x, T, H, F, even, 1)
+    if stream is not None:
+        _hold((dx, dw_gate, dw_up, h, workspace), stream)
+    _check(_lib.sf_gated_ffn_grad(px, _DTYPES[dtype], T, H, ldx, pg, pu, F, ldw, number, dh.data_ptr(), lddh, _p(dx), lddx,
+                                  _p(dw_gate), _p(dw_up), SF_F32 if dw_gate is None else _DTYPES[dw_gate.dtype], lddw,
+                                  1 if accumulate else 0, _p(h), ldh, _p(workspace),
+                                  0 if workspace is None else workspace.numel(), _p(status), _on(stream, d)),
+           "sf_gated_ffn_grad")
     return GatedFfnGrad(dx, dw_gate, dw_up, h)
 
 
@@ -957,17 +966,19 @@ def sf_dropout(x, p: float, key, residual=None, out=None, stream=None) -> torch.
     `out` may be x or residual itself."""
     N, D, ldx = _rows(x, "x")
     _vec(key, 2, torch.int64, "key")
-    _here(x, key, residual, out)
+    d = _here((x, key, residual, out))
+    dtype = x.dtype
     ldr = ldo = D
     if residual is not None:
-        ldr = _like_rows(residual, (N, D), (x.dtype,), "residual")
+        ldr = _like_rows(residual, (N, D), (dtype,), "residual")
     if out is None:
-        out = _empty((N, D), x.dtype, x)
-        _hold([out], stream)
+        out = torch.empty((N, D), dtype=dtype, device=x.device)
+        if stream is not None:
+            _hold((out,), stream)
     else:
-        ldo = _like_rows(out, (N, D), (x.dtype,), "out")
-    _check(_lib.sf_dropout(_p(x), _DTYPES[x.dtype], N, D, ldx, p, _p(key), _p(residual), ldr, _p(out), ldo,
-                           _stream(stream)), "sf_dropout")
+        ldo = _like_rows(out, (N, D), (dtype,), "out")
+    _check(_lib.sf_dropout(x.data_ptr(), _DTYPES[dtype], N, D, ldx, p, key.data_ptr(), _p(residual), ldr, out.data_ptr(),
+                           ldo, _on(stream, d)), "sf_dropout")
     return out
 
 
@@ -980,16 +991,15 @@ class Verified:
 
 def _row_stack(t, shape, dtype, name: str):
     """The row stride of a [B][n][V] tensor whose rows are evenly spaced."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or t.dim() != 3:
-        raise TypeError(f"{name} must be a CUDA tensor [B][rows][V] of float32, bfloat16 or float16")
-    if tuple(t.shape) != shape or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} must be {list(shape)} of {dtype}")
     B, n, V = shape
-    if V > 1 and t.stride(2) != 1:
+    far, ld, one = t.stride()
+    if V > 1 and one != 1:
         raise TypeError(f"{name} must have contiguous rows")
-    if n > 1 and B > 1 and t.stride(0) != n * t.stride(1):
+    if n > 1 and B > 1 and far != n * ld:
         raise TypeError(f"{name}'s rows must be evenly spaced")
-    return t.stride(1) if n > 1 else t.stride(0) if B > 1 and n > 0 else V
+    return ld if n > 1 else far if B > 1 and n > 0 else V
 
 
 def sf_verify_draft(target, token, draft=None, lengths=None, uniform=None, noise=None, inv_temperature: float = 1.0,
@@ -1005,32 +1015,34 @@ def sf_verify_draft(target, token, draft=None, lengths=None, uniform=None, noise
     if token.dim() != 2:
         raise ValueError("token must be [B][L]")
     B, L = token.shape
-    if not isinstance(target, torch.Tensor) or target.dim() != 3:
-        raise TypeError("target must be a CUDA tensor [B][L + 1][V]")
+    for t in (target, draft):
+        if t is not None and not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _DTYPES and t.dim() == 3):
+            raise TypeError("target and draft must be CUDA tensors [B][rows][V] of float32, bfloat16 or float16")
+    dtype, device = target.dtype, target.device
     V = target.shape[2]
-    ldt = _row_stack(target, (B, L + 1, V), target.dtype, "target")
-    ldq = V if draft is None else _row_stack(draft, (B, L, V), target.dtype, "draft")
+    ldt = _row_stack(target, (B, L + 1, V), dtype, "target")
+    ldq = V if draft is None else _row_stack(draft, (B, L, V), dtype, "draft")
     _vec(lengths, B, torch.int32, "lengths")
     _vec(uniform, B * L, torch.float32, "uniform")
     _vec(noise, B * V, torch.float32, "noise")
     if (uniform is None) != (noise is None):
         raise ValueError("uniform and noise go together")
-    _here(target, token, draft, lengths, uniform, noise, out_token, accepted, logp, status)
-    made = []
-
-    def new(shape, dtype):
-        made.append(torch.empty(shape, dtype=dtype, device=target.device))
-        return made[-1]
-
-    out_token = new((B, L + 1), torch.int64) if out_token is None else _vec(out_token, B * (L + 1), torch.int64,
-                                                                            "out_token")
-    accepted = new(B, torch.int32) if accepted is None else _vec(accepted, B, torch.int32, "accepted")
+    d = _here((target, token, draft, lengths, uniform, noise, out_token, accepted, logp, status))
+    if out_token is None:
+        out_token = torch.empty((B, L + 1), dtype=torch.int64, device=device)
+    else:
+        _vec(out_token, B * (L + 1), torch.int64, "out_token")
+    if accepted is None:
+        accepted = torch.empty(B, dtype=torch.int32, device=device)
+    else:
+        _vec(accepted, B, torch.int32, "accepted")
     if logp is not None:
         _vec(logp, B * (L + 1), torch.float32, "logp")
     elif "logp" in want:
-        logp = new((B, L + 1), torch.float32)
-    _hold(made, stream)
-    _check(_lib.sf_verify_draft(_p(target), _DTYPES[target.dtype], B, L, V, ldt, _p(draft), ldq, _p(token), _p(lengths),
-                                _p(uniform), _p(noise), inv_temperature, _p(out_token), _p(accepted), _p(logp),
-                                _p(status), _stream(stream)), "sf_verify_draft")
+        logp = torch.empty((B, L + 1), dtype=torch.float32, device=device)
+    if stream is not None:
+        _hold((out_token, accepted, logp), stream)
+    _check(_lib.sf_verify_draft(target.data_ptr(), _DTYPES[dtype], B, L, V, ldt, _p(draft), ldq, token.data_ptr(),
+                                _p(lengths), _p(uniform), _p(noise), inv_temperature, out_token.data_ptr(),
+                                accepted.data_ptr(), _p(logp), _p(status), _on(stream, d)), "sf_verify_draft")
     return Verified(out_token, accepted, logp)
