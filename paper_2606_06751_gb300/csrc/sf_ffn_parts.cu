@@ -318,6 +318,8 @@ bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t len, int64_
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+constexpr size_t kSmem = 226 * 1024;  // of 227 KB, 1 KB for the barriers
+
 struct Cut {
   int N, stages;
   int64_t m_tiles, n_tiles;
@@ -341,7 +343,7 @@ Cut cut_of(int64_t M, int64_t Nall, int blocks) {
     if (c.us < best.us) best = c;
   }
   const size_t stage = 3 * (kABytes + size_t(best.N / 2) * kDepthBytes);
-  best.stages = static_cast<int>(std::min<size_t>(kMaxStages, (227 * 1024 - 1024 - 1024 - kSwapBytes) / stage));
+  best.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmem - 1024 - kSwapBytes) / stage));
   return best;
 }
 
@@ -371,7 +373,7 @@ cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
     maps.b1 = maps.b0;
   }
   if (!fine) return cudaErrorUnknown;
-  const size_t smem = 1024 + s.stages * 3 * (kABytes + size_t(s.N / 2) * kDepthBytes) + kSwapBytes;
+  const size_t smem = kSmem;  // all, whatever the stages take: no other CTA on its SM
   const auto kernel = ffn_parts_kernel<kProduct>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;

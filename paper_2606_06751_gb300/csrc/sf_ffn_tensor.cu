@@ -273,6 +273,7 @@ constexpr int kSplitThreads = 256;
 
 // Each CTA of a cluster sums its share of the blocks for the same 128 rows and N
 // columns; then CTA r adds up, in the CTAs' order, and stores a share of the columns.
+// Tensor memory is given back before the CTAs wait for one another.
 template <typename T, int kProduct>
 __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_constant__ Maps maps, const FfnJob j,
                                                                   const Shape s) {
@@ -356,49 +357,33 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
     while (global_timer_ns() - t0 < 2000000u) {
     }
   }
-  cluster_sync();  // the stages of every CTA are free
-
   const int q = warp & 3;
   const uint32_t mine = sums + (uint32_t(q) << 21);
-  if (!L::kGated && C == 1) {  // nothing to add up or exchange
-    for (int c = 16 * (warp >> 2); c < s.N; c += 32) {
-      uint32_t v[16];
-      float x[16];
-      tensor_load16(mine + c, v);
-      tensor_loaded();
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(v[i]);
-      if constexpr (!L::kGated) store_plain<T, kProduct>(j, second, m + 32 * q + lane, n + c, 1, 16, x);
-    }
-    tensor_fence_before();
-    __syncthreads();
-    if (warp == 2) tensor_free<1>(sums, s.columns);
-    return;
-  }
-  // partial sums: [source CTA][column of the share][128 rows] in the CTA that stores them
-  float* partial = reinterpret_cast<float*>(base);
-  const int share = (s.N + C - 1) / C;
+  float* partial = reinterpret_cast<float*>(base);  // [column][128 rows], where the stages were
+  const bool direct = !L::kGated && C == 1;         // nothing to add up or exchange
   for (int c = 16 * (warp >> 2); c < s.N; c += 32) {
     uint32_t v[16];
+    float x[16];
     tensor_load16(mine + c, v);
     tensor_loaded();
-    int to = c / share, left = (to + 1) * share - c;
-    uint32_t at = at_rank(partial + (rank * share + c - to * share) * 128 + 32 * q + lane, to);
 #pragma unroll
-    for (int i = 0; i < 16; ++i, at += 512) {
-      if (left-- == 0) {
-        left = share - 1;
-        at = at_rank(partial + rank * share * 128 + 32 * q + lane, ++to);
-      }
-      store_at(at, __uint_as_float(v[i]));
+    for (int i = 0; i < 16; ++i) x[i] = last > first ? __uint_as_float(v[i]) : 0.f;
+    if constexpr (!L::kGated) {
+      if (direct) store_plain<T, kProduct>(j, second, m + 32 * q + lane, n + c, 1, 16, x);
+    }
+    if (!direct) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) partial[(c + i) * 128 + 32 * q + lane] = x[i];
     }
   }
   tensor_fence_before();
-  cluster_sync();
-  if (warp == 2) tensor_free<1>(sums, s.columns);
-  const int from = rank * share, count = min(share, s.N - from);
+  __syncthreads();
+  if (warp == 2) tensor_free<1>(sums, s.columns);  // before the CTAs wait for one another
+  if (direct) return;
+  if (C > 1) cluster_sync();
+  const int share = (s.N + C - 1) / C, from = rank * share, count = min(share, s.N - from);
   // a thread a row, K columns at a time
-  constexpr int K = 4, kStep = kSplitThreads / L::kRows;
+  constexpr int K = 8, kStep = kSplitThreads / L::kRows;
   const int r = tid & (L::kRows - 1);
   const int64_t row = m + r;
   for (int c = tid / L::kRows; c < count; c += K * kStep) {
@@ -408,12 +393,12 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
 #pragma unroll
     for (int i = 0; i < K; ++i) v[i] = u[i] = 0.f;
     for (int k = 0; k < C; ++k) {
-      const float* p = partial + (k * share + c) * 128 + r;
+      const uint32_t p = at_rank(partial + (from + c) * 128 + r, k);
 #pragma unroll
       for (int i = 0; i < K; ++i)
         if (c + i * kStep < count) {
-          v[i] += p[i * kStep * 128];
-          if (L::kGated) u[i] += p[i * kStep * 128 + 64];
+          v[i] += load_at(p + i * kStep * 512);
+          if (L::kGated) u[i] += load_at(p + i * kStep * 512 + 256);
         }
     }
     const int most = min(count - c, K * kStep);
@@ -422,6 +407,7 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
     else
       store_plain<T, kProduct>(j, second, row, n + from + c, kStep, most, v);
   }
+  if (C > 1) cluster_sync();  // the others have read this CTA's sums
 }
 
 // ---------------------------------------------------------------- host
@@ -463,7 +449,7 @@ bool make_maps(Maps& maps, const FfnJob& j, int n_rows) {
          make_map(&maps.a1, j.w_up, j.dtype, j.F, j.H, j.ldw, kBox);
 }
 
-constexpr size_t kSmemMost = 227 * 1024, kSmemFixed = 1024 + 1024;  // alignment; barriers
+constexpr size_t kSmemMost = 227 * 1024, kSmemBarriers = 1024, kSmemFixed = kSmemBarriers + 1024;  // and alignment
 
 // The split kernel's shared memory.
 uint32_t columns_of(int N) {
@@ -478,7 +464,7 @@ int split_stages(int N, int C, int blocks) {
   return std::min(most, std::min<int>(4, static_cast<int>(ceil_div(blocks, C))));
 }
 size_t split_smem(int N, int C, int blocks) {
-  const size_t sums = size_t(ceil_div(N, C)) * C * 512;
+  const size_t sums = size_t(N) * 512;
   // CTAs that share an SM must find room in tensor memory: shared memory allows no more of them than that
   const size_t room = kSmemMost * columns_of(N) / 512;
   return 1024 + std::max({sums, room, split_stages(N, C, blocks) * (kABytes + size_t(N) * kDepthBytes)});
@@ -490,7 +476,7 @@ cudaError_t launch_pairs(const FfnJob& j, Shape s, cudaStream_t stream) {
   if (!make_maps<kProduct>(maps, j, s.N / 2)) return cudaErrorUnknown;
   const size_t stage = kABytes + size_t(s.N / 2) * kDepthBytes, swap = Layout<kProduct>::kGated ? kSwapBytes : 0;
   s.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemMost - kSmemFixed - swap) / stage));
-  const size_t smem = 1024 + s.stages * stage + swap;
+  const size_t smem = kSmemMost - kSmemBarriers;  // all, whatever the stages take: no other CTA on its SM
   const auto kernel = ffn_pair_kernel<T, kProduct>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;

@@ -60,7 +60,9 @@ __device__ __forceinline__ void products_arrive(uint64_t* bar) {
                  : "memory");
 }
 
-// One warp; waits while other CTAs of the SM hold the columns.
+// One warp; waits while other CTAs of the SM hold the columns.  So that no two kernels
+// can wait for each other's columns, a CTA either waits for no other CTA while it holds
+// some, or takes all shared memory of its SM with them.
 template <int kCtas>
 __device__ __forceinline__ void tensor_alloc(uint32_t* at, uint32_t columns) {
   if constexpr (kCtas == 2) {
@@ -119,8 +121,11 @@ __device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map
 __device__ __forceinline__ void arrive_at(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void store_at(uint32_t at, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+// From the shared memory of a CTA of the cluster.
+__device__ __forceinline__ float load_at(uint32_t at) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
 }
 
 }  // namespace sf
