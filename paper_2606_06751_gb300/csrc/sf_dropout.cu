@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kThreads) dropout_pack_kernel(const DropoutJob
   load_keys(keys, j.key);
   const int lane = threadIdx.x & 31, in_row = lane & ((1 << t.shift) - 1), below = lane >> t.shift;
   const int packs = static_cast<int>((j.D + (kShift ? N - 1 : 0) + kCols - 1) / kCols);
-  const int D = static_cast<int>(j.D);
+  const int64_t D = j.D;
   const T *x = static_cast<const T*>(j.x), *res = static_cast<const T*>(j.residual);
   T* out = static_cast<T*>(j.out);
   const int64_t step = int64_t(gridDim.x) * (kThreads / 32);
@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(kThreads) dropout_pack_kernel(const DropoutJob
     const int64_t row0 = tile_row * t.rows + below;
     const int at0 = static_cast<int>(seg) * (kTurns * 32) + in_row;
     uint32_t rows[kTurns], ats[kTurns];
-    int off[kTurns], c[kTurns];
+    int off[kTurns];
+    int64_t c[kTurns];
     bool mine[kTurns], whole[kTurns];
     uint4 u[kTurns][P], v[kTurns][P], w[kTurns];
 #pragma unroll
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(kThreads) dropout_pack_kernel(const DropoutJob
       rows[k] = static_cast<uint32_t>(row);
       ats[k] = static_cast<uint32_t>(at);
       off[k] = kShift ? row_off<T>(j, row) : 0;
-      c[k] = at * kCols - off[k];
+      c[k] = int64_t(at) * kCols - off[k];
       mine[k] = row < j.N && at < packs;
       whole[k] = mine[k] && c[k] >= 0 && c[k] + kCols <= D;
       if (whole[k]) {

@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kThreads) ffn_few_sum_kernel(const FfnJob j, c
   const int64_t all = j.T * j.H, step = int64_t(gridDim.x) * kThreads;
   for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < all; i += step) {
     float s = 0.f;
-#pragma unroll 8
+#pragma unroll 16
     for (int k = 0; k < slabs; ++k) s += parts[k * all + i];
     const int64_t t = i / j.H;
     static_cast<float*>(j.dx)[t * j.lddx + i - t * j.H] = s;

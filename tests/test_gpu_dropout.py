@@ -207,6 +207,24 @@ def test_long_tensor(sf):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("start", [0, 3])
+def test_longest_row(sf, start):
+    """A row of 2^31 - 1 columns, from a 16-byte boundary and from within: its last columns."""
+    D = (1 << 31) - 1
+    flat = torch.ones(D + 16, dtype=torch.bfloat16, device="cuda")
+    x = flat[start:start + D].view(1, D)
+    sf.sf_dropout(x, 0.5, key_of(1, 1), out=x)
+    for pack in (0, (1 << 28) - 2):
+        at = np.arange(pack, pack + 2)[None]
+        z = np.zeros_like(at)
+        w = philox([at, z, z + 1, z], (1, 0))
+        bits = np.stack([v for u in w for v in (u & np.uint64(0xFFFF), u >> np.uint64(16))], -1).reshape(-1)
+        got = x[0, pack * 8:pack * 8 + 16].float().cpu().numpy()
+        assert np.array_equal(got, np.where(bits >= 32768, 2.0, 0.0)[:len(got)])
+    assert bool((flat[start + D:] == 1).all()) and bool((flat[:start] == 1).all())
+
+
+@pytest.mark.gpu
 def test_refusals(sf):
     x = torch.zeros((4, 64), device="cuda")
     key = key_of(1, 1)
