@@ -94,19 +94,36 @@ __device__ __forceinline__ float warp_top(float v) {
   return r;
 }
 
-// kPacks packs a lane of a row: packs p, p + 32, ... before `to`.
+// kPacks packs a lane of a row.
 template <typename T>
 struct Piece {
   uint4 u[kPacks];
-  __device__ __forceinline__ void load(const T* z, int off, int p, int to, int V) {
+  int base;  // the place in the row of the lane's first value
+  int row;
+};
+constexpr int kStride = kPacks * 32;  // packs of a piece
+
+// Where a warp is in its run of pieces.
+template <typename T>
+struct Cursor {
+  const T* z;      // the row
+  int off, p;      // its distance from a 16-byte boundary; the lane's next pack
+  int whole, end;  // packs of the row that end in it; of the CTA's slice
+  int row, left;   // pieces left of this row
+  // packs p, p + 32, ...; outside the slice -inf
+  __device__ __forceinline__ void load(Piece<T>& piece, int V) const {
     constexpr int N = Pack<T>::kN;
-    const int p0 = p - static_cast<int>(threadIdx.x & 31), end = p0 + kPacks * 32;
-    if (p0 > 0 && end <= to && end * N - off <= V) {
+    const int p0 = p - static_cast<int>(threadIdx.x & 31);
+    piece.base = p * N - off;
+    piece.row = row;
+    if ((p0 > 0 || off == 0) && p0 + kStride <= min(whole, end)) {
+      const T* at = z + piece.base;
 #pragma unroll
-      for (int k = 0; k < kPacks; ++k) u[k] = load16(z + (p + k * 32) * N - off);
+      for (int k = 0; k < kPacks; ++k) piece.u[k] = load16(at + k * 32 * N);
     } else {
 #pragma unroll
-      for (int k = 0; k < kPacks; ++k) u[k] = p + k * 32 < to ? row_pack(z, off, p + k * 32, V) : lowest_pack(T());
+      for (int k = 0; k < kPacks; ++k)
+        piece.u[k] = p + k * 32 < end ? row_pack(z, off, p + k * 32, V) : lowest_pack(T());
     }
   }
 };
@@ -118,7 +135,7 @@ struct Running {
   float m = neg_inf(), scale;
   uint64_t s = 0;  // a pair of sums
   int at = kNowhere;
-  __device__ __forceinline__ void add(const Piece<T>& piece, int off, int p) {
+  __device__ __forceinline__ void add(const Piece<T>& piece) {
     constexpr int N = Pack<T>::kN;
     const float top = warp_top(packs_max(piece.u, T()));
     if (top > m) {  // one branch for the warp
@@ -138,7 +155,7 @@ struct Running {
         float x, y;
         if (kGreedy) {
           split(w[q], x, y);
-          const int place = (p + k * 32) * N - off + 2 * q;
+          const int place = piece.base + k * 32 * N + 2 * q;
           if (y == m) at = min(at, place + 1);
           if (x == m) at = min(at, place);
         }
@@ -211,6 +228,10 @@ __global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJo
   const T* target = static_cast<const T*>(j.target) + b * (L + 1) * j.ldt;
   const T* draft = !kGreedy && j.draft != nullptr ? static_cast<const T*>(j.draft) + b * L * j.ldq : nullptr;
   const float scale = j.tau * kLog2e;
+  // packs of a CTA's slice; rows that do not all start on 16 bytes may have one more
+  const bool even_rows = ((reinterpret_cast<uintptr_t>(j.target) | uint64_t(j.ldt) * sizeof(T)) & 15u) == 0 &&
+                         (draft == nullptr || ((reinterpret_cast<uintptr_t>(j.draft) | uint64_t(j.ldq) * sizeof(T)) & 15u) == 0);
+  const int slice = ((V + (even_rows ? 0 : N - 1) + N - 1) / N + C - 1) / C;
   uint32_t bits = given != n ? SF_ST_INDEX : 0u;
   Stop o;
   for (int g0 = 0, turn = 0; o.at < 0; g0 += kGroup, turn ^= 1) {
@@ -219,21 +240,32 @@ __global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJo
     for (int i = lane; i < all; i += 32) warps[i][warp] = nothing();
     __syncwarp();
     // the slices of all rows as one run of pieces, cut evenly among the warps
-    const int slice = ((V + 2 * N - 2) / N + C - 1) / C, per_row = (slice + kPacks * 32 - 1) / (kPacks * 32);
+    const int per_row = (slice + kStride - 1) / kStride;
     const int first = all * per_row * warp / kWarps, last = all * per_row * (warp + 1) / kWarps;
-    const auto place = [&](int item, int& i, const T*& z, int& off, int& p, int& to) {
-      i = item / per_row;
-      z = i < g ? target + (g0 + i) * j.ldt : draft + (g0 + i - g) * j.ldq;
-      off = row_offset(z);
-      p = rank * slice + (item - i * per_row) * (kPacks * 32) + lane;
-      to = min((rank + 1) * slice, (off + V + N - 1) / N);
+    Cursor<T> at;
+    const auto to_row = [&](int row) {
+      at.row = row;
+      at.z = row < g ? target + (g0 + row) * j.ldt : draft + (g0 + row - g) * j.ldq;
+      at.off = row_offset(at.z);
+      at.p = rank * slice + lane;
+      at.whole = (at.off + V) / N;
+      at.end = min((rank + 1) * slice, (at.off + V + N - 1) / N);
+      at.left = per_row;
+    };
+    const auto fetch = [&](Piece<T>& piece) {
+      at.load(piece, V);
+      if (--at.left > 0)
+        at.p += kStride;
+      else if (at.row + 1 < all)
+        to_row(at.row + 1);
     };
     Piece<T> odd, even;
-    int i, off, p, to, i2, off2, p2;
-    const T* z;
     if (first < last) {
-      place(first, i, z, off, p, to);
-      even.load(z, off, p, to, V);
+      const int row = first / per_row, gone = first - row * per_row;
+      to_row(row);
+      at.p += gone * kStride;
+      at.left -= gone;
+      fetch(even);
     }
     if (g0 == 0 && tid < n) {  // what the decisions need besides
       const int64_t y = j.token[b * L + tid];
@@ -254,19 +286,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJo
     };
     for (int item = first; item < last; item += 2) {  // the next piece is on its way while one is summed
       const bool two = item + 1 < last, three = item + 2 < last;
-      if (two) {
-        place(item + 1, i2, z, off2, p2, to);
-        odd.load(z, off2, p2, to, V);
-      }
-      run.add(even, off, p);
-      if (!two || i2 != i) keep(i);
+      if (two) fetch(odd);
+      run.add(even);
+      if (!two || odd.row != even.row) keep(even.row);
       if (!two) break;
-      if (three) {
-        place(item + 2, i, z, off, p, to);
-        even.load(z, off, p, to, V);
-      }
-      run.add(odd, off2, p2);
-      if (!three || i != i2) keep(i2);
+      if (three) fetch(even);
+      run.add(odd);
+      if (!three || even.row != odd.row) keep(odd.row);
     }
     __syncthreads();
     for (int i = warp; i < all; i += kWarps) {
