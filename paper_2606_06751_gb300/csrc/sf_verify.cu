@@ -7,14 +7,14 @@
 // CTAs a sequence, each with a slice of the vocabulary.  The positions go by in
 // groups: each warp streams its part of the group's rows (policy's and draft's) into
 // (maximum, sum of exponentials) pairs, the CTAs exchange them, and all decide alike
-// whether the sequence stops there.  Rows behind the stop are never read.  The slice
+// whether the sequence stops there.  Rows behind that group are not read.  The slice
 // of the one row that the next token comes from is then raced against the noise.
 // Bound by memory for many sequences: 64 of 4 tokens over 131072 bf16 entries, 187 MB,
-// take 46 us (60 % of the copy rate; the exponentials alone some 16 us of the special
+// take 42 us (66 % of the copy rate; the exponentials alone some 16 us of the special
 // function units, and the race begins when the rows are done).  One sequence over
-// 32768 takes 10 us of latency.  Four CTAs of 256 threads an SM: with the registers
-// of two or three 61 us.  Groups of fewer positions, which read fewer rows, were no
-// faster (3: 47, 2: 49 us): another exchange costs what they save.
+// 32768 takes 10 us of latency.  Four CTAs of 256 threads an SM: three take 48 us, two
+// with pieces of twice the size 44.  Groups of three positions, which read fewer rows,
+// were no faster: another exchange costs what they save.
 
 #include "sf_float.cuh"
 #include "sf_launch.h"
@@ -442,7 +442,7 @@ template <typename T, bool kGreedy>
 cudaError_t launch_type(const VerifyJob& j, cudaStream_t stream) {
   // CTAs a sequence: while all stay at once and each thread has a pack of a row.
   // 64 sequences of 4 tokens, 131072 bf16 entries: 55, 46, 55 us with 4, 8, 16; one of
-  // 32768: 14.7, 11.5, 10.2 us.
+  // 32768: 15, 12, 10 us.
   int C = 1;
   while (C < kMostCtas && j.B * C * 2 <= int64_t(sm_count()) * kPerSm && j.V > int64_t(C) * kThreads * Pack<T>::kN) C *= 2;
   const auto kernel = verify_kernel<T, kGreedy>;
