@@ -85,10 +85,9 @@ size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 // Whether a call takes the form for a few tokens.  Products, us here against the tensor cores:
 //   f32          16 tokens through 2048 x 4096  32 / 57, 8 through 4096 x 12288  88 / 296, 64 through
 //                1024 x 4096  60 / 29; gradients have this form up to 8 tokens
-//   16 bits      one token through 4096 x 12288  33.8 / 35.2, two 37.0 / 34.7; through 1024 x 2048
+//   16 bits      one token through 4096 x 12288  32.7 / 35.2, two 37.0 / 34.7; through 1024 x 2048
 //                one 3.7 / 5.4, four 4.4 / 5.4
-//   uneven rows  one token through 4097 x 12288  55 / 131 (with the copy of the weights), two 90 / 132,
-//                four 304 / 132
+//   uneven rows  one token through 4097 x 12288  55 / 131 (with the copy of the weights), two 90 / 132
 bool few_tokens(int32_t dtype, int64_t T, int64_t H, int64_t F, bool aligned, bool grad) {
   if (F > kFewMostFeatures) return false;
   if (dtype == SF_F32) return T <= (grad ? kFewGradTokens : 32);

@@ -10,7 +10,12 @@ namespace sf {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFeatures = 2;  // of a warp
+
+// Features of a warp, for their sake that the tokens are read for (us with 1 and 2, one GB300):
+// even rows f32 4 x 2048 x 7452 28 and 25, 8 x 1024 x 4096 15 and 12, bf16 1 x 4096 x 12288 32.7 and 34.2;
+// uneven rows f32 4 x 2009 x 7452 29 and 45, 8 x 2009 x 7452 95 and 67.
+template <typename T, int kTokens, bool kEven>
+constexpr int kFeaturesOf = kEven ? (sizeof(T) == 2 && kTokens == 1 ? 1 : 2) : kTokens <= 4 ? 1 : 2;
 
 // One value of h, or of dg and du in f32 (and h), from its g and u.
 template <typename T, int kAct, bool kInner>
@@ -28,13 +33,15 @@ __device__ __forceinline__ void store_value(const FfnJob& j, int64_t t, int64_t 
   }
 }
 
-// Feature rows 2 w and 2 w + 1 of both weights times kTokens tokens.  Each lane sums every
-// 32nd pack of 16 bytes (kEven: all rows start on 16 bytes) or value of a row, and the
-// lanes' sums are added.  Bound by the weights' bytes up to some 8 tokens (f32), then by
-// the multiply-adds; the tokens are read from L1, once for four weight rows.
+// A warp's rows of both weights times kTokens tokens.  Each lane sums every 32nd pack of
+// 16 bytes (kEven: all rows start on 16 bytes) or value of a row, and the lanes' sums are
+// added.  Bound by the weights' bytes (f32 1 x 4096 x 12288: 60 us, 99 % of the copy rate;
+// 8 tokens 88 us); the tokens are read from L1, once for all of the warp's rows, which the
+// weights do not pass through (that took 68 and 137 us).
 template <typename T, int kTokens, bool kEven, bool kInner>
-__global__ void __launch_bounds__(kThreads) ffn_rows_kernel(const FfnJob j) {
-  constexpr int N = kEven ? Pack<T>::kN : 1, kAhead = kEven ? (kTokens <= 2 ? 4 : 2) : 8;
+__global__ void __launch_bounds__(kThreads, kEven ? 2 : 4) ffn_rows_kernel(const FfnJob j) {
+  constexpr int kFeatures = kFeaturesOf<T, kTokens, kEven>;
+  constexpr int N = kEven ? Pack<T>::kN : 1, kAhead = kEven ? (kTokens <= 2 ? 4 : 2) : kFeatures == 1 ? 8 : 4;
   griddep_launch_dependents();
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t(blockIdx.y) * (kThreads / 32)) + (threadIdx.x >> 5);
@@ -125,19 +132,22 @@ __global__ void __launch_bounds__(kThreads) ffn_rows_kernel(const FfnJob j) {
   }
 }
 
-template <typename T, int kTokens, bool kInner>
-cudaError_t launch_rows(const FfnJob& j, bool even, cudaStream_t stream) {
+template <typename T, int kTokens, bool kEven, bool kInner>
+cudaError_t launch_warps(const FfnJob& j, cudaStream_t stream) {
+  constexpr int kFeatures = kFeaturesOf<T, kTokens, kEven>;
   const int64_t warps = (j.F + kFeatures - 1) / kFeatures, blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
   // the tokens' groups of the same features side by side: they share the weights in L2
   const dim3 grid(static_cast<unsigned>((j.T + kTokens - 1) / kTokens), static_cast<unsigned>(blocks));
   count_launch();
-  if constexpr (sizeof(T) == 2 && kTokens > 2)  // uneven rows of 16 bits: up to two tokens
-    ffn_rows_kernel<T, kTokens, true, kInner><<<grid, kThreads, 0, stream>>>(j);
-  else if (even)
-    ffn_rows_kernel<T, kTokens, true, kInner><<<grid, kThreads, 0, stream>>>(j);
-  else
-    ffn_rows_kernel<T, kTokens, false, kInner><<<grid, kThreads, 0, stream>>>(j);
+  ffn_rows_kernel<T, kTokens, kEven, kInner><<<grid, kThreads, 0, stream>>>(j);
   return cudaGetLastError();
+}
+template <typename T, int kTokens, bool kInner>
+cudaError_t launch_rows(const FfnJob& j, bool even, cudaStream_t stream) {
+  if constexpr (sizeof(T) == 4 || kTokens <= 2) {  // uneven rows of 16 bits: up to two tokens
+    if (!even) return launch_warps<T, kTokens, false, kInner>(j, stream);
+  }
+  return launch_warps<T, kTokens, true, kInner>(j, stream);
 }
 template <typename T, bool kInner>
 cudaError_t launch_few(const FfnJob& j, bool even, cudaStream_t stream) {

@@ -14,7 +14,7 @@ cudaError_t launch_ffn_parts(FfnJob job, bool grad, void* workspace, cudaStream_
 
 // A few tokens: products of any type (f32, or up to four tokens), f32 gradients of up to kFewGradTokens.
 // even: rows of x and the weights start on 16 bytes.
-constexpr int64_t kFewGradTokens = 8, kFewMostFeatures = int64_t(65535) * 16;
+constexpr int64_t kFewGradTokens = 8, kFewMostFeatures = int64_t(65535) * 8;
 cudaError_t launch_ffn_few(const FfnJob& job, bool even, cudaStream_t stream);
 size_t ffn_few_workspace(int64_t T, int64_t H, int64_t F);
 cudaError_t launch_ffn_few_grad(FfnJob job, void* workspace, cudaStream_t stream);
