@@ -35,13 +35,29 @@ struct Activation<SF_ACT_SILU, kFast> {
 
 template <bool kFast>
 struct Activation<SF_ACT_GELU, kFast> {
-  // (1 + erf(g / sqrt 2)) / 2 = erfc(-g / sqrt 2) / 2, which does not cancel for negative g
-  static __device__ __forceinline__ float part(float g) { return 0.5f * erfcf(-0.70710678f * g); }
-  static __device__ __forceinline__ float value(float g) { return g * part(g); }
+  // (1 + erf(g / sqrt 2)) / 2 = erfc(-g / sqrt 2) / 2, which does not cancel for negative
+  // g, and e = exp(-g^2 / 2).  For 16 bits erfc by a polynomial times e (Abramowitz and
+  // Stegun, Handbook of Mathematical Functions, 7.1.26: within 1.5e-7).
+  static __device__ __forceinline__ float part(float g, float& e) {
+    e = exp_of<kFast>(-0.5f * g * g);
+    if (!kFast) return 0.5f * erfcf(-0.70710678f * g);
+    const float t = quotient<true>(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(g), 1.f));
+    float p = fmaf(t, 1.061405429f, -1.453152027f);
+    p = fmaf(t, p, 1.421413741f);
+    p = fmaf(t, p, -0.284496736f);
+    p = fmaf(t, p, 0.254829592f);
+    const float tail = 0.5f * t * p * e;
+    return g < 0.f ? tail : 1.f - tail;
+  }
+  static __device__ __forceinline__ float value(float g) {
+    float e;
+    return g * part(g, e);
+  }
   static __device__ __forceinline__ void both(float g, float& a, float& slope) {
-    const float c = part(g);
+    float e;
+    const float c = part(g, e);
     a = g * c;
-    slope = c + 0.39894228f * g * exp_of<kFast>(-0.5f * g * g);
+    slope = c + 0.39894228f * g * e;
   }
 };
 
