@@ -234,15 +234,28 @@ __global__ void __launch_bounds__(kThreads) ffn_few_dx_kernel(const FfnJob j, fl
     if (t < j.T) store_part<kEven>(parts + (blockIdx.y * j.T + t) * j.H, c0, j.H, sum[t]);
 }
 
-// The slabs' parts added up, in their order.
+// The slabs' parts added up, every kQuarters-th by a thread, in a fixed order.
+constexpr int kQuarters = 4, kSums = kThreads / kQuarters;
 __global__ void __launch_bounds__(kThreads) ffn_few_sum_kernel(const FfnJob j, const float* parts, int slabs) {
-  const int64_t all = j.T * j.H, step = int64_t(gridDim.x) * kThreads;
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < all; i += step) {
+  __shared__ float sums[kQuarters][kSums];
+  const int quarter = threadIdx.x / kSums, at = threadIdx.x % kSums;
+  const int64_t all = j.T * j.H;
+  for (int64_t i0 = int64_t(blockIdx.x) * kSums; i0 < all; i0 += int64_t(gridDim.x) * kSums) {
+    const int64_t i = i0 + at;
     float s = 0.f;
+    if (i < all) {
 #pragma unroll 16
-    for (int k = 0; k < slabs; ++k) s += parts[k * all + i];
-    const int64_t t = i / j.H;
-    static_cast<float*>(j.dx)[t * j.lddx + i - t * j.H] = s;
+      for (int k = quarter; k < slabs; k += kQuarters) s += parts[k * all + i];
+    }
+    sums[quarter][at] = s;
+    __syncthreads();
+    if (quarter == 0 && i < all) {
+#pragma unroll
+      for (int q = 1; q < kQuarters; ++q) s += sums[q][at];
+      const int64_t t = i / j.H;
+      static_cast<float*>(j.dx)[t * j.lddx + i - t * j.H] = s;
+    }
+    __syncthreads();
   }
 }
 
@@ -307,7 +320,7 @@ cudaError_t launch_grad(const FfnJob& j, float* parts, cudaStream_t stream) {
       ffn_few_dx_kernel<kTokens, true><<<grid, kThreads, 0, stream>>>(j, parts, slab);
     else
       ffn_few_dx_kernel<kTokens, false><<<grid, kThreads, 0, stream>>>(j, parts, slab);
-    const int64_t blocks = (j.T * j.H + kThreads - 1) / kThreads;
+    const int64_t blocks = (j.T * j.H + kSums - 1) / kSums;
     ffn_few_sum_kernel<<<static_cast<unsigned>(std::min<int64_t>(blocks, int64_t(sm_count()) * 8)), kThreads, 0, stream>>>(
         j, parts, static_cast<int>(slabs));
     e = cudaGetLastError();

@@ -470,6 +470,15 @@ size_t split_smem(int N, int C, int blocks) {
   return 1024 + std::max({sums, room, split_stages(N, C, blocks) * (kABytes + size_t(N) * kDepthBytes)});
 }
 
+int split_per_sm(int N, int C, int blocks) {
+  return std::max<int>(1, static_cast<int>(kSmemMost / (split_smem(N, C, blocks) + 2048)));
+}
+// CTAs that run at once with `per_sm` on an SM: clusters of four and eight do not fill every
+// group of some 19 SMs.
+int64_t split_slots(int C, int per_sm) {
+  return C == 8 ? (per_sm == 1 ? 120 : per_sm * 19 / 8 * 64) : per_sm * (C == 4 ? 144 : sm_count());
+}
+
 template <typename T, int kProduct>
 cudaError_t launch_pairs(const FfnJob& j, Shape s, cudaStream_t stream) {
   Maps maps;
@@ -502,12 +511,18 @@ cudaError_t launch_split(const FfnJob& j, Shape s, int C, cudaStream_t stream) {
   if (!make_maps<kProduct>(maps, j, s.N)) return cudaErrorUnknown;
   s.columns = columns_of(s.N);
   s.stages = split_stages(s.N, C, s.blocks);
-  const size_t smem = split_smem(s.N, C, s.blocks);
+  size_t smem = split_smem(s.N, C, s.blocks);
+  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
+  if (tiles * C >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
+  // clusters are placed side by side on an SM while it has room: no more room than the fewest
+  // that run at once need (100 x 512 x 2048, C = 4: 9.1 -> 8.0 us)
+  const int most = split_per_sm(s.N, C, s.blocks);
+  int per_sm = 1;
+  while (per_sm < most && split_slots(C, per_sm) < tiles * C) ++per_sm;
+  if (per_sm < most) smem = std::max(smem, kSmemMost / per_sm - 2048);
   const auto kernel = ffn_split_kernel<T, kProduct>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
-  if (tiles * C >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * C));
   cfg.blockDim = dim3(kSplitThreads);
@@ -556,15 +571,16 @@ Choice choose(int64_t M, int64_t Nall, int blocks, int64_t bytes) {
     const int N = width(kProduct == kDw ? 64 : 16);
     const int64_t n_tiles = ceil_div(Nall, N), tiles = ceil_div(M, L::kRows) * n_tiles * two;
     for (int C = 1; C <= 8 && (C == 1 || blocks >= 2 * C); C *= 2) {
-      const int per_sm = std::max<int>(1, static_cast<int>(kSmemMost / (split_smem(N, C, blocks) + 2048)));
-      // clusters of four and eight do not fill every group of SMs
-      const double slots = per_sm * (C == 8 ? 120 : C == 4 ? 144 : sms), ctas = double(tiles * C);
-      const double at_once = std::min<double>(per_sm, std::ceil(ctas / sms));
+      const int per_sm = split_per_sm(N, C, blocks);
+      const double slots = double(split_slots(C, per_sm)), ctas = double(tiles * C), waves = std::ceil(ctas / slots);
+      const double share = ctas / sms;  // of an SM, on the average; the fullest has more
+      const double at_once = std::min<double>(per_sm, std::max(1.0, (share + std::ceil(share)) / 2));
       const double sum = double(ceil_div(blocks, C)) * block_us(N) * at_once;
       // bytes on their way: 2.3 us of them make the rate of memory
       const double way = std::min(ctas, slots) * split_stages(N, C, blocks) * (kABytes + double(N) * kDepthBytes);
       const double reads = std::max(least, double(bytes) / (way / 2.3));
-      const double us = 4.5 + std::max(reads, std::ceil(ctas / slots) * (sum + 1.0 + (C > 1 ? 0.015 : 0.008) * N));
+      const double us = 4.5 + std::max(reads + 4.0 * (waves - 1), waves * (sum + 1.0 + (C > 1 ? 0.015 : 0.008) * N)) +
+                        (C == 8 ? 2.4 : C == 4 ? 1.6 : C == 2 ? 0.8 : 0.0);
       if (us < best.us) best = {false, N, static_cast<int>(n_tiles), C, us};
     }
   }
