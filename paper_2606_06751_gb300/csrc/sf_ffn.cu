@@ -24,45 +24,77 @@ struct Spread {
   uint4* to[3];
   int64_t rows[3], ld[3];
 };
+// Eight 16-bit values from `off` in two 16-byte words; off is one number for the warp.
+__device__ __forceinline__ uint4 eight_from(const uint4& a, const uint4& b, int off) {
+  uint32_t w[5];
+  switch (off >> 1) {
+    case 0: w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x; break;
+    case 1: w[0] = a.y, w[1] = a.z, w[2] = a.w, w[3] = b.x, w[4] = b.y; break;
+    case 2: w[0] = a.z, w[1] = a.w, w[2] = b.x, w[3] = b.y, w[4] = b.z; break;
+    default: w[0] = a.w, w[1] = b.x, w[2] = b.y, w[3] = b.z, w[4] = b.w;
+  }
+  if (off & 1) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // A warp a run of 128 packs of a row.  A pack's 8 values lie in two of the source's
-// 16-byte words; the second is the next lane's first, read once more.
+// 16-byte words; the second is the next lane's first, read once more.  Bound by memory
+// with all reads of a run on their way at once.
 __global__ void __launch_bounds__(kThreads) ffn_spread_kernel(const __grid_constant__ Spread s, int64_t len, int packs,
                                                               int runs) {
+  constexpr int kPacks = 4;
   griddep_launch_dependents();
   const int part = blockIdx.y, lane = threadIdx.x & 31;
-  const int64_t all = s.rows[part] * runs, step = int64_t(gridDim.x) * (kThreads / 32);
-  const int64_t last = s.rows[part] * int64_t(s.ld[part]) - (s.ld[part] - len);  // values from the first to the last
-  for (int64_t i = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); i < all; i += step) {
-    const int64_t r = i / runs;
-    const int run = static_cast<int>(i - r * runs);
-    const unsigned short* row = s.from[part] + r * s.ld[part];
+  const int64_t rows = s.rows[part], ld = s.ld[part], step = int64_t(gridDim.x) * (kThreads / 32);
+  const int64_t first = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  const unsigned short *from = s.from[part], *end = from + (rows - 1) * ld + len;  // behind the last value
+  int64_t r = first / runs;
+  int run = static_cast<int>(first - r * runs);
+  const int64_t rows_on = step / runs;
+  const int runs_on = static_cast<int>(step - rows_on * runs);
+  while (r < rows) {
+    const unsigned short* row = from + r * ld;
     const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 7u);
-    uint4* to = s.to[part] + r * packs;
-#pragma unroll 4
-    for (int p = run * 128 + lane; p < min(packs, run * 128 + 128); p += 32) {
-      const int64_t c = int64_t(p) * 8;
-      const int64_t at = r * s.ld[part] + c - off;  // of the first word
-      uint32_t w[9] = {0};
-      if (at >= 0 && at + 16 <= last) {
-        const uint4 a = load16(row + c - off), b = off != 0 ? load16(row + c - off + 8) : a;
-        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
-        w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-        // by `off` values: whole words, then half a word
-        const int words = off >> 1;
+    const int p = run * (32 * kPacks) + lane;
+    const unsigned short* at = row + int64_t(p) * 8 - off;
+    uint4* to = s.to[part] + r * packs + p;
+    uint4 a[kPacks], b[kPacks];
+    bool whole[kPacks];
 #pragma unroll
-        for (int k = 0; k < 5; ++k) w[k] = words == 0 ? w[k] : words == 1 ? w[k + 1] : words == 2 ? w[k + 2] : w[min(k + 3, 8)];
-        if (off & 1) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t lo = c + 2 * k < len ? row[c + 2 * k] : 0u, hi = c + 2 * k + 1 < len ? row[c + 2 * k + 1] : 0u;
-          w[k] = lo | hi << 16;
-        }
+    for (int k = 0; k < kPacks; ++k) {
+      const unsigned short* q = at + k * 256;
+      whole[k] = p + k * 32 < packs && q >= from && q + 16 <= end;
+      if (whole[k]) {
+        a[k] = *reinterpret_cast<const uint4*>(q);
+        b[k] = off != 0 ? *reinterpret_cast<const uint4*>(q + 8) : a[k];  // from L1
       }
-      to[p] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+#pragma unroll
+    for (int k = 0; k < kPacks; ++k) {
+      if (p + k * 32 >= packs) break;
+      uint4 v;
+      if (whole[k]) {
+        v = eight_from(a[k], b[k], off);
+      } else {
+        const int64_t c = int64_t(p + k * 32) * 8;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t lo = c + 2 * i < len ? row[c + 2 * i] : 0u, hi = c + 2 * i + 1 < len ? row[c + 2 * i + 1] : 0u;
+          w[i] = lo | hi << 16;
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      to[k * 32] = v;
+    }
+    r += rows_on;
+    run += runs_on;
+    if (run >= runs) {
+      run -= runs;
+      ++r;
     }
   }
 }
