@@ -315,15 +315,13 @@ cudaError_t launch_grad(const FfnJob& j, float* parts, cudaStream_t stream) {
   const int64_t slabs = (j.F + slab - 1) / slab;
   const dim3 grid(static_cast<unsigned>((j.H + kBlock - 1) / kBlock), static_cast<unsigned>(slabs));
   if (e == cudaSuccess && j.dx != nullptr) {
-    count_launch(2);
+    count_launch();
     if (weights)
       ffn_few_dx_kernel<kTokens, true><<<grid, kThreads, 0, stream>>>(j, parts, slab);
     else
       ffn_few_dx_kernel<kTokens, false><<<grid, kThreads, 0, stream>>>(j, parts, slab);
-    const int64_t blocks = (j.T * j.H + kSums - 1) / kSums;
-    ffn_few_sum_kernel<<<static_cast<unsigned>(std::min<int64_t>(blocks, int64_t(sm_count()) * 8)), kThreads, 0, stream>>>(
-        j, parts, static_cast<int>(slabs));
     e = cudaGetLastError();
+    if (e == cudaSuccess) e = launch_ffn_sum(j, parts, static_cast<int>(slabs), stream);
   }
   if (e == cudaSuccess && j.dw_gate != nullptr) {
     count_launch();
@@ -337,6 +335,14 @@ cudaError_t launch_grad(const FfnJob& j, float* parts, cudaStream_t stream) {
 }
 
 }  // namespace
+
+cudaError_t launch_ffn_sum(const FfnJob& j, const float* parts, int slabs, cudaStream_t stream) {
+  const int64_t blocks = (j.T * j.H + kSums - 1) / kSums;
+  count_launch();
+  ffn_few_sum_kernel<<<static_cast<unsigned>(std::min<int64_t>(blocks, int64_t(sm_count()) * 8)), kThreads, 0, stream>>>(
+      j, parts, slabs);
+  return cudaGetLastError();
+}
 
 cudaError_t launch_ffn_few(const FfnJob& j, bool even, cudaStream_t stream) {
   return j.dtype == SF_F32    ? launch_few<float, false>(j, even, stream)

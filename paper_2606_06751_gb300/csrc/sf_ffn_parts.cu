@@ -79,7 +79,15 @@ struct Shape {
   int64_t m_tiles, n_tiles;  // dW: n tiles of one of the two matrices
   int N, stages;
   int blocks, half;  // blocks of 64 k; dx: those of the first half
+  int splits;        // dx: ways in which the blocks of a tile are shared out, else 1
+  float* sums;       // [splits][T][H] where splits > 1
 };
+
+// A split's blocks.
+__device__ __forceinline__ void blocks_of(const Shape& s, int split, int& first, int& last) {
+  first = static_cast<int>(int64_t(s.blocks) * split / s.splits);
+  last = static_cast<int>(int64_t(s.blocks) * (split + 1) / s.splits);
+}
 
 __device__ __forceinline__ void part_copy(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t part,
                                           uint32_t bar) {
@@ -150,7 +158,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
   const uint32_t rank = cluster_rank();
   const int half_n = s.N / 2;
   const uint32_t b_bytes = uint32_t(half_n) * kDepthBytes, stage_bytes = 3 * (kABytes + b_bytes);
-  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
+  // the splits of a tile one after another: they run at once
+  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1) * s.splits;
   const int64_t pairs = gridDim.x / 2;
 
   if (tid == 0) {
@@ -185,8 +194,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += pairs) {
         int64_t m, n;
         bool second;
-        tile_of<kProduct>(tile, s.m_tiles, s.n_tiles, s.N, m, n, second);
-        for (int kb = 0; kb < s.blocks; ++kb) {
+        tile_of<kProduct>(tile / s.splits, s.m_tiles, s.n_tiles, s.N, m, n, second);
+        int first, last;
+        blocks_of(s, static_cast<int>(tile % s.splits), first, last);
+        for (int kb = first; kb < last; ++kb) {
           ok = mbar_wait_bounded(&empty[stage], parity, &abort);
           if (!ok) break;
           const uint32_t a = smem_u32(base) + stage * stage_bytes;
@@ -208,12 +219,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       int64_t run = 0;
       bool ok = true;
       for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += pairs) {
-        for (int kb0 = 0; ok && kb0 < s.blocks; kb0 += kRun, ++run) {
+        int first, last;
+        blocks_of(s, static_cast<int>(tile % s.splits), first, last);
+        for (int kb0 = first; ok && kb0 < last; kb0 += kRun, ++run) {
           const int buf = static_cast<int>(run & 1);
           ok = mbar_wait_bounded(&sums_empty[buf], uint32_t(run >> 1 & 1) ^ 1u, &abort);
           if (!ok) break;
           tensor_fence_after();
-          for (int kb = kb0; kb < min(kb0 + kRun, s.blocks); ++kb) {
+          for (int kb = kb0; kb < min(kb0 + kRun, last); ++kb) {
             ok = mbar_wait_bounded(&full[stage], parity, &abort);
             if (!ok) break;
             tensor_fence_after();
@@ -237,14 +250,17 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     for (int64_t tile = blockIdx.x / 2; tile < tiles; tile += pairs) {
       int64_t m, n;
       bool second;
-      tile_of<kProduct>(tile, s.m_tiles, s.n_tiles, s.N, m, n, second);
+      const int split = static_cast<int>(tile % s.splits);
+      tile_of<kProduct>(tile / s.splits, s.m_tiles, s.n_tiles, s.N, m, n, second);
       m += rank * L::kRows;
+      int first, last;
+      blocks_of(s, split, first, last);
       float sum[kChunks][16];
 #pragma unroll
       for (int c = 0; c < kChunks; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum[c][i] = 0.f;
-      for (int kb0 = 0; kb0 < s.blocks; kb0 += kRun, ++run) {
+      for (int kb0 = first; kb0 < last; kb0 += kRun, ++run) {
         const int buf = static_cast<int>(run & 1);
         // after a timeout garbage, and a status
         if (!mbar_wait_bounded(&sums_full[buf], uint32_t(run >> 1 & 1), &abort) && lane == 0)
@@ -287,6 +303,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
           }
           named_barrier(1 + group * 2 + (q & 1), 64);
           store_gated<float, kProduct>(j, t0, 1, f, 8, g, u, dh);
+        } else if (kProduct == kDx && s.splits > 1) {
+          const int64_t row = m + 32 * q + lane, t = n + at;
+          const int left = row < j.H && t < j.T ? static_cast<int>(min(int64_t(16), j.T - t)) : 0;
+          store_down(s.sums + (split * j.T + t) * j.H + row, j.H, 1, left, sum[c]);
         } else {
           store_plain<float, kProduct>(j, second, m + 32 * q + lane, n + at, 1, 16, sum[c]);
         }
@@ -321,34 +341,40 @@ bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t len, int64_
 constexpr size_t kSmem = 226 * 1024;  // of 227 KB, 1 KB for the barriers
 
 struct Cut {
-  int N, stages;
+  int N, splits;
   int64_t m_tiles, n_tiles;
   double us;
 };
 
-// The width of the tiles by estimated time: a block of 64 k takes an SM the longer of its 24
-// products and its 3 x (16 KB + 64 N) bytes at 48 a clock.
+// The width of the tiles, and for dx, whose sums are long and whose tiles may be few, in how many
+// ways k is split, by estimated time: a block of 64 k takes an SM the longer of its 24 products
+// and its 3 x (16 KB + 64 N) bytes at 48 a clock; sums of splits are written and read once more.
+// 175 x 193 x 5239: the gradient 190 us without splits, 58 with those of dx.
 template <int kProduct>
 Cut cut_of(int64_t M, int64_t Nall, int blocks) {
   const int two = kProduct == kDw ? 2 : 1;
   Cut best = {};
   best.us = 1e30;
   for (int N = kProduct == kDw ? 128 : 32; N <= kMostN; N += 32) {
-    Cut c;
-    c.N = N;
-    c.m_tiles = ceil_div(M, 2 * Layout<kProduct>::kRows);
-    c.n_tiles = ceil_div(Nall, N);
-    const double rounds = double(ceil_div(c.m_tiles * c.n_tiles * two, sm_count() / 2));
-    c.us = 6.0 + 0.02 * N + rounds * (1.0 + blocks * std::max(12.0 * N, 3.0 * (kABytes + 64.0 * N) / 48.0) / 1900.0);
-    if (c.us < best.us) best = c;
+    for (int splits = 1; splits == 1 || (kProduct == kDx && splits <= 16 && blocks >= 4 * splits); splits *= 2) {
+      Cut c;
+      c.N = N;
+      c.splits = splits;
+      c.m_tiles = ceil_div(M, 2 * Layout<kProduct>::kRows);
+      c.n_tiles = ceil_div(Nall, N);
+      const double rounds = double(ceil_div(c.m_tiles * c.n_tiles * two * splits, sm_count() / 2));
+      const double block = std::max(12.0 * N, 3.0 * (kABytes + 64.0 * N) / 48.0) / 1900.0;
+      c.us = 6.0 + 0.02 * N + rounds * (1.0 + double(ceil_div(blocks, splits)) * block) +
+             (splits > 1 ? 3.0 + 8.0 * splits * double(M) * double(Nall) / 6.5e6 : 0.0);
+      if (c.us < best.us) best = c;
+    }
   }
-  const size_t stage = 3 * (kABytes + size_t(best.N / 2) * kDepthBytes);
-  best.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmem - 1024 - kSwapBytes) / stage));
   return best;
 }
+Cut cut_of_dx(int64_t T, int64_t H, int64_t F) { return cut_of<kDx>(H, T, static_cast<int>(2 * ceil_div(F, kBox))); }
 
 template <int kProduct>
-cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
+cudaError_t launch_product(const FfnJob& j, float* sums, cudaStream_t stream) {
   using L = Layout<kProduct>;
   Shape s = {};
   const int64_t k = kProduct == kDx ? j.F : kProduct == kDw ? j.T : j.H;
@@ -356,7 +382,10 @@ cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
   s.blocks = kProduct == kDx ? 2 * s.half : s.half;
   const Cut c = cut_of<kProduct>(L::kGated ? j.F : j.H, kProduct == kDw ? j.F : j.T, s.blocks);
   s.N = c.N;
-  s.stages = c.stages;
+  s.splits = c.splits;
+  s.sums = sums;
+  const size_t stage = 3 * (kABytes + size_t(s.N / 2) * kDepthBytes);
+  s.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmem - 1024 - kSwapBytes) / stage));
   s.m_tiles = c.m_tiles;
   s.n_tiles = c.n_tiles;
   Maps maps;
@@ -377,7 +406,7 @@ cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
   const auto kernel = ffn_parts_kernel<kProduct>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
+  const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1) * s.splits;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * static_cast<unsigned>(std::min<int64_t>(tiles, sm_count() / 2)));
   cfg.blockDim = dim3(kPairThreads);
@@ -389,7 +418,9 @@ cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   count_launch();
-  return cudaLaunchKernelEx(&cfg, kernel, maps, j, s);
+  const cudaError_t launched = cudaLaunchKernelEx(&cfg, kernel, maps, j, s);
+  if (launched != cudaSuccess || s.splits == 1) return launched;
+  return launch_ffn_sum(j, s.sums, s.splits, stream);
 }
 
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
@@ -397,7 +428,11 @@ int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 }  // namespace
 
 size_t ffn_parts_workspace(int64_t T, int64_t H, int64_t F, bool grad) {
-  return 6 * (size_t(T + 2 * F) * size_t(padded(H)) + (grad ? 2 * size_t(T) * size_t(padded(F)) : 0));
+  size_t values = size_t(T + 2 * F) * size_t(padded(H));
+  if (!grad) return 6 * values;
+  values += 2 * size_t(T) * size_t(padded(F));
+  const int splits = cut_of_dx(T, H, F).splits;
+  return (6 * values + 15) / 16 * 16 + (splits > 1 ? 4 * size_t(splits) * size_t(T) * size_t(H) : 0);
 }
 
 cudaError_t launch_ffn_parts(FfnJob j, bool grad, void* workspace, cudaStream_t stream) {
@@ -418,17 +453,20 @@ cudaError_t launch_ffn_parts(FfnJob j, bool grad, void* workspace, cudaStream_t 
     j.ldg = padded(j.F);
     j.dg = at;
     j.du = at + 3 * j.T * j.ldg;
+    at += 6 * j.T * j.ldg;
   }
+  float* sums = reinterpret_cast<float*>(static_cast<char*>(workspace) +
+                                         ((reinterpret_cast<char*>(at) - static_cast<char*>(workspace)) + 15) / 16 * 16);
   const int64_t most = (std::max(j.T, j.F) * runs + kThreads / 32 - 1) / (kThreads / 32);
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(most, int64_t(sm_count()) * 8)), 3);
   count_launch();
   ffn_parts_of_kernel<<<grid, kThreads, 0, stream>>>(s, j.H, static_cast<int>(packs), static_cast<int>(runs));
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  if (!grad) return launch_product<kForward>(j, stream);
-  e = launch_product<kInner>(j, stream);
-  if (e == cudaSuccess && j.dx != nullptr) e = launch_product<kDx>(j, stream);
-  if (e == cudaSuccess && j.dw_gate != nullptr) e = launch_product<kDw>(j, stream);
+  if (!grad) return launch_product<kForward>(j, nullptr, stream);
+  e = launch_product<kInner>(j, nullptr, stream);
+  if (e == cudaSuccess && j.dx != nullptr) e = launch_product<kDx>(j, sums, stream);
+  if (e == cudaSuccess && j.dw_gate != nullptr) e = launch_product<kDw>(j, nullptr, stream);
   return e;
 }
 
