@@ -664,7 +664,7 @@ sf_status sf_gated_ffn_grad(const void* x, int32_t dtype, int64_t T, int64_t H, 
                             int32_t accumulate, void* h, int64_t ldh, void* workspace, size_t workspace_bytes,
                             uint32_t* status, cudaStream_t stream);
 
-/* Workspace bytes of sf_gated_ffn (grad = 0) and sf_gated_ffn_grad (grad = 1).
+/* Workspace bytes of sf_gated_ffn (grad = 0) and sf_gated_ffn_grad (grad = 1) on the current device.
    aligned: 1 if x, w_gate and w_up start on 16 bytes and ldx, ldw are multiples
    of 16 bytes.  0 on bad arguments and for T = 0. */
 size_t sf_gated_ffn_workspace_size(int32_t dtype, int64_t T, int64_t H, int64_t F, int32_t aligned, int32_t grad);

@@ -234,26 +234,27 @@ __global__ void __launch_bounds__(kThreads) ffn_few_dx_kernel(const FfnJob j, fl
     if (t < j.T) store_part<kEven>(parts + (blockIdx.y * j.T + t) * j.H, c0, j.H, sum[t]);
 }
 
-// The slabs' parts added up, every kQuarters-th by a thread, in a fixed order.
+// A job's parts added up, every kQuarters-th by a thread, in a fixed order.
 constexpr int kQuarters = 4, kSums = kThreads / kQuarters;
-__global__ void __launch_bounds__(kThreads) ffn_few_sum_kernel(const FfnJob j, const float* parts, int slabs) {
+__global__ void __launch_bounds__(kThreads) ffn_sum_kernel(const FfnSum j) {
   __shared__ float sums[kQuarters][kSums];
   const int quarter = threadIdx.x / kSums, at = threadIdx.x % kSums;
-  const int64_t all = j.T * j.H;
+  const int64_t all = j.rows * j.len;
   for (int64_t i0 = int64_t(blockIdx.x) * kSums; i0 < all; i0 += int64_t(gridDim.x) * kSums) {
     const int64_t i = i0 + at;
     float s = 0.f;
     if (i < all) {
 #pragma unroll 16
-      for (int k = quarter; k < slabs; k += kQuarters) s += parts[k * all + i];
+      for (int k = quarter; k < j.parts; k += kQuarters) s += j.from[k * j.stride + i];
     }
     sums[quarter][at] = s;
     __syncthreads();
     if (quarter == 0 && i < all) {
 #pragma unroll
       for (int q = 1; q < kQuarters; ++q) s += sums[q][at];
-      const int64_t t = i / j.H;
-      static_cast<float*>(j.dx)[t * j.lddx + i - t * j.H] = s;
+      const int64_t r = i / j.len;
+      float* to = j.to + r * j.ld + i - r * j.len;
+      *to = j.accumulate ? *to + s : s;
     }
     __syncthreads();
   }
@@ -321,7 +322,9 @@ cudaError_t launch_grad(const FfnJob& j, float* parts, cudaStream_t stream) {
     else
       ffn_few_dx_kernel<kTokens, false><<<grid, kThreads, 0, stream>>>(j, parts, slab);
     e = cudaGetLastError();
-    if (e == cudaSuccess) e = launch_ffn_sum(j, parts, static_cast<int>(slabs), stream);
+    if (e == cudaSuccess)
+      e = launch_ffn_sum({parts, j.T * j.H, static_cast<int>(slabs), static_cast<float*>(j.dx), j.T, j.H, j.lddx, false},
+                         stream);
   }
   if (e == cudaSuccess && j.dw_gate != nullptr) {
     count_launch();
@@ -336,11 +339,10 @@ cudaError_t launch_grad(const FfnJob& j, float* parts, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_ffn_sum(const FfnJob& j, const float* parts, int slabs, cudaStream_t stream) {
-  const int64_t blocks = (j.T * j.H + kSums - 1) / kSums;
+cudaError_t launch_ffn_sum(const FfnSum& j, cudaStream_t stream) {
+  const int64_t blocks = (j.rows * j.len + kSums - 1) / kSums;
   count_launch();
-  ffn_few_sum_kernel<<<static_cast<unsigned>(std::min<int64_t>(blocks, int64_t(sm_count()) * 8)), kThreads, 0, stream>>>(
-      j, parts, slabs);
+  ffn_sum_kernel<<<static_cast<unsigned>(std::min<int64_t>(blocks, int64_t(sm_count()) * 8)), kThreads, 0, stream>>>(j);
   return cudaGetLastError();
 }
 

@@ -79,8 +79,8 @@ struct Shape {
   int64_t m_tiles, n_tiles;  // dW: n tiles of one of the two matrices
   int N, stages;
   int blocks, half;  // blocks of 64 k; dx: those of the first half
-  int splits;        // dx: ways in which the blocks of a tile are shared out, else 1
-  float* sums;       // [splits][T][H] where splits > 1
+  int splits;        // dx, dW: ways in which the blocks of a tile are shared out; else 1
+  float* sums;       // [splits][T][H] or [splits][2][F][H] where splits > 1
 };
 
 // A split's blocks.
@@ -303,10 +303,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
           }
           named_barrier(1 + group * 2 + (q & 1), 64);
           store_gated<float, kProduct>(j, t0, 1, f, 8, g, u, dh);
-        } else if (kProduct == kDx && s.splits > 1) {
-          const int64_t row = m + 32 * q + lane, t = n + at;
-          const int left = row < j.H && t < j.T ? static_cast<int>(min(int64_t(16), j.T - t)) : 0;
-          store_down(s.sums + (split * j.T + t) * j.H + row, j.H, 1, left, sum[c]);
+        } else if (s.splits > 1) {
+          const int64_t row = m + 32 * q + lane, column = n + at, columns = kProduct == kDx ? j.T : j.F;
+          const int left = row < j.H && column < columns ? static_cast<int>(min(int64_t(16), columns - column)) : 0;
+          const int64_t matrix = kProduct == kDx ? split : 2 * split + (second ? 1 : 0);
+          store_down(s.sums + (matrix * columns + column) * j.H + row, j.H, 1, left, sum[c]);
         } else {
           store_plain<float, kProduct>(j, second, m + 32 * q + lane, n + at, 1, 16, sum[c]);
         }
@@ -346,17 +347,19 @@ struct Cut {
   double us;
 };
 
-// The width of the tiles, and for dx, whose sums are long and whose tiles may be few, in how many
+// The width of the tiles, and for dx and dW, whose sums may be long and their tiles few, in how many
 // ways k is split, by estimated time: a block of 64 k takes an SM the longer of its 24 products
 // and its 3 x (16 KB + 64 N) bytes at 48 a clock; sums of splits are written and read once more.
-// 175 x 193 x 5239: the gradient 190 us without splits, 58 with those of dx.
+// 175 x 193 x 5239: the gradient 190 us without splits, 58 with those of dx; 1247 x 72 x 993:
+// 66 us without those of dW, 58 with them.
 template <int kProduct>
 Cut cut_of(int64_t M, int64_t Nall, int blocks) {
   const int two = kProduct == kDw ? 2 : 1;
   Cut best = {};
   best.us = 1e30;
   for (int N = kProduct == kDw ? 128 : 32; N <= kMostN; N += 32) {
-    for (int splits = 1; splits == 1 || (kProduct == kDx && splits <= 16 && blocks >= 4 * splits); splits *= 2) {
+    for (int splits = 1; splits == 1 || (!Layout<kProduct>::kGated && splits <= 16 && blocks >= 4 * splits);
+         splits *= 2) {
       Cut c;
       c.N = N;
       c.splits = splits;
@@ -365,13 +368,18 @@ Cut cut_of(int64_t M, int64_t Nall, int blocks) {
       const double rounds = double(ceil_div(c.m_tiles * c.n_tiles * two * splits, sm_count() / 2));
       const double block = std::max(12.0 * N, 3.0 * (kABytes + 64.0 * N) / 48.0) / 1900.0;
       c.us = 6.0 + 0.02 * N + rounds * (1.0 + double(ceil_div(blocks, splits)) * block) +
-             (splits > 1 ? 3.0 + 8.0 * splits * double(M) * double(Nall) / 6.5e6 : 0.0);
+             (splits > 1 ? two * (3.0 + 8.0 * splits * double(M) * double(Nall) / 6.5e6) : 0.0);
       if (c.us < best.us) best = c;
     }
   }
   return best;
 }
-Cut cut_of_dx(int64_t T, int64_t H, int64_t F) { return cut_of<kDx>(H, T, static_cast<int>(2 * ceil_div(F, kBox))); }
+// f32 values that the splits of dx, then of dW, need room for.
+size_t split_values(int64_t T, int64_t H, int64_t F) {
+  const int dx = cut_of<kDx>(H, T, static_cast<int>(2 * ceil_div(F, kBox))).splits;
+  const int dw = cut_of<kDw>(H, F, static_cast<int>(ceil_div(T, kBox))).splits;
+  return std::max(dx > 1 ? size_t(dx) * size_t(T) * size_t(H) : 0, dw > 1 ? 2 * size_t(dw) * size_t(F) * size_t(H) : 0);
+}
 
 template <int kProduct>
 cudaError_t launch_product(const FfnJob& j, float* sums, cudaStream_t stream) {
@@ -420,7 +428,13 @@ cudaError_t launch_product(const FfnJob& j, float* sums, cudaStream_t stream) {
   count_launch();
   const cudaError_t launched = cudaLaunchKernelEx(&cfg, kernel, maps, j, s);
   if (launched != cudaSuccess || s.splits == 1) return launched;
-  return launch_ffn_sum(j, s.sums, s.splits, stream);
+  if (kProduct == kDx)
+    return launch_ffn_sum({s.sums, j.T * j.H, s.splits, static_cast<float*>(j.dx), j.T, j.H, j.lddx, false}, stream);
+  const cudaError_t e1 = launch_ffn_sum(
+      {s.sums, 2 * j.F * j.H, s.splits, static_cast<float*>(j.dw_gate), j.F, j.H, j.lddw, j.accumulate}, stream);
+  if (e1 != cudaSuccess) return e1;
+  return launch_ffn_sum(
+      {s.sums + j.F * j.H, 2 * j.F * j.H, s.splits, static_cast<float*>(j.dw_up), j.F, j.H, j.lddw, j.accumulate}, stream);
 }
 
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
@@ -431,8 +445,7 @@ size_t ffn_parts_workspace(int64_t T, int64_t H, int64_t F, bool grad) {
   size_t values = size_t(T + 2 * F) * size_t(padded(H));
   if (!grad) return 6 * values;
   values += 2 * size_t(T) * size_t(padded(F));
-  const int splits = cut_of_dx(T, H, F).splits;
-  return (6 * values + 15) / 16 * 16 + (splits > 1 ? 4 * size_t(splits) * size_t(T) * size_t(H) : 0);
+  return (6 * values + 15) / 16 * 16 + 4 * split_values(T, H, F);
 }
 
 cudaError_t launch_ffn_parts(FfnJob j, bool grad, void* workspace, cudaStream_t stream) {
@@ -466,7 +479,7 @@ cudaError_t launch_ffn_parts(FfnJob j, bool grad, void* workspace, cudaStream_t 
   if (!grad) return launch_product<kForward>(j, nullptr, stream);
   e = launch_product<kInner>(j, nullptr, stream);
   if (e == cudaSuccess && j.dx != nullptr) e = launch_product<kDx>(j, sums, stream);
-  if (e == cudaSuccess && j.dw_gate != nullptr) e = launch_product<kDw>(j, nullptr, stream);
+  if (e == cudaSuccess && j.dw_gate != nullptr) e = launch_product<kDw>(j, sums, stream);
   return e;
 }
 

@@ -19,7 +19,15 @@ cudaError_t launch_ffn_few(const FfnJob& job, bool even, cudaStream_t stream);
 size_t ffn_few_workspace(int64_t T, int64_t H, int64_t F);
 cudaError_t launch_ffn_few_grad(FfnJob job, void* workspace, cudaStream_t stream);
 
-// dx = the sum of `slabs` matrices [T][H] of f32, one behind the other.
-cudaError_t launch_ffn_sum(const FfnJob& job, const float* parts, int slabs, cudaStream_t stream);
+// The sum of `parts` matrices of rows x len f32, `stride` apart, written or added to rows `ld` apart.
+struct FfnSum {
+  const float* from;
+  int64_t stride;
+  int parts;
+  float* to;
+  int64_t rows, len, ld;
+  bool accumulate;
+};
+cudaError_t launch_ffn_sum(const FfnSum& job, cudaStream_t stream);
 
 }  // namespace sf

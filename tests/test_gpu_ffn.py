@@ -111,7 +111,7 @@ def inputs(T, H, F, dtype, seed, grad=False, pad=0, offset=0):
 SHAPES = [(1, 1, 1), (1, 64, 64), (1, 4096, 300), (2, 8, 16), (3, 1000, 1001), (5, 33, 7), (8, 72, 640), (16, 256, 128),
           (17, 257, 129), (48, 2048, 1024), (64, 64, 8), (100, 520, 1000), (128, 128, 128), (129, 130, 191),
           (255, 96, 65), (256, 1024, 2048), (257, 1001, 333), (300, 512, 700), (513, 64, 1100), (1357, 200, 2731),
-          (2049, 136, 72), (2305, 2296, 1301)]
+          (2049, 136, 72), (2305, 2296, 1301), (8200, 40, 50), (33, 64, 3001)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
