@@ -31,6 +31,9 @@ struct Maps {
   CUtensorMap a0, a1, b0, b1;
 };
 
+// A tile's sums take this much longer than any other wait, at most: 10 us a block (a third of one is measured).
+__device__ __forceinline__ uint64_t sums_limit(const Shape& s) { return kWaitLimitNs + uint64_t(s.blocks) * 10000u; }
+
 __device__ __forceinline__ void prefetch_maps(const Maps& maps) {
   prefetch_tensormap(&maps.a0);
   prefetch_tensormap(&maps.a1);
@@ -106,7 +109,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sums_full[i], 1);
-      mbar_init(&sums_empty[i], 2 * kStoreWarps);
+      mbar_init(&sums_empty[i], 2 * (kStoreWarps + (kProduct == kInner ? 1 : 0)));
     }
     fence_barrier_init();
   }
@@ -187,7 +190,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
     fetch(blockIdx.x / 2);
     for (int64_t tile = blockIdx.x / 2; tile < tiles; tile += pairs, ++done) {
       fetch(tile + pairs);
-      if (!mbar_wait_bounded(&sums_full[done & 1], uint32_t(done >> 1 & 1), &abort)) break;
+      mbar_wait_bounded(&sums_full[done & 1], uint32_t(done >> 1 & 1), &abort, sums_limit(s));
+      // a warp that waits for every phase of a barrier has to hold back the one after next
+      __syncwarp();
+      if (lane == 0) arrive_at(at_rank(&sums_empty[done & 1], 0));
     }
   } else if (warp >= 4) {
     // groups of four warps take chunks of 16 columns in turn; a warp reads the 32 lanes of its quadrant
@@ -204,7 +210,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       T dh_next[8];
       if constexpr (kProduct == kInner)
         load_dh<T>(j, n + 16 * group + (q < 2 ? 0 : 8), 1, m + 32 * (q & 1) + lane, dh_next);
-      const bool ok = mbar_wait_bounded(&sums_full[buf], uint32_t(done >> 1 & 1), &abort);  // else garbage, and a status
+      // else garbage, and a status
+      const bool ok = mbar_wait_bounded(&sums_full[buf], uint32_t(done >> 1 & 1), &abort, sums_limit(s));
       tensor_fence_after();
       const uint32_t at = sums + buf * 256 + (uint32_t(q) << 21);
       const auto give_back = [&] {  // this warp has read its last columns of the tile
@@ -349,7 +356,7 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
     }
     __syncwarp();
   }
-  const bool ok = mbar_wait_bounded(&sums_full, 0, &abort);
+  const bool ok = mbar_wait_bounded(&sums_full, 0, &abort, sums_limit(s));
   tensor_fence_after();
   if (!ok || *static_cast<volatile int*>(&abort)) {  // let copies in flight land
     if (tid == 0) report(j.status, SF_ST_TIMEOUT);
@@ -521,7 +528,9 @@ cudaError_t launch_split(const FfnJob& j, Shape s, int C, cudaStream_t stream) {
   while (per_sm < most && split_slots(C, per_sm) < tiles * C) ++per_sm;
   if (per_sm < most) smem = std::max(smem, kSmemMost / per_sm - 2048);
   const auto kernel = ffn_split_kernel<T, kProduct>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  // one limit for all sizes: calls from other threads set it too
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(kSmemMost - kSmemBarriers));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * C));
