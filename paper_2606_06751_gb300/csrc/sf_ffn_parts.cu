@@ -365,7 +365,7 @@ Cut cut_of(int64_t M, int64_t Nall, int blocks) {
       c.splits = splits;
       c.m_tiles = ceil_div(M, 2 * Layout<kProduct>::kRows);
       c.n_tiles = ceil_div(Nall, N);
-      const double rounds = double(ceil_div(c.m_tiles * c.n_tiles * two * splits, sm_count() / 2));
+      const double rounds = double(ceil_div(c.m_tiles * c.n_tiles * two * splits, sm_pairs()));
       const double block = std::max(12.0 * N, 3.0 * (kABytes + 64.0 * N) / 48.0) / 1900.0;
       c.us = 6.0 + 0.02 * N + rounds * (1.0 + double(ceil_div(blocks, splits)) * block) +
              (splits > 1 ? two * (3.0 + 8.0 * splits * double(M) * double(Nall) / 6.5e6) : 0.0);
@@ -416,7 +416,7 @@ cudaError_t launch_product(const FfnJob& j, float* sums, cudaStream_t stream) {
   if (e != cudaSuccess) return e;
   const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1) * s.splits;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * static_cast<unsigned>(std::min<int64_t>(tiles, sm_count() / 2)));
+  cfg.gridDim = dim3(2 * static_cast<unsigned>(std::min<int64_t>(tiles, sm_pairs())));
   cfg.blockDim = dim3(kPairThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;

@@ -502,7 +502,7 @@ cudaError_t launch_pairs(const FfnJob& j, Shape s, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
-  const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, sm_count() / 2));
+  const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, sm_pairs()));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kPairThreads);
@@ -578,7 +578,7 @@ Choice choose(int64_t M, int64_t Nall, int blocks, int64_t bytes) {
     {
       const int N = width(kProduct == kDw ? 128 : 32);
       const int64_t n_tiles = ceil_div(Nall, N), tiles = ceil_div(M, 2 * L::kRows) * n_tiles * two;
-      const double rounds = double(ceil_div(tiles, sms / 2));
+      const double rounds = double(ceil_div(tiles, sm_pairs()));
       const double us = 5.5 + std::max(least, rounds * std::max(blocks * block_us(N / 2), stores(N))) + stores(N);
       if (us < best.us) best = {true, N, static_cast<int>(n_tiles), 1, us};
     }

@@ -14,6 +14,8 @@ enum Product { kForward, kInner, kDx, kDw };
 constexpr uint32_t kABytes = 128 * kDepthBytes;
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Pairs of SMs; one where there is no device to ask.
+inline int64_t sm_pairs() { return sm_count() > 1 ? sm_count() / 2 : 1; }
 
 template <int kProduct>
 struct Layout {
