@@ -272,6 +272,10 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Its two halves, for what only needs the other CTAs to have started: before the first access to
+// another CTA's shared memory.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 // The address of `p` in the shared memory of CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t at_rank(const void* p, uint32_t rank) {
   uint32_t at;

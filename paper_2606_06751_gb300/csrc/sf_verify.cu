@@ -222,6 +222,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJo
   constexpr int N = Pack<T>::kN;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = static_cast<int>(cluster_size()), rank = static_cast<int>(cluster_rank());
+  cluster_arrive();
   const int64_t b = blockIdx.x / static_cast<unsigned>(C);
   const int V = static_cast<int>(j.V), L = static_cast<int>(j.L);
   const int given = j.length == nullptr ? L : j.length[b], n = min(max(given, 0), L);
@@ -295,6 +296,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJo
       if (!three || even.row != odd.row) keep(odd.row);
     }
     __syncthreads();
+    if (g0 == 0) cluster_wait();  // the others have started
     for (int i = warp; i < all; i += kWarps) {
       Part a = joined_lanes<kGreedy>(lane < kWarps ? warps[i][lane] : nothing(), kWarps, scale);
       a.m = __shfl_sync(kFull, a.m, 0);
