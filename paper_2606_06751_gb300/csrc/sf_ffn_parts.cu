@@ -210,6 +210,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
           }
         }
       }
+      // the last products' arrivals have landed here before this CTA may end
+      for (int i = 0; ok && i < s.stages; ++i) {
+        ok = mbar_wait_bounded(&empty[stage], parity, &abort);
+        if (++stage == s.stages) {
+          stage = 0;
+          parity ^= 1;
+        }
+      }
     }
   } else if (warp == 1) {
     if (rank == 0 && lane == 0) {

@@ -146,6 +146,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
           }
         }
       }
+      // the last products' arrivals have landed here before this CTA may end
+      for (int i = 0; ok && i < s.stages; ++i) {
+        ok = mbar_wait_bounded(&empty[stage], parity, &abort);
+        if (++stage == s.stages) {
+          stage = 0;
+          parity ^= 1;
+        }
+      }
     }
   } else if (warp == 1) {
     if (rank == 0 && lane == 0) {
@@ -334,6 +342,13 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
         mbar_arrive_expect_tx(&full[stage], stage_bytes);
         copy_block<kProduct, 1>(maps, s, kb, static_cast<int>(m), static_cast<int>(n), s.N, second, a, a + kABytes,
                                 smem_u32(&full[stage]));
+        if (++stage == s.stages) {
+          stage = 0;
+          parity ^= 1;
+        }
+      }
+      for (int i = 0; i < s.stages; ++i) {  // the last products' arrivals, before this CTA may end
+        if (!mbar_wait_bounded(&empty[stage], parity, &abort)) break;
         if (++stage == s.stages) {
           stage = 0;
           parity ^= 1;
