@@ -156,17 +156,33 @@ def _stream(stream) -> int:
     return _raw_stream(torch.cuda.current_device())
 
 
-def _hold(tensors, *streams):
-    """Temporaries the binding allocated for work enqueued on `streams`: the
-    caching allocator may reuse their memory only once that work is done."""
-    if all(st is None for st in streams):
-        return
-    cur = torch.cuda.current_stream()
-    for st in streams:
-        if st is not None and st != cur:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(st)
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """Memory for a result of work on `stream` (None: the current one).  It comes from
+    that stream's pool, so that the work follows whatever used the memory before, and
+    stays until the current stream, where the caller reads the result, is done with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    t = _scratch(shape, dtype, device, stream)
+    here = torch.cuda.current_stream()
+    if stream != here:
+        t.record_stream(here)
+    return t
+
+
+def _scratch(shape, dtype, device, stream) -> torch.Tensor:
+    """Memory that only work on `stream` uses, from that stream's pool: freed when the
+    call returns, it goes to later work on the same stream."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _hold(tensors, stream):
+    """Tensors of the caller's that work on `stream` uses: their memory stays until that work is done."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
 
 
 def _check(rc: int, where: str):
@@ -187,8 +203,8 @@ def _d3(d: torch.Tensor):
     return d.shape
 
 
-def _empty(shape, dtype, like: torch.Tensor):
-    return torch.empty(shape, dtype=dtype, device=like.device)
+def _empty(shape, dtype, like: torch.Tensor, stream):
+    return _new(shape, dtype, like.device, stream)
 
 
 def num_windows(t0: int, T: int, W: int) -> int:
@@ -219,11 +235,11 @@ class Frontier:
 def sf_frontier(d, a=None, lead=None, makespan=None, status=None, stream=None, outputs=("a", "lead", "makespan")):
     T, R, S = _d3(d)
     if a is None and "a" in outputs:
-        a = _empty((T, S), torch.int64, d)
+        a = _empty((T, S), torch.int64, d, stream)
     if lead is None and "lead" in outputs:
-        lead = _empty((T, S), torch.int32, d)
+        lead = _empty((T, S), torch.int32, d, stream)
     if makespan is None and "makespan" in outputs:
-        makespan = _empty((T,), torch.int64, d)
+        makespan = _empty((T,), torch.int64, d, stream)
     _check(_lib.sf_frontier(_p(d), T, R, S, _p(a), _p(lead), _p(makespan), _p(status), _stream(stream)),
            "sf_frontier")
     return Frontier(a, lead, makespan)
@@ -235,7 +251,7 @@ def sf_frontier_ties(d, a=None, ties=None, status=None, stream=None):
     T, R, S = _d3(d)
     if a is None:
         a = sf_frontier(d, status=status, stream=stream, outputs=("a",)).a
-    ties = ties if ties is not None else _empty((T, S), torch.int32, d)
+    ties = ties if ties is not None else _empty((T, S), torch.int32, d, stream)
     _check(_lib.sf_frontier_ties(_p(d), T, R, S, _p(a), _p(ties), _p(status), _stream(stream)),
            "sf_frontier_ties")
     return ties
@@ -254,14 +270,14 @@ def sf_window_aggregate(d, W: int, t0: int = 0, X=None, D=None, E=None, C=None, 
                         accumulate: bool = False, want=("E", "C", "step_lead"), status=None, stream=None):
     T, R, S = _d3(d)
     nW = num_windows(t0, T, W)
-    X = X if X is not None else _empty((nW, S), torch.int64, d)
-    D = D if D is not None else _empty((nW,), torch.int64, d)
+    X = X if X is not None else _empty((nW, S), torch.int64, d, stream)
+    D = D if D is not None else _empty((nW,), torch.int64, d, stream)
     if E is None and "E" in want:
-        E = _empty((nW, S, R), torch.int64, d)
+        E = _empty((nW, S, R), torch.int64, d, stream)
     if C is None and "C" in want:
-        C = _empty((nW, S, R), torch.int32, d)
+        C = _empty((nW, S, R), torch.int32, d, stream)
     if step_lead is None and "step_lead" in want:
-        step_lead = _empty((T,), torch.uint8, d)
+        step_lead = _empty((T,), torch.uint8, d, stream)
     _check(_lib.sf_window_aggregate(_p(d), T, R, S, t0, W, _p(X), _p(D), _p(E), _p(C), _p(step_lead),
                                     1 if accumulate else 0, _p(status), _stream(stream)),
            "sf_window_aggregate")
@@ -281,9 +297,9 @@ def sf_topk_suspects(X, E, k: int, stream=None, out: Optional[TopK] = None):
     nW, S = X.shape
     R = E.shape[2] if E is not None else 1
     if out is None:
-        out = TopK(_empty((nW, k), torch.int32, X), _empty((nW, k), torch.int64, X),
-                   None if E is None else _empty((nW, k, 2), torch.int32, X),
-                   None if E is None else _empty((nW, k), torch.int64, X))
+        out = TopK(_empty((nW, k), torch.int32, X, stream), _empty((nW, k), torch.int64, X, stream),
+                   None if E is None else _empty((nW, k, 2), torch.int32, X, stream),
+                   None if E is None else _empty((nW, k), torch.int64, X, stream))
     _check(_lib.sf_topk_suspects(_p(X), _p(E), nW, S, R, k, _p(out.stage), _p(out.stage_value),
                                  _p(out.pair), _p(out.pair_value), _stream(stream)), "sf_topk_suspects")
     return out
@@ -292,7 +308,7 @@ def sf_topk_suspects(X, E, k: int, stream=None, out: Optional[TopK] = None):
 def sf_window_median(d, W: int, m=None, status=None, stream=None):
     T, R, S = _d3(d)
     nW = (T + W - 1) // W
-    m = m if m is not None else _empty((nW, R, S), torch.int64, d)
+    m = m if m is not None else _empty((nW, R, S), torch.int64, d, stream)
     _check(_lib.sf_window_median(_p(d), T, R, S, W, _p(m), _p(status), _stream(stream)), "sf_window_median")
     return m
 
@@ -313,12 +329,12 @@ def sf_direct_gain(d, W: int, m, wall=None, other_stage: int = -1, eta_Q=(1, 20)
     T, R, S = _d3(d)
     nW = (T + W - 1) // W
     if out is None:
-        q = _empty((nW, 6), torch.uint64, d) if (wall is not None or other_stage >= 0) else None
-        out = Evidence(_empty((nW, S), torch.int64, d), _empty((nW, S), torch.int64, d),
-                       _empty((nW,), torch.int64, d), _empty((T,), torch.uint8, d), q)
+        q = _empty((nW, 6), torch.uint64, d, stream) if (wall is not None or other_stage >= 0) else None
+        out = Evidence(_empty((nW, S), torch.int64, d, stream), _empty((nW, S), torch.int64, d, stream),
+                       _empty((nW,), torch.int64, d, stream), _empty((T,), torch.uint8, d, stream), q)
         if lead_credit:
-            out.E = _empty((nW, S, R), torch.int64, d)
-            out.C = _empty((nW, S, R), torch.int32, d)
+            out.E = _empty((nW, S, R), torch.int64, d, stream)
+            out.C = _empty((nW, S, R), torch.int32, d, stream)
     _check(_lib.sf_direct_gain(_p(d), T, R, S, W, _p(m), _p(wall), other_stage, Ratio(*eta_Q), _p(out.X),
                                _p(out.Y), _p(out.D), _p(out.E), _p(out.C), _p(out.step_lead), _p(out.quality),
                                _p(status), _stream(stream)), "sf_direct_gain")
@@ -339,10 +355,10 @@ class Labels:
     D: Optional[torch.Tensor] = None
 
 
-def _label_out(nW, S, like):
-    return Labels(_empty((nW,), torch.int32, like), _empty((nW,), torch.int32, like),
-                  _empty((nW,), torch.int32, like), _empty((nW, S), torch.float64, like),
-                  _empty((nW, S), torch.float64, like))
+def _label_out(nW, S, like, stream):
+    return Labels(_empty((nW,), torch.int32, like, stream), _empty((nW,), torch.int32, like, stream),
+                  _empty((nW,), torch.int32, like, stream), _empty((nW, S), torch.float64, like, stream),
+                  _empty((nW, S), torch.float64, like, stream))
 
 
 def sf_label_gates(T: int, R: int, S: int, W: int, ev: Evidence, role=None, missing=None, cfg=None,
@@ -350,9 +366,9 @@ def sf_label_gates(T: int, R: int, S: int, W: int, ev: Evidence, role=None, miss
     nW = (T + W - 1) // W
     cfg = cfg if cfg is not None else default_config()
     if out is None:
-        out = _label_out(nW, S, ev.X)
-        out.n_confident = _empty((nW,), torch.int32, ev.X)
-        out.n_switch = _empty((nW,), torch.int32, ev.X)
+        out = _label_out(nW, S, ev.X, stream)
+        out.n_confident = _empty((nW,), torch.int32, ev.X, stream)
+        out.n_switch = _empty((nW,), torch.int32, ev.X, stream)
     _check(_lib.sf_label_gates(T, R, S, W, _p(ev.X), _p(ev.Y), _p(ev.D), _p(ev.step_lead), _p(ev.quality),
                                _p(role), _p(missing), ctypes.byref(cfg), _p(out.labels), _p(out.route_mask),
                                _p(out.amb_mask), _p(out.share), _p(out.gain), _p(out.n_confident),
@@ -372,14 +388,13 @@ def sf_label_windows(d, W: int, role=None, missing=None, wall=None, other_stage:
     cfg = cfg if cfg is not None else default_config()
     need = workspace_size(T, R, S, W)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=d.device)
-        _hold([workspace], stream)
+        workspace = _scratch(need, torch.uint8, d.device, stream)
     if out is None:
-        out = _label_out(nW, S, d)
+        out = _label_out(nW, S, d, stream)
         if evidence:
-            out.X = _empty((nW, S), torch.int64, d)
-            out.Y = _empty((nW, S), torch.int64, d)
-            out.D = _empty((nW,), torch.int64, d)
+            out.X = _empty((nW, S), torch.int64, d, stream)
+            out.Y = _empty((nW, S), torch.int64, d, stream)
+            out.D = _empty((nW,), torch.int64, d, stream)
     _check(_lib.sf_label_windows(_p(d), T, R, S, W, _p(role), _p(missing), _p(wall), other_stage,
                                  ctypes.byref(cfg), _p(workspace), workspace.numel(), _p(out.labels),
                                  _p(out.route_mask), _p(out.amb_mask), _p(out.share), _p(out.gain),
@@ -425,15 +440,19 @@ class Streamed:
 
 
 class StreamBuffers:
-    """Device staging, workspace and outputs for sf_stream_windows, reusable across calls."""
+    """Device staging, workspace and outputs for sf_stream_windows, reusable across calls.  Calls on other
+    streams than the current one follow it, or get those streams here."""
 
     def __init__(self, T: int, R: int, S: int, W: int, k: int, chunk_steps: int, device, lead_credit=True,
-                 gathered=False):
+                 gathered=False, stream=None, copy_stream=None):
         nW = (T + W - 1) // W
-        e = lambda shape, dt: torch.empty(shape, dtype=dt, device=device)  # noqa: E731
+        e = lambda shape, dt: _new(shape, dt, device, stream)  # noqa: E731
         self.shape = (T, R, S, W, k, chunk_steps)
         size = _lib.sf_stream_gathered_staging_size if gathered else _lib.sf_stream_windows_staging_size
-        self.staging = e((int(size(T, R, S, chunk_steps)),), torch.uint8)
+        # copies write it first, then `stream` reads it
+        self.staging = _new((int(size(T, R, S, chunk_steps)),), torch.uint8, device, copy_stream)
+        if stream is not None:
+            self.staging.record_stream(stream)
         self.workspace = e((workspace_size(min(chunk_steps, T), R, S, W),), torch.uint8)
         self.out = Streamed(e((nW, S), torch.int64), e((nW, S), torch.int64), e((nW,), torch.int64),
                             e((nW, S, R), torch.int64) if lead_credit else None,
@@ -454,9 +473,7 @@ def sf_stream_windows(h_d: torch.Tensor, W: int, k: int, chunk_steps: int, bufs:
     dev = torch.device("cuda", torch.cuda.current_device())
     cs = copy_stream if copy_stream is not None else (stream if stream is not None else torch.cuda.current_stream())
     if bufs is None:
-        # staging and workspace are used by both streams: keep them until that work is done
-        bufs = StreamBuffers(T, R, S, W, k, chunk_steps, dev)
-        _hold([bufs.staging, bufs.workspace], cs, stream)
+        bufs = StreamBuffers(T, R, S, W, k, chunk_steps, dev, stream=stream, copy_stream=cs)
     o = bufs.out
     _check(_lib.sf_stream_windows(h_d.data_ptr(), T, R, S, W, k, chunk_steps, ctypes.byref(cfg),
                                   _p(bufs.staging), bufs.staging.numel(), _p(bufs.workspace), bufs.workspace.numel(),
@@ -483,8 +500,8 @@ def sf_window_baselines(d, W: int, t0: int = 0, out: Optional[Baselines] = None,
     T, R, S = _d3(d)
     nW = num_windows(t0, T, W)
     if out is None:
-        out = Baselines(_empty((nW, S), torch.int64, d), _empty((nW, S, 2), torch.uint64, d),
-                        _empty((nW, S), torch.int64, d), _empty((nW, S), torch.int64, d))
+        out = Baselines(_empty((nW, S), torch.int64, d, stream), _empty((nW, S, 2), torch.uint64, d, stream),
+                        _empty((nW, S), torch.int64, d, stream), _empty((nW, S), torch.int64, d, stream))
     _check(_lib.sf_window_baselines(_p(d), T, R, S, t0, W, _p(out.M), _p(out.SUM), _p(out.SLOW), _p(out.RANK0),
                                     1 if accumulate else 0, _p(status), _stream(stream)), "sf_window_baselines")
     return out
@@ -505,11 +522,10 @@ def rank_workspace(T: int, R: int, S: int, device) -> torch.Tensor:
 def sf_rank_lag(d, out: Optional[Lag] = None, workspace=None, status=None, stream=None) -> Lag:
     T, R, S = _d3(d)
     if out is None:
-        out = Lag(_empty((T, S), torch.int64, d), _empty((T, S), torch.int64, d), _empty((T, S), torch.int64, d))
+        out = Lag(*(_empty((T, S), torch.int64, d, stream) for _ in range(3)))
     ws = workspace
     if ws is None:
-        ws = rank_workspace(T, R, S, d.device)
-        _hold([ws], stream)
+        ws = _scratch(int(_lib.sf_rank_workspace_size(T, R, S)), torch.uint8, d.device, stream)
     _check(_lib.sf_rank_lag(_p(d), T, R, S, _p(out.L), _p(out.dL), _p(out.G), _p(ws), ws.numel(), _p(status),
                             _stream(stream)), "sf_rank_lag")
     return out
@@ -518,11 +534,10 @@ def sf_rank_lag(d, out: Optional[Lag] = None, workspace=None, status=None, strea
 def sf_raw_spread(d, W: int, t0: int = 0, spread=None, accumulate: bool = False, workspace=None, status=None,
                   stream=None):
     T, R, S = _d3(d)
-    spread = spread if spread is not None else _empty((num_windows(t0, T, W), S), torch.int64, d)
+    spread = spread if spread is not None else _empty((num_windows(t0, T, W), S), torch.int64, d, stream)
     ws = workspace
     if ws is None:
-        ws = rank_workspace(T, R, S, d.device)
-        _hold([ws], stream)
+        ws = _scratch(int(_lib.sf_rank_workspace_size(T, R, S)), torch.uint8, d.device, stream)
     _check(_lib.sf_raw_spread(_p(d), T, R, S, t0, W, _p(spread), 1 if accumulate else 0, _p(ws), ws.numel(),
                               _p(status), _stream(stream)), "sf_raw_spread")
     return spread
@@ -540,7 +555,7 @@ def sf_group_aggregate(d, group, G: int, W: int, t0: int = 0, out: Optional[Grou
     group = _dev(group, torch.int32, "group")
     nW = num_windows(t0, T, W)
     if out is None:
-        out = GroupWindows(_empty((nW, G, S), torch.int64, d), _empty((nW, G), torch.int64, d))
+        out = GroupWindows(_empty((nW, G, S), torch.int64, d, stream), _empty((nW, G), torch.int64, d, stream))
     _check(_lib.sf_group_aggregate(_p(d), T, R, S, _p(group), G, t0, W, _p(out.X), _p(out.D),
                                    1 if accumulate else 0, _p(status), _stream(stream)), "sf_group_aggregate")
     return out
@@ -550,7 +565,7 @@ def sf_stage_group_sum(X, stage_group, K: int, Y=None, stream=None):
     """stage_group: a host sequence of S group ids in [0, K)."""
     nW, S = X.shape
     sg = (ctypes.c_int32 * S)(*[int(v) for v in stage_group])
-    Y = Y if Y is not None else _empty((nW, K), torch.int64, X)
+    Y = Y if Y is not None else _empty((nW, K), torch.int64, X, stream)
     _check(_lib.sf_stage_group_sum(_p(X), nW, S, sg, K, _p(Y), _stream(stream)), "sf_stage_group_sum")
     return Y
 
@@ -566,8 +581,7 @@ def sf_stream_gathered_windows(h_g: torch.Tensor, T: int, R: int, S: int, W: int
     dev = torch.device("cuda", torch.cuda.current_device())
     cs = copy_stream if copy_stream is not None else (stream if stream is not None else torch.cuda.current_stream())
     if bufs is None:
-        bufs = StreamBuffers(T, R, S, W, k, chunk_steps, dev, gathered=True)
-        _hold([bufs.staging, bufs.workspace], cs, stream)
+        bufs = StreamBuffers(T, R, S, W, k, chunk_steps, dev, gathered=True, stream=stream, copy_stream=cs)
     o = bufs.out
     _check(_lib.sf_stream_gathered_windows(h_g.data_ptr(), T, R, S, W, k, chunk_steps, ctypes.byref(cfg),
                                            _p(bufs.staging), bufs.staging.numel(), _p(bufs.workspace),
@@ -582,7 +596,7 @@ def sf_gathered_to_steps(src: torch.Tensor, T: int, R: int, S: int, N: int, dst=
     """src: device int64 holding ceil(T/N) gathered [R][n][S] blocks; returns [T][R][S]."""
     if not src.is_cuda or src.dtype != torch.int64 or not src.is_contiguous() or src.numel() != T * R * S:
         raise TypeError("src must be a contiguous int64 CUDA tensor of T*R*S values")
-    dst = dst if dst is not None else torch.empty((T, R, S), dtype=torch.int64, device=src.device)
+    dst = dst if dst is not None else _empty((T, R, S), torch.int64, src, stream)
     _check(_lib.sf_gathered_to_steps(_p(src), T, R, S, N, _p(dst), _stream(stream)), "sf_gathered_to_steps")
     return dst
 
@@ -592,12 +606,11 @@ def sf_rank_lag_windows(d, W: int, t0: int = 0, Lw=None, Gw=None, accumulate: bo
     """Window sums of the lag and the gap: (Lw, Gw), each [nW][S]."""
     T, R, S = _d3(d)
     nW = num_windows(t0, T, W)
-    Lw = Lw if Lw is not None else _empty((nW, S), torch.int64, d)
-    Gw = Gw if Gw is not None else _empty((nW, S), torch.int64, d)
+    Lw = Lw if Lw is not None else _empty((nW, S), torch.int64, d, stream)
+    Gw = Gw if Gw is not None else _empty((nW, S), torch.int64, d, stream)
     ws = workspace
     if ws is None:
-        ws = rank_workspace(T, R, S, d.device)
-        _hold([ws], stream)
+        ws = _scratch(int(_lib.sf_rank_workspace_size(T, R, S)), torch.uint8, d.device, stream)
     _check(_lib.sf_rank_lag_windows(_p(d), T, R, S, t0, W, _p(Lw), _p(Gw), 1 if accumulate else 0, _p(ws),
                                     ws.numel(), _p(status), _stream(stream)), "sf_rank_lag_windows")
     return Lw, Gw
@@ -655,12 +668,7 @@ def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=No
     _vec(ref_logp, N, torch.float32, "ref_logp")
     _vec(weight, N, torch.float32, "weight")
     _vec(grad_out, 1, torch.float32, "grad_out")
-    device, made = logits.device, []
-
-    def new(n, dtype=torch.float32):
-        made.append(torch.empty(n, dtype=dtype, device=device))
-        return made[-1]
-
+    new = lambda n, dtype=torch.float32: _new(n, dtype, logits.device, stream)  # noqa: E731
     if logp is not None:
         _vec(logp, N, torch.float32, "logp")
     elif "logp" in want:
@@ -678,8 +686,7 @@ def sf_policy_loss(logits, target, old_logp, advantage, ref_logp=None, weight=No
     elif grad:
         dlogits = new((N, V), logits.dtype)
     if workspace is None and (logp is None or N > SF_POLICY_DIRECT_ROWS):
-        workspace = new(_lib.sf_policy_loss_workspace_size(N, V), torch.uint8)
-    _hold(made, stream)
+        workspace = _scratch(_lib.sf_policy_loss_workspace_size(N, V), torch.uint8, logits.device, stream)
     cfg = PolicyConfig(clip[0], clip[1], kl_coef, inv_temperature)
     _check(_lib.sf_policy_loss(_p(logits), _DTYPES[logits.dtype], N, V, ld, _p(target), _p(old_logp), _p(ref_logp),
                                _p(advantage), _p(weight), ctypes.byref(cfg), _p(grad_out), _p(logp), _p(token_loss),
@@ -715,12 +722,7 @@ def sf_route_experts(logits, k: int, bias=None, score: str = "softmax", groups: 
     _vec(bias, E, torch.float32, "bias")
     if accumulate and load is None:
         raise ValueError("accumulate adds to a load that the caller gives")
-    device, made = logits.device, []
-
-    def new(shape, dtype):
-        made.append(torch.empty(shape, dtype=dtype, device=device))
-        return made[-1]
-
+    new = lambda shape, dtype: _new(shape, dtype, logits.device, stream)  # noqa: E731
     slots = T * k if k > 0 else 0  # a bad k is the library's to refuse
     index = new((T, max(k, 0)), torch.int32) if index is None else _vec(index, slots, torch.int32, "index")
     weight = new((T, max(k, 0)), torch.float32) if weight is None else _vec(weight, slots, torch.float32, "weight")
@@ -728,7 +730,6 @@ def sf_route_experts(logits, k: int, bias=None, score: str = "softmax", groups: 
         _vec(load, E, torch.int32, "load")
     elif "load" in want:
         load = new(E, torch.int32)
-    _hold(made, stream)
     cfg = RouteConfig(k, _score(score), groups, top_groups, group_top, 1 if renorm else 0, scale)
     _check(_lib.sf_route_experts(_p(logits), _DTYPES[logits.dtype], T, E, ld, _p(bias), ctypes.byref(cfg), _p(index),
                                  _p(weight), _p(load), 1 if accumulate else 0, _p(status), _stream(stream)),
@@ -747,8 +748,7 @@ def sf_route_experts_grad(logits, index, dweight, score: str = "softmax", renorm
     _vec(dweight, T * k, torch.float32, "dweight")
     ldd = E
     if dlogits is None:
-        dlogits = _empty((T, E), logits.dtype, logits)
-        _hold([dlogits], stream)
+        dlogits = _empty((T, E), logits.dtype, logits, stream)
     else:
         n, m, ldd = _rows(dlogits, "dlogits")
         if (n, m) != (T, E) or dlogits.dtype != logits.dtype:
@@ -793,12 +793,7 @@ def _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, worksp
         out_ptr, out_numel, out_dtype = _tensor_list(list(out), "out")
         if out_numel != numel or out_dtype != dtype:
             raise ValueError("out must have the gradients' sizes and types")
-    made = []
-
-    def new(m, dt=torch.float32):
-        made.append(torch.empty(m, dtype=dt, device=device))
-        return made[-1]
-
+    new = lambda m: _new(m, torch.float32, device, stream)  # noqa: E731
     norm = new(1) if norm is None else _vec(norm, 1, torch.float32, "norm")
     if tensor_norm is not None:
         _vec(tensor_norm, n, torch.float32, "tensor_norm")
@@ -806,15 +801,13 @@ def _grad(grads, out, max_norm, eps, norm, coef, tensor_norm, per_tensor, worksp
         tensor_norm = new(n)
     at = lambda a: a.buffer_info()[0]  # noqa: E731
     if workspace is None and _lib.sf_grad_needs_workspace(at(numel), at(dtype), n):
-        workspace = new(_lib.sf_grad_workspace_size(n), torch.uint8)
+        workspace = _scratch(_lib.sf_grad_workspace_size(n), torch.uint8, device, stream)
     size = 0 if workspace is None else workspace.numel()
     if max_norm is None:
-        _hold(made, stream)
         _check(_lib.sf_grad_norm(at(ptr), at(numel), at(dtype), n, _p(norm), _p(tensor_norm), _p(workspace), size,
                                  _p(status), _stream(stream)), "sf_grad_norm")
         return GradNorm(norm, None, tensor_norm)
     coef = new(1) if coef is None else _vec(coef, 1, torch.float32, "coef")
-    _hold(made, stream)
     _check(_lib.sf_grad_clip(at(ptr), None if out_ptr is None else at(out_ptr), at(numel), at(dtype), n, max_norm, eps,
                              _p(norm), _p(coef), _p(tensor_norm), _p(workspace), size, _p(status), _stream(stream)),
            "sf_grad_clip")
@@ -882,9 +875,9 @@ def _ffn_inputs(x, w_gate, w_up, act: str):
     return T, H, F, ldx, ldw, number, even, px, pg, pu
 
 
-def _ffn_workspace(x, T, H, F, even, grad):
+def _ffn_workspace(x, T, H, F, even, grad, stream):
     n = _lib.sf_gated_ffn_workspace_size(_DTYPES[x.dtype], T, H, F, 1 if even else 0, grad)
-    return None if n == 0 else torch.empty(n, dtype=torch.uint8, device=x.device)
+    return None if n == 0 else _scratch(n, torch.uint8, x.device, stream)
 
 
 def sf_gated_ffn(x, w_gate, w_up, act: str = "silu", h=None, workspace=None, status=None, stream=None) -> torch.Tensor:
@@ -893,11 +886,11 @@ def sf_gated_ffn(x, w_gate, w_up, act: str = "silu", h=None, workspace=None, sta
     T, H, F, ldx, ldw, number, even, px, pg, pu = _ffn_inputs(x, w_gate, w_up, act)
     d = _here((x, w_gate, w_up, h, workspace, status))
     if h is None:
-        h, ldh = torch.empty((T, F), dtype=x.dtype, device=x.device), F
+        h, ldh = _new((T, F), x.dtype, x.device, stream), F
     else:
         ldh = _like_rows(h, (T, F), (x.dtype,), "h")
     if workspace is None:
-        workspace = _ffn_workspace(x, T, H, F, even, 0)
+        workspace = _ffn_workspace(x, T, H, F, even, 0, stream)
     if stream is not None:
         _hold((h, workspace), stream)
     _check(_lib.sf_gated_ffn(px, _DTYPES[x.dtype], T, H, ldx, pg, pu, F, ldw, number, h.data_ptr(), ldh, _p(workspace),
@@ -929,7 +922,7 @@ def sf_gated_ffn_grad(x, w_gate, w_up, dh, act: str = "silu", dx=None, dw_gate=N
     if dx is not None:
         lddx = _like_rows(dx, (T, H), (dtype,), "dx")
     elif "dx" in want:
-        dx = torch.empty((T, H), dtype=dtype, device=device)
+        dx = _new((T, H), dtype, device, stream)
     if dw_gate is not None:
         lddw = _like_rows(dw_gate, (F, H), (dtype, torch.float32), "dw_gate")
         if _like_rows(dw_up, (F, H), (dw_gate.dtype,), "dw_up") != lddw:
@@ -941,14 +934,14 @@ def sf_gated_ffn_grad(x, w_gate, w_up, dh, act: str = "silu", dx=None, dw_gate=N
             dw_dtype = dtype
         elif dw_dtype is not dtype and dw_dtype is not torch.float32:
             raise ValueError("dw_dtype must be x's type or float32")
-        dw_gate = torch.empty((F, H), dtype=dw_dtype, device=device)
-        dw_up = torch.empty((F, H), dtype=dw_dtype, device=device)
+        dw_gate = _new((F, H), dw_dtype, device, stream)
+        dw_up = _new((F, H), dw_dtype, device, stream)
     if h is not None:
         ldh = _like_rows(h, (T, F), (dtype,), "h")
     elif "h" in want:
-        h = torch.empty((T, F), dtype=dtype, device=device)
+        h = _new((T, F), dtype, device, stream)
     if workspace is None:
-        workspace = _ffn_workspace(x, T, H, F, even, 1)
+        workspace = _ffn_workspace(x, T, H, F, even, 1, stream)
     if stream is not None:
         _hold((dx, dw_gate, dw_up, h, workspace), stream)
     _check(_lib.sf_gated_ffn_grad(px, _DTYPES[dtype], T, H, ldx, pg, pu, F, ldw, number, dh.data_ptr(), lddh, _p(dx), lddx,
@@ -972,9 +965,7 @@ def sf_dropout(x, p: float, key, residual=None, out=None, stream=None) -> torch.
     if residual is not None:
         ldr = _like_rows(residual, (N, D), (dtype,), "residual")
     if out is None:
-        out = torch.empty((N, D), dtype=dtype, device=x.device)
-        if stream is not None:
-            _hold((out,), stream)
+        out = _new((N, D), dtype, x.device, stream)
     else:
         ldo = _like_rows(out, (N, D), (dtype,), "out")
     _check(_lib.sf_dropout(x.data_ptr(), _DTYPES[dtype], N, D, ldx, p, key.data_ptr(), _p(residual), ldr, out.data_ptr(),
@@ -1029,17 +1020,17 @@ def sf_verify_draft(target, token, draft=None, lengths=None, uniform=None, noise
         raise ValueError("uniform and noise go together")
     d = _here((target, token, draft, lengths, uniform, noise, out_token, accepted, logp, status))
     if out_token is None:
-        out_token = torch.empty((B, L + 1), dtype=torch.int64, device=device)
+        out_token = _new((B, L + 1), torch.int64, device, stream)
     else:
         _vec(out_token, B * (L + 1), torch.int64, "out_token")
     if accepted is None:
-        accepted = torch.empty(B, dtype=torch.int32, device=device)
+        accepted = _new(B, torch.int32, device, stream)
     else:
         _vec(accepted, B, torch.int32, "accepted")
     if logp is not None:
         _vec(logp, B * (L + 1), torch.float32, "logp")
     elif "logp" in want:
-        logp = torch.empty((B, L + 1), dtype=torch.float32, device=device)
+        logp = _new((B, L + 1), torch.float32, device, stream)
     if stream is not None:
         _hold((out_token, accepted, logp), stream)
     _check(_lib.sf_verify_draft(target.data_ptr(), _DTYPES[dtype], B, L, V, ldt, _p(draft), ldq, token.data_ptr(),
