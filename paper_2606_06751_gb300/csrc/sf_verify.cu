@@ -39,6 +39,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
 __device__ __forceinline__ uint64_t place_key(uint32_t value, int at) {
   return uint64_t(value) << 32 | (0xffffffffu - static_cast<uint32_t>(at));
 }
+constexpr uint64_t kUndrawn = 1;  // below all keys: there are values above 0, but none can be drawn
 __device__ __forceinline__ int place_of(uint64_t key) {
   return static_cast<int>(0xffffffffu - static_cast<uint32_t>(key));
 }
@@ -187,11 +188,11 @@ struct Stop {
   int last;      // greedy: the next token; 3: the drafted token
 };
 
-// The largest r_j / e_j a thread has met, r_j = p_j - q_j as `form` says; its
-// indices rise, so the first of equal ones stays.
+// The largest r_j / e_j a thread has met, r_j = p_j - q_j as `form` says, and the
+// largest r_j; its indices rise, so the first of equal ones stays.
 struct Race {
-  float best = 0.f;
-  int at = -1;
+  float best, top;
+  int at;
   float m, by, mq, byq, scale;  // maxima, reciprocal sums
   int form, token;
   __device__ __forceinline__ void run(float z, float zq, float e, int j) {
@@ -199,6 +200,7 @@ struct Race {
     float r = __fmul_rn(exp2_fast((z - m) * scale), by);
     if (form == 2) r = __fsub_rn(r, __fmul_rn(exp2_fast((zq - mq) * scale), byq));
     if (form == 3 && j == token) r = 0.f;
+    top = fmaxf(top, r);
     const float v = __fdividef(r, e);
     if (v > best && e > 0.f) {
       best = v;
@@ -372,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJo
                        15u) == 0;
     uint64_t best = 0;
     for (;;) {
-      race.best = 0.f;
+      race.best = race.top = 0.f;
       race.at = -1;
       int rest = 0;
       if (even) {  // whole packs of the three rows side by side
@@ -401,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJo
         for (int q = from + tid; q < to; q += kThreads)
           race.run(to_f32(z[q]), race.form == 2 ? to_f32(zq[q]) : 0.f, e[q], q);
       }
-      best = race.at >= 0 ? place_key(__float_as_uint(race.best), race.at) : 0;
+      best = race.at >= 0 ? place_key(__float_as_uint(race.best), race.at) : race.top > 0.f ? kUndrawn : 0;
       best = warp_max_u64(best);
       if (lane == 0) warps_best[warp] = best;
       __syncthreads();
@@ -414,10 +416,10 @@ __global__ void __launch_bounds__(kThreads, kPerSm) verify_kernel(const VerifyJo
       best = 0;
       for (int c = 0; c < C; ++c) best = best_of[c] > best ? best_of[c] : best;
       cluster_sync();  // all have read before a second race writes
-      if (best != 0 || race.form != 2) break;
+      if (best != 0 || race.form == 1) break;
       race.form = 1;  // no residual above 0
     }
-    next = best != 0 ? place_of(best) : -1;
+    next = best > kUndrawn ? place_of(best) : -1;
   }
   if (rank != 0) return;
   if (next < 0) bits |= SF_ST_NONFINITE;
