@@ -324,12 +324,13 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
     mbar_init(&sums_full, 1);
     fence_barrier_init();
   }
-  griddep_launch_dependents();
+  // columns between the kernel before and the one behind: neither can wait for them while this one waits for it
+  griddep_wait();
   if (warp == 2) tensor_alloc<1>(&tensor_at, s.columns);
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();
-  griddep_wait();
+  griddep_launch_dependents();
   const uint32_t sums = tensor_at;
 
   if (warp == 0) {

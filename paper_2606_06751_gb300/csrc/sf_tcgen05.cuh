@@ -60,9 +60,12 @@ __device__ __forceinline__ void products_arrive(uint64_t* bar) {
                  : "memory");
 }
 
-// One warp; waits while other CTAs of the SM hold the columns.  So that no two kernels
-// can wait for each other's columns, a CTA either waits for no other CTA while it holds
-// some, or takes all shared memory of its SM with them.
+// One warp; waits while other CTAs of the SM hold the columns.  So that no two kernels,
+// of this library or another, can wait for each other's columns, a CTA either takes all
+// shared memory of its SM with them, or waits for no other CTA while it holds some: it
+// allocates behind griddep_wait, lets the next kernel start (griddep_launch_dependents)
+// when all its warps know that the columns are there, and gives them back before it waits
+// for its cluster.
 template <int kCtas>
 __device__ __forceinline__ void tensor_alloc(uint32_t* at, uint32_t columns) {
   if constexpr (kCtas == 2) {
