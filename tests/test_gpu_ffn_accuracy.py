@@ -7,9 +7,15 @@ its type.  Before that it is in f32 with the hardware's exponential: 2 + 1.2 |x|
 units of 2^-23 for an argument x.  For silu and gelu |x| is at most 72 here, 1.1e-5,
 with 5e-6 for gelu's polynomial: within 2^-15 of the value.  For gelu by tanh |x| is at
 most 81, 1.2e-5, and the argument's own roundings, four of 2^-24 of it, make 2e-5 more:
-within 2^-14.  A slope's terms may cancel: the same share of the sum of their sizes."""
+within 2^-14.  A slope's terms may cancel: the same share of the sum of their sizes.
+
+f32.  Errors as roots of the mean square against ffn_bounds, which a lost product of
+parts breaks, and inputs whose sums lie in the lower parts alone.  In the tails the
+exact functions' errors and their arguments' roundings, in units of 2^-24, with one
+each for the products behind them."""
 import math
 
+import ffn_bounds
 import pytest
 import torch
 
@@ -67,3 +73,69 @@ def test_tails(sf, T, act, dtype):
             off = (got.double() - want).abs()
             bound = own * near + half * (want.abs() + own * near) + tiny
             assert bool((off <= bound).all()), (u, float((off / bound).max()), float(g[int((off / bound).argmax())]))
+
+
+def f32_inputs(T, H, F, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    n = lambda *s, k=1.0: torch.randn(s, generator=gen, device="cuda") * k  # noqa: E731
+    return n(T, H), n(F, H, k=H ** -0.5), n(F, H, k=H ** -0.5), n(T, F, k=0.0625)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("T,H,F", [(1, 4096, 300), (3, 2001, 700), (8, 520, 640), (20, 1000, 257), (32, 2048, 1024), (33, 512, 300),
+                                   (64, 256, 512), (175, 193, 5239), (300, 1001, 333), (1247, 72, 993), (2305, 2296, 130)])
+def test_f32_errors(sf, T, H, F, act):
+    x, wg, wu, dh = f32_inputs(T, H, F, T + H)
+    want = ffn_bounds.expected(x, wg, wu, act, dh)
+    r = sf.sf_gated_ffn_grad(x, wg, wu, dh, act=act, want=("dx", "dw", "h"))
+    off = {n: ffn_bounds.share(getattr(r, n), want[n]) for n in want}
+    off["forward"] = ffn_bounds.share(sf.sf_gated_ffn(x, wg, wu, act=act), want["h"])
+    assert all(v <= 1 for v in off.values()), off
+
+
+@pytest.mark.parametrize("T", [1, 8, 20, 33, 300])
+def test_f32_sums_of_the_lower_parts(sf, T):
+    """h = relu(g) with g a sum whose upper parts cancel: of third parts of x, of third parts of the weights, and
+    of products of second parts.  256 terms of size 1 whose sums in f32 are off by 256 2^-24 = 2^-16 at most;
+    the sums are 2^-13 (128 2^-20) and 2^-11.1 (64 (2^-8.5)^2, 1.8 2^-9 each)."""
+    H, F = 264, 72
+    x, wg, wu = torch.zeros((T, H), device="cuda"), torch.zeros((F, H), device="cuda"), torch.zeros((F, H), device="cuda")
+    x[:, 256] = 1
+    wu[:, 256] = 1
+    low, near = 1 + 2.0 ** -8 + 2.0 ** -20, 1 + 2.0 ** -8
+    x[:, 0:256:2], x[:, 1:256:2] = low, near
+    wg[:, 0:256:2], wg[:, 1:256:2] = 1, -1
+    h = sf.sf_gated_ffn(x, wg, wu, act="relu")
+    assert bool(((h - 2.0 ** -13).abs() <= 2.0 ** -16).all())
+    x[:, 0:256:2], x[:, 1:256:2] = 1, -1
+    wg[:, 0:256:2], wg[:, 1:256:2] = low, near
+    h = sf.sf_gated_ffn(x, wg, wu, act="relu")
+    assert bool(((h - 2.0 ** -13).abs() <= 2.0 ** -16).all())
+    a = 1.8 * 2.0 ** -9
+    for k, (v, w) in enumerate(((1 + a, 1 + a), (1 + a, -1.0), (1.0, -1 - a), (1.0, 1.0))):
+        x[:, k:256:4], wg[:, k:256:4] = v, w
+    want = (x[0].double() * wg[0].double()).sum()
+    assert float(want) > 2.0 ** -11.2
+    h = sf.sf_gated_ffn(x, wg, wu, act="relu")
+    assert bool(((h.double() - want).abs() <= 2.0 ** -16).all())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("T", [1, 7, 40])
+def test_f32_tails(sf, T, act):
+    """g and u are single products, exact in every form; values in the normal range of f32."""
+    H, F = 64, 3001
+    g = torch.linspace(-8 if act == "gelu_tanh" else -12, 3, F, device="cuda")
+    x, dh = torch.zeros((T, H), device="cuda"), torch.zeros((T, F), device="cuda")
+    x[:, 0] = x[:, 1] = 1
+    dh[0] = 1
+    wg, wu = torch.zeros((F, H), device="cuda"), torch.zeros((F, H), device="cuda")
+    wg[:, 0], wu[:, 1] = g, -3.0
+    a, slope, size, own = ffn_bounds.act64(g.double(), act)
+    unit = ffn_bounds.UNIT
+    r = sf.sf_gated_ffn_grad(x, wg, wu, dh, act=act, want=("dw", "h"))
+    for got, want, near in ((sf.sf_gated_ffn(x, wg, wu, act=act)[T - 1], -3 * a, 3 * a.abs()), (r.h[T - 1], -3 * a, 3 * a.abs()),
+                            (r.dw_up[:, 1], a, a.abs()), (r.dw_gate[:, 0], -3 * slope, 3 * size)):
+        bound = (own + 2) * unit * near
+        off = (got.double() - want).abs()
+        assert bool((off <= bound).all()), (float((off / bound).max()), float(g[int((off / bound).nan_to_num().argmax())]))
