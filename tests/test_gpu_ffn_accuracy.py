@@ -139,3 +139,88 @@ def test_f32_tails(sf, T, act):
         bound = (own + 2) * unit * near
         off = (got.double() - want).abs()
         assert bool((off <= bound).all()), (float((off / bound).max()), float(g[int((off / bound).nan_to_num().argmax())]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("T", [601, 20011, 65537])
+def test_long_sums_of_one_sign(sf, T, dtype):
+    """Weights' gradients in f32 from 16-bit inputs, summed over many tokens: 16 products at a time, each sum cut off
+    by 2^-23 of it at most.  du is d itself (relu of 1), exact; the products are exact in f32."""
+    H, F, t = 64, 72, TYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    x = (1 + torch.randint(0, 128, (T, H), generator=gen, device="cuda") / 128).to(t)
+    x[:, 0] = 1
+    dh = (1 + torch.randint(0, 64, (T, F), generator=gen, device="cuda") / 64).to(t)
+    wg, wu = torch.zeros((F, H), dtype=t, device="cuda"), torch.zeros((F, H), dtype=t, device="cuda")
+    wg[:, 0] = wu[:, 0] = 1
+    r = sf.sf_gated_ffn_grad(x, wg, wu, dh, act="relu", want=("dw",), dw_dtype=torch.float32)
+    want = dh.double().t() @ x.double()
+    for got in (r.dw_gate, r.dw_up):
+        assert bool(((got.double() - want).abs() <= (T / 16 + 2) * 2.0 ** -23 * want).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("T", [601, 20011])
+def test_f32_weight_gradients_of_many_tokens(sf, T, dtype):
+    """Mixed signs, against dg and du rounded once to the type (half a step each, at random) and sums as above,
+    whose partial sums grow as the root of their length: 2/3 T / 16 2^-23 of the root of the squares' sum."""
+    H, F, t = 96, 136, TYPES[dtype]
+    x, wg, wu, dh = (v.to(t) for v in f32_inputs(T, H, F, T))
+    want = ffn_bounds.expected(x, wg, wu, "silu", dh)
+    g, u = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+    a, slope, _ = act64(g, "silu")
+    r = sf.sf_gated_ffn_grad(x, wg, wu, dh, want=("dw",), dw_dtype=torch.float32)
+    for name, got, q in (("dw_gate", r.dw_gate, dh.double() * u * slope), ("dw_up", r.dw_up, dh.double() * a)):
+        # own: f32 sums before the rounding, the hardware's exponential (2^-18), and what is below the type's numbers
+        size = ffn_bounds.squares(q.t(), x.double())
+        each = torch.finfo(t).eps / 2 + 2.0 ** -18 + T / 24 * 2.0 ** -23
+        least = TINY[dtype] * ffn_bounds.squares(torch.ones_like(q).t(), x.double())
+        bound = each * size + want[name][1] + least
+        assert ffn_bounds.share(got, (want[name][0], bound)) <= 1
+
+
+def test_f16_gradients_leave_the_range(sf):
+    """dg and du are f16 between the products: above 65504 infinite, below 2^-25 zero, also for weights in f32."""
+    T, H, F = 70, 64, 96
+    t = torch.float16
+    x, wg, wu = torch.zeros((T, H), dtype=t, device="cuda"), torch.zeros((F, H), dtype=t, device="cuda"), torch.zeros((F, H), dtype=t, device="cuda")
+    x[:, 0] = x[:, 1] = 1
+    wg[:, 0], wu[:, 1] = 2, 1000
+    dh = torch.zeros((T, F), dtype=t, device="cuda")
+    dh[0, :40], dh[0, 40:] = 100, 2.0 ** -14
+    wu[50:, 1] = 2.0 ** -13
+    for dt in (t, torch.float32):
+        r = sf.sf_gated_ffn_grad(x, wg, wu, dh, want=("dw",), dw_dtype=dt)
+        assert bool((r.dw_gate[:40, 0] == float("inf")).all()) and bool(r.dw_up[:40, 0].isfinite().all())
+        assert bool((r.dw_gate[40:50, 0] > 0).all()) and bool((r.dw_gate[50:, 0] == 0).all())
+        assert bool((r.dw_up[40:, 0] > 0).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,H", [(1, 16), (3, 9)])
+def test_many_features_of_few_tokens(sf, T, H, dtype):
+    """More features than the form for a few tokens takes: one row for each, its gradients against the formulas."""
+    F, t = 65535 * 8 + 9, TYPES[dtype]
+    x, wg, wu, dh = (v.to(t) for v in f32_inputs(T, H, F, T))
+    st = sf.new_status("cuda")
+    r = sf.sf_gated_ffn_grad(x, wg, wu, dh, want=("dx", "dw", "h"), status=st)
+    h = sf.sf_gated_ffn(x, wg, wu, status=st)
+    assert int(st.item()) == 0
+    want = ffn_bounds.expected(x, wg, wu, "silu", dh)
+    g, u = x.double() @ wg.double().t(), x.double() @ wu.double().t()
+    a, slope, _ = act64(g, "silu")
+    d = dh.double()
+    half = 0.0 if dtype == "f32" else torch.finfo(t).eps / 2
+    tiny = 0.0 if dtype == "f32" else TINY[dtype]
+    dg, du = d * u * slope, d * a
+    each = half + (0 if dtype == "f32" else 2.0 ** -18)  # dg and du as they are stored
+    through = {"dx": torch.hypot(ffn_bounds.squares(dg, wg.double()), ffn_bounds.squares(du, wu.double())),
+               "dw_gate": ffn_bounds.squares(dg.t(), x.double()), "dw_up": ffn_bounds.squares(du.t(), x.double())}
+    # sums of all features' products, 16 bits: 2 F / 16 steps of 2^-23 of partial sums that grow as the root of their length
+    steps = {"dx": 0.0 if dtype == "f32" else 2 * F / 24 * 2.0 ** -23}
+    for name, got in (("h", h), ("h", r.h), ("dx", r.dx), ("dw_gate", r.dw_gate), ("dw_up", r.dw_up)):
+        value, bound = want[name]
+        bound = bound + half * value.abs() + tiny * (1 + F ** 0.5)
+        if name in through:
+            bound = bound + (each + steps.get(name, 0.0)) * through[name]
+        assert ffn_bounds.share(got, (value, bound)) <= 1, name
