@@ -630,10 +630,14 @@ int32_t sf_grad_needs_workspace(const int64_t* numel, const int32_t* dtype, int6
  *             may be null where that is 0
  * Products are summed in f32 and h is rounded once.  bf16 and f16 go by the
  * tensor cores; rows of x or weights that do not all start on 16 bytes are
- * copied to the workspace first.  f32 goes by the tensor cores too, each value as
- * the exact sum of three bf16, with the error of f32 sums.  NaN and infinities go
- * where the formula takes them, but for f32 with more than a few tokens, where an
- * infinity may also make NaN.  T, H, F < 2^31, and T H, T F, F H < 2^40.
+ * copied to the workspace first.  The tensor cores cut their sums off instead of
+ * rounding them: a sum of 4096 products of one sign is low by 1.4e-5 of it, of 8192
+ * by 3.5e-5, where a rounding to bf16 or f16 is up to 3.9e-3 or 4.9e-4.  f32 goes by
+ * the tensor cores too, each value as the sum of three bf16 (exact for values of
+ * 2^-109 and more; what is below 2^-134 is lost), in runs of 256 products that are
+ * added in f32: with the error of f32 sums.  NaN and infinities go where the formula
+ * takes them, but for f32 with more than a few tokens, where an infinity may also
+ * make NaN.  T, H, F < 2^31, and T H, T F, F H < 2^40.
  */
 sf_status sf_gated_ffn(const void* x, int32_t dtype, int64_t T, int64_t H, int64_t ldx, const void* w_gate,
                        const void* w_up, int64_t F, int64_t ldw, int32_t act, void* h, int64_t ldh, void* workspace,
@@ -654,7 +658,9 @@ sf_status sf_gated_ffn(const void* x, int32_t dtype, int64_t T, int64_t H, int64
  *           micro-batches of a step), 0: they overwrite them
  *   workspace device, 16-byte aligned, sf_gated_ffn_workspace_size(...) bytes
  * At least one of dx, the weights' gradients and h.  dg and du are rounded once
- * to dtype between the products, as the tensor cores take them (f32: not rounded).  Outputs must
+ * to dtype between the products, as the tensor cores take them (f32: not rounded): in
+ * f16 they are infinite above 65504 and 0 below 2^-25, also for weights' gradients in
+ * f32.  These are summed in runs of 256 tokens that are added in f32.  Outputs must
  * not overlap inputs or one another.  Without tokens (T = 0) the weights'
  * gradients are 0, or stay as they are with accumulate.
  */

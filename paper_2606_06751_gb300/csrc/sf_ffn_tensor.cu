@@ -19,6 +19,13 @@ namespace {
 
 constexpr int kMaxStages = 12;
 
+// The tensor cores cut their f32 sums off instead of rounding them, 16 k at a time, by up to 2^-23
+// of the sum: 3.5e-5 of a sum of 8192 products of one sign, 3.7e-7 of 256 (measured).  That is
+// little against a result of 16 bits.  Weights' gradients in f32 are summed there in runs of kRun
+// blocks of 64 k, which are added up in registers: 3.8e-7 however long the sum.  8192 x 4096 x 12288
+// bf16: dW in f32 takes 1170 us so, in bf16 without runs 1100.
+constexpr int kRun = 4;
+
 struct Shape {
   int64_t m_tiles, n_tiles;  // dW: n tiles of one of the two matrices
   int N;                     // columns of D
@@ -76,9 +83,31 @@ __device__ __forceinline__ void multiply_block(uint32_t d, uint32_t a, uint32_t 
                           operand_of<L::kBAlongK>(b + k * kStepBytes<L::kBAlongK>), desc, !(first && k == 0));
 }
 
+// Adds 16 columns of every kStep to `sum`, while they are below `columns`.
+template <int kStep, int kChunks>
+__device__ __forceinline__ void add_columns(uint32_t at, int columns, float (&sum)[kChunks][16]) {
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    if (kStep * c >= columns) break;
+#pragma unroll
+    for (int h = 0; h < 16; h += 8) {
+      uint32_t v[8];
+      tensor_load8(at + kStep * c + h, v);
+      tensor_loaded();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[c][h + i] += __uint_as_float(v[i]);
+    }
+  }
+}
+
 // ---------------------------------------------------------------- large products: a pair of SMs a tile
 
-constexpr int kGroups = 3, kStoreWarps = 4 * kGroups, kPairThreads = 128 + 32 * kStoreWarps;
+constexpr int kGroups = 3;
+// Groups of store warps; with runs a warp's share of a tile's columns stays in its registers.
+template <bool kRuns>
+constexpr int kGroupsOf = kRuns ? 4 : kGroups;
+template <bool kRuns>
+constexpr int kPairThreads = 128 + 128 * kGroupsOf<kRuns>;
 constexpr int kSwapBytes = kGroups * 2 * 4 * 8 * 32 * 4;  // groups, parities, quadrants, columns, lanes
 
 // Persistent pairs of CTAs: each pair multiplies 256 rows by N columns, the sums of
@@ -87,10 +116,11 @@ constexpr int kSwapBytes = kGroups * 2 * 4 * 8 * 32 * 4;  // groups, parities, q
 // the tiles fill the SMs: forward 8192 x 4096 x 12288 bf16 902 us (1.83 PFLOP/s) in a
 // burst, 1015 at the power limit; else by the copies from L2 (32 KB of operands a pair's
 // SM and block of 64 k, at 48 bytes a clock) and by a launch's first and last tile.
-template <typename T, int kProduct>
-__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
+template <typename T, int kProduct, bool kRuns>
+__global__ void __launch_bounds__(kPairThreads<kRuns>, 1) __cluster_dims__(2, 1, 1)
     ffn_pair_kernel(const __grid_constant__ Maps maps, const FfnJob j, const Shape s) {
   using L = Layout<kProduct>;
+  constexpr int kStoreWarps = 4 * kGroupsOf<kRuns>;
   extern __shared__ unsigned char raw[];
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], sums_full[2], sums_empty[2];
   __shared__ uint32_t tensor_at;
@@ -102,6 +132,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
   const uint32_t stage_bytes = kABytes + uint32_t(half_n) * kDepthBytes;
   const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
   const int64_t pairs = gridDim.x / 2;
+  const int run = kRuns ? kRun : s.blocks;  // blocks that are summed at once
 
   if (tid == 0) {
     prefetch_maps(maps);
@@ -162,24 +193,26 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       uint32_t parity = 0;
       int64_t done = 0;
       bool ok = true;
-      for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += pairs, ++done) {
-        const int buf = static_cast<int>(done & 1);
-        ok = mbar_wait_bounded(&sums_empty[buf], uint32_t(done >> 1 & 1) ^ 1u, &abort);
-        if (!ok) break;
-        tensor_fence_after();
-        for (int kb = 0; kb < s.blocks; ++kb) {
-          ok = mbar_wait_bounded(&full[stage], parity, &abort);
+      for (int64_t tile = blockIdx.x / 2; ok && tile < tiles; tile += pairs) {
+        for (int kb0 = 0; ok && kb0 < s.blocks; kb0 += run, ++done) {
+          const int buf = static_cast<int>(done & 1), end = min(kb0 + run, s.blocks);
+          ok = mbar_wait_bounded(&sums_empty[buf], uint32_t(done >> 1 & 1) ^ 1u, &abort);
           if (!ok) break;
           tensor_fence_after();
-          const uint32_t a = smem_u32(base) + stage * stage_bytes;
-          multiply_block<kProduct, 2>(sums + buf * 256, a, a + kABytes, desc, kb == 0);
-          products_arrive<2>(&empty[stage]);
-          if (++stage == s.stages) {
-            stage = 0;
-            parity ^= 1;
+          for (int kb = kb0; kb < end; ++kb) {
+            ok = mbar_wait_bounded(&full[stage], parity, &abort);
+            if (!ok) break;
+            tensor_fence_after();
+            const uint32_t a = smem_u32(base) + stage * stage_bytes;
+            multiply_block<kProduct, 2>(sums + buf * 256, a, a + kABytes, desc, kb == kb0);
+            products_arrive<2>(&empty[stage]);
+            if (++stage == s.stages) {
+              stage = 0;
+              parity ^= 1;
+            }
           }
+          if (ok) products_arrive<2>(&sums_full[buf]);
         }
-        if (ok) products_arrive<2>(&sums_full[buf]);
       }
     }
   } else if (kProduct == kInner && warp == 3) {
@@ -205,6 +238,37 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
       // a warp that waits for every phase of a barrier has to hold back the one after next
       __syncwarp();
       if (lane == 0) arrive_at(at_rank(&sums_empty[done & 1], 0));
+    }
+  } else if (kRuns && warp >= 4) {
+    // as below, but a warp adds its columns of a tile's runs up first
+    const int q = warp & 3, group = (warp - 4) >> 2;
+    constexpr int kStep = 16 * kGroupsOf<kRuns>, kChunks = 256 / kStep;
+    int64_t done = 0;
+    for (int64_t tile = blockIdx.x / 2; tile < tiles; tile += pairs) {
+      int64_t m, n;
+      bool second;
+      tile_of<kProduct>(tile, s.m_tiles, s.n_tiles, s.N, m, n, second);
+      m += rank * L::kRows;
+      float sum[kChunks][16];
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[c][i] = 0.f;
+      for (int kb0 = 0; kb0 < s.blocks; kb0 += run, ++done) {
+        const int buf = static_cast<int>(done & 1);
+        // after a timeout garbage, and a status
+        if (!mbar_wait_bounded(&sums_full[buf], uint32_t(done >> 1 & 1), &abort, sums_limit(s)) && lane == 0)
+          report(j.status, SF_ST_TIMEOUT);
+        tensor_fence_after();
+        add_columns<kStep>(sums + buf * 256 + (uint32_t(q) << 21) + 16 * group, s.N - 16 * group, sum);
+        tensor_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_at(at_rank(&sums_empty[buf], 0));
+      }
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+        if (16 * group + kStep * c < s.N)
+          store_plain<T, kProduct>(j, second, m + 32 * q + lane, n + 16 * group + kStep * c, 1, 16, sum[c]);
     }
   } else if (warp >= 4) {
     // groups of four warps take chunks of 16 columns in turn; a warp reads the 32 lanes of its quadrant
@@ -288,13 +352,16 @@ __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
 // ---------------------------------------------------------------- small products: a tile a cluster, k split among its CTAs
 
 constexpr int kSplitThreads = 256;
+constexpr int kMostRunN = 128;  // columns of a tile that is summed in runs
 
 // Each CTA of a cluster sums its share of the blocks for the same 128 rows and N
 // columns; then CTA r adds up, in the CTAs' order, and stores a share of the columns.
 // Tensor memory is given back before the CTAs wait for one another.  Bound by the
 // weights' bytes for few tokens: 48 through 4096 x 12288 37 us (81 % of the copy rate),
 // through 2048 x 8192 15 us (10 are the bytes').
-template <typename T, int kProduct>
+// With runs every warp adds its columns of a run up before the next is multiplied; the next
+// run's first blocks are on their way by then.
+template <typename T, int kProduct, bool kRuns>
 __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_constant__ Maps maps, const FfnJob j,
                                                                   const Shape s) {
   using L = Layout<kProduct>;
@@ -333,75 +400,151 @@ __global__ void __launch_bounds__(kSplitThreads) ffn_split_kernel(const __grid_c
   griddep_launch_dependents();
   const uint32_t sums = tensor_at;
 
-  if (warp == 0) {
-    if (lane == 0) {
-      int stage = 0;
-      uint32_t parity = 1;
-      for (int kb = first; kb < last; ++kb) {
-        if (!mbar_wait_bounded(&empty[stage], parity, &abort)) break;
-        const uint32_t a = smem_u32(base) + stage * stage_bytes;
-        mbar_arrive_expect_tx(&full[stage], stage_bytes);
-        copy_block<kProduct, 1>(maps, s, kb, static_cast<int>(m), static_cast<int>(n), s.N, second, a, a + kABytes,
-                                smem_u32(&full[stage]));
-        if (++stage == s.stages) {
-          stage = 0;
-          parity ^= 1;
+  constexpr int kWarpStep = 32, kChunks = kRuns ? kMostRunN / kWarpStep : 1;  // of a warp's columns
+  float sum[kChunks][16];
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[c][i] = 0.f;
+  const int q = warp & 3;
+  const uint32_t mine = sums + (uint32_t(q) << 21) + 16 * (warp >> 2);
+  bool ok = true;
+  if constexpr (kRuns) {
+    const uint32_t desc = product_of(j.dtype == SF_BF16, L::kAAlongK, L::kBAlongK, 128, s.N);
+    int stage = 0, copied = first;
+    uint32_t parity = warp == 0 ? 1 : 0, sums_parity = 0;  // the copies wait for the phase before the first
+    for (int kb0 = first; kb0 < last; kb0 += kRun) {
+      const int end = min(kb0 + kRun, last);
+      if (warp == 0) {
+        if (lane == 0) {
+          for (const int ahead = min(last, end + s.stages); copied < ahead; ++copied) {
+            if (!mbar_wait_bounded(&empty[stage], parity, &abort)) break;
+            const uint32_t a = smem_u32(base) + stage * stage_bytes;
+            mbar_arrive_expect_tx(&full[stage], stage_bytes);
+            copy_block<kProduct, 1>(maps, s, copied, static_cast<int>(m), static_cast<int>(n), s.N, second, a, a + kABytes,
+                                    smem_u32(&full[stage]));
+            if (++stage == s.stages) {
+              stage = 0;
+              parity ^= 1;
+            }
+          }
         }
-      }
-      for (int i = 0; i < s.stages; ++i) {  // the last products' arrivals, before this CTA may end
-        if (!mbar_wait_bounded(&empty[stage], parity, &abort)) break;
-        if (++stage == s.stages) {
-          stage = 0;
-          parity ^= 1;
+        __syncwarp();
+      } else if (warp == 1) {
+        if (lane == 0) {
+          for (int kb = kb0; kb < end; ++kb) {
+            if (!mbar_wait_bounded(&full[stage], parity, &abort)) break;
+            tensor_fence_after();
+            const uint32_t a = smem_u32(base) + stage * stage_bytes;
+            multiply_block<kProduct, 1>(sums, a, a + kABytes, desc, kb == kb0);
+            products_arrive<1>(&empty[stage]);
+            if (++stage == s.stages) {
+              stage = 0;
+              parity ^= 1;
+            }
+          }
+          products_arrive<1>(&sums_full);
         }
+        __syncwarp();
       }
+      ok = mbar_wait_bounded(&sums_full, sums_parity, &abort, sums_limit(s)) && ok;
+      sums_parity ^= 1;
+      tensor_fence_after();
+      add_columns<kWarpStep>(mine, s.N - 16 * (warp >> 2), sum);
+      tensor_fence_before();
+      __syncthreads();  // before the next run's products
+      tensor_fence_after();
     }
-    __syncwarp();
-  } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t desc = product_of(j.dtype == SF_BF16, L::kAAlongK, L::kBAlongK, 128, s.N);
-      int stage = 0;
-      uint32_t parity = 0;
-      for (int kb = first; kb < last; ++kb) {
-        if (!mbar_wait_bounded(&full[stage], parity, &abort)) break;
-        tensor_fence_after();
-        const uint32_t a = smem_u32(base) + stage * stage_bytes;
-        multiply_block<kProduct, 1>(sums, a, a + kABytes, desc, kb == first);
-        products_arrive<1>(&empty[stage]);
-        if (++stage == s.stages) {
-          stage = 0;
-          parity ^= 1;
+    if (warp == 0) {
+      if (lane == 0) {
+        for (int i = 0; i < s.stages; ++i) {  // the last products' arrivals, before this CTA may end
+          if (!mbar_wait_bounded(&empty[stage], parity, &abort)) break;
+          if (++stage == s.stages) {
+            stage = 0;
+            parity ^= 1;
+          }
         }
       }
-      products_arrive<1>(&sums_full);
+      __syncwarp();
     }
-    __syncwarp();
+  } else {
+    if (warp == 0) {
+      if (lane == 0) {
+        int stage = 0;
+        uint32_t parity = 1;
+        for (int kb = first; kb < last; ++kb) {
+          if (!mbar_wait_bounded(&empty[stage], parity, &abort)) break;
+          const uint32_t a = smem_u32(base) + stage * stage_bytes;
+          mbar_arrive_expect_tx(&full[stage], stage_bytes);
+          copy_block<kProduct, 1>(maps, s, kb, static_cast<int>(m), static_cast<int>(n), s.N, second, a, a + kABytes,
+                                  smem_u32(&full[stage]));
+          if (++stage == s.stages) {
+            stage = 0;
+            parity ^= 1;
+          }
+        }
+        for (int i = 0; i < s.stages; ++i) {  // the last products' arrivals, before this CTA may end
+          if (!mbar_wait_bounded(&empty[stage], parity, &abort)) break;
+          if (++stage == s.stages) {
+            stage = 0;
+            parity ^= 1;
+          }
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      if (lane == 0) {
+        const uint32_t desc = product_of(j.dtype == SF_BF16, L::kAAlongK, L::kBAlongK, 128, s.N);
+        int stage = 0;
+        uint32_t parity = 0;
+        for (int kb = first; kb < last; ++kb) {
+          if (!mbar_wait_bounded(&full[stage], parity, &abort)) break;
+          tensor_fence_after();
+          const uint32_t a = smem_u32(base) + stage * stage_bytes;
+          multiply_block<kProduct, 1>(sums, a, a + kABytes, desc, kb == first);
+          products_arrive<1>(&empty[stage]);
+          if (++stage == s.stages) {
+            stage = 0;
+            parity ^= 1;
+          }
+        }
+        products_arrive<1>(&sums_full);
+      }
+      __syncwarp();
+    }
+    ok = mbar_wait_bounded(&sums_full, 0, &abort, sums_limit(s));
+    tensor_fence_after();
   }
-  const bool ok = mbar_wait_bounded(&sums_full, 0, &abort, sums_limit(s));
-  tensor_fence_after();
   if (!ok || *static_cast<volatile int*>(&abort)) {  // let copies in flight land
     if (tid == 0) report(j.status, SF_ST_TIMEOUT);
     const uint64_t t0 = global_timer_ns();
     while (global_timer_ns() - t0 < 2000000u) {
     }
   }
-  const int q = warp & 3;
-  const uint32_t mine = sums + (uint32_t(q) << 21);
   float* partial = reinterpret_cast<float*>(base);  // [column][128 rows], where the stages were
   const bool direct = !L::kGated && C == 1;         // nothing to add up or exchange
-  for (int c = 16 * (warp >> 2); c < s.N; c += 32) {
-    uint32_t v[16];
-    float x[16];
-    tensor_load16(mine + c, v);
-    tensor_loaded();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = last > first ? __uint_as_float(v[i]) : 0.f;
+  const auto put = [&](int c, const float (&x)[16]) {
     if constexpr (!L::kGated) {
       if (direct) store_plain<T, kProduct>(j, second, m + 32 * q + lane, n + c, 1, 16, x);
     }
     if (!direct) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) partial[(c + i) * 128 + 32 * q + lane] = x[i];
+    }
+  };
+  if constexpr (kRuns) {
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+      if (16 * (warp >> 2) + kWarpStep * c < s.N) put(16 * (warp >> 2) + kWarpStep * c, sum[c]);
+  } else {
+    for (int c = 0; c < s.N - 16 * (warp >> 2); c += kWarpStep) {
+      uint32_t v[16];
+      float x[16];
+      tensor_load16(mine + c, v);
+      tensor_loaded();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = last > first ? __uint_as_float(v[i]) : 0.f;
+      put(c + 16 * (warp >> 2), x);
     }
   }
   tensor_fence_before();
@@ -507,21 +650,21 @@ int64_t split_slots(int C, int per_sm) {
   return C == 8 ? (per_sm == 1 ? 120 : per_sm * 19 / 8 * 64) : per_sm * (C == 4 ? 144 : sm_count());
 }
 
-template <typename T, int kProduct>
+template <typename T, int kProduct, bool kRuns>
 cudaError_t launch_pairs(const FfnJob& j, Shape s, cudaStream_t stream) {
   Maps maps;
   if (!make_maps<kProduct>(maps, j, s.N / 2)) return cudaErrorUnknown;
   const size_t stage = kABytes + size_t(s.N / 2) * kDepthBytes, swap = Layout<kProduct>::kGated ? kSwapBytes : 0;
   s.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemMost - kSmemFixed - swap) / stage));
   const size_t smem = kSmemMost - kSmemBarriers;  // all, whatever the stages take: no other CTA on its SM
-  const auto kernel = ffn_pair_kernel<T, kProduct>;
+  const auto kernel = ffn_pair_kernel<T, kProduct, kRuns>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   const int64_t tiles = s.m_tiles * s.n_tiles * (kProduct == kDw ? 2 : 1);
   const unsigned grid = 2 * static_cast<unsigned>(std::min<int64_t>(tiles, sm_pairs()));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kPairThreads);
+  cfg.blockDim = dim3(kPairThreads<kRuns>);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -533,7 +676,7 @@ cudaError_t launch_pairs(const FfnJob& j, Shape s, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, kernel, maps, j, s);
 }
 
-template <typename T, int kProduct>
+template <typename T, int kProduct, bool kRuns>
 cudaError_t launch_split(const FfnJob& j, Shape s, int C, cudaStream_t stream) {
   Maps maps;
   if (!make_maps<kProduct>(maps, j, s.N)) return cudaErrorUnknown;
@@ -548,7 +691,7 @@ cudaError_t launch_split(const FfnJob& j, Shape s, int C, cudaStream_t stream) {
   int per_sm = 1;
   while (per_sm < most && split_slots(C, per_sm) < tiles * C) ++per_sm;
   if (per_sm < most) smem = std::max(smem, kSmemMost / per_sm - 2048);
-  const auto kernel = ffn_split_kernel<T, kProduct>;
+  const auto kernel = ffn_split_kernel<T, kProduct, kRuns>;
   // one limit for all sizes: calls from other threads set it too
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(kSmemMost - kSmemBarriers));
@@ -580,7 +723,7 @@ struct Choice {
 };
 double block_us(int rows_n) { return (kABytes + double(rows_n) * kDepthBytes) / 91200.0; }
 
-template <int kProduct>
+template <int kProduct, bool kRuns>
 Choice choose(int64_t M, int64_t Nall, int blocks, int64_t bytes) {
   using L = Layout<kProduct>;
   const int two = kProduct == kDw ? 2 : 1, sms = sm_count();
@@ -599,6 +742,7 @@ Choice choose(int64_t M, int64_t Nall, int blocks, int64_t bytes) {
       if (us < best.us) best = {true, N, static_cast<int>(n_tiles), 1, us};
     }
     const int N = width(kProduct == kDw ? 64 : 16);
+    if (kRuns && N > kMostRunN) continue;
     const int64_t n_tiles = ceil_div(Nall, N), tiles = ceil_div(M, L::kRows) * n_tiles * two;
     for (int C = 1; C <= 8 && (C == 1 || blocks >= 2 * C); C *= 2) {
       const int per_sm = split_per_sm(N, C, blocks);
@@ -617,7 +761,7 @@ Choice choose(int64_t M, int64_t Nall, int blocks, int64_t bytes) {
   return best;
 }
 
-template <typename T, int kProduct>
+template <typename T, int kProduct, bool kRuns = false>
 cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
   using L = Layout<kProduct>;
   const int64_t M = L::kGated ? j.F : j.H, Nall = kProduct == kDw ? j.F : j.T;
@@ -626,11 +770,12 @@ cudaError_t launch_product(const FfnJob& j, cudaStream_t stream) {
   s.half = static_cast<int>(ceil_div(k, kBox));
   s.blocks = kProduct == kDx ? 2 * s.half : s.half;
   const int64_t bytes = 2 * (j.T * j.H + 2 * j.F * j.H + (kProduct == kForward ? 1 : 2) * j.T * j.F);
-  const Choice c = choose<kProduct>(M, Nall, s.blocks, bytes);
+  const Choice c = choose<kProduct, kRuns>(M, Nall, s.blocks, bytes);
   s.N = c.N;
   s.n_tiles = c.n_tiles;
   s.m_tiles = ceil_div(M, c.pairs ? 2 * L::kRows : L::kRows);
-  return c.pairs ? launch_pairs<T, kProduct>(j, s, stream) : launch_split<T, kProduct>(j, s, c.C, stream);
+  return c.pairs ? launch_pairs<T, kProduct, kRuns>(j, s, stream)
+                 : launch_split<T, kProduct, kRuns>(j, s, c.C, stream);
 }
 
 template <typename T>
@@ -638,7 +783,9 @@ cudaError_t launch_type(const FfnJob& j, bool grad, cudaStream_t stream) {
   if (!grad) return launch_product<T, kForward>(j, stream);
   cudaError_t e = launch_product<T, kInner>(j, stream);
   if (e == cudaSuccess && j.dx != nullptr) e = launch_product<T, kDx>(j, stream);
-  if (e == cudaSuccess && j.dw_gate != nullptr) e = launch_product<T, kDw>(j, stream);
+  if (e == cudaSuccess && j.dw_gate != nullptr)
+    e = j.dw_dtype == SF_F32 && j.T > kRun * kBox ? launch_product<T, kDw, true>(j, stream)
+                                                  : launch_product<T, kDw>(j, stream);
   return e;
 }
 

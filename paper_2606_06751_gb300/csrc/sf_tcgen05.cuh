@@ -89,7 +89,13 @@ __device__ __forceinline__ void tensor_free(uint32_t at, uint32_t columns) {
 __device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// 16 columns of the warp's 32 lanes, in flight until tensor_loaded().
+// 8 or 16 columns of the warp's 32 lanes, in flight until tensor_loaded().
+__device__ __forceinline__ void tensor_load8(uint32_t at, uint32_t (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(at)
+               : "memory");
+}
 __device__ __forceinline__ void tensor_load16(uint32_t at, uint32_t (&v)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "

@@ -159,6 +159,28 @@ def test_long_sums_of_one_sign(sf, T, dtype):
         assert bool(((got.double() - want).abs() <= (T / 16 + 2) * 2.0 ** -23 * want).all())
 
 
+@pytest.mark.parametrize("T,H,F", [(257, 64, 72), (5003, 136, 200), (65537, 64, 72), (65537, 520, 1304), (300007, 72, 520)])
+def test_long_f32_sums_do_not_drift(sf, T, H, F):
+    """The same in runs of 256 tokens that are added in f32.  A run's partial sums are half of it on the average:
+    8 2^-23 of it, one more for its last step; the n runs' additions round by 2^-24 of a partial sum, evenly spread and
+    at random, a deviation of 2^-24 n^1/2 / 3: six of them are 2^-23 n^1/2.  Over all elements these cancel."""
+    t = torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(T + F)
+    x = (1 + torch.randint(0, 128, (T, H), generator=gen, device="cuda") / 128).to(t)
+    x[:, 0] = 1
+    dh = (1 + torch.randint(0, 64, (T, F), generator=gen, device="cuda") / 64).to(t)
+    wg, wu = torch.zeros((F, H), dtype=t, device="cuda"), torch.zeros((F, H), dtype=t, device="cuda")
+    wg[:, 0] = wu[:, 0] = 1
+    was = [torch.randn((F, H), generator=gen, device="cuda") for _ in range(2)]
+    r = sf.sf_gated_ffn_grad(x, wg, wu, dh, act="relu", want=("dw",), dw_dtype=torch.float32)
+    more = sf.sf_gated_ffn_grad(x, wg, wu, dh, act="relu", dw_gate=was[0].clone(), dw_up=was[1].clone(), accumulate=True, want=())
+    want = sum(dh[a:a + 16384].double().t() @ x[a:a + 16384].double() for a in range(0, T, 16384))
+    for got, again, before in ((r.dw_gate, more.dw_gate, was[0]), (r.dw_up, more.dw_up, was[1])):
+        off = (got.double() - want) / want
+        assert float(off.abs().max()) <= (9 + (T / 256) ** 0.5) * 2.0 ** -23 and abs(float(off.mean())) <= 10 * 2.0 ** -23
+        assert torch.equal(again, got + before)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("T", [601, 20011])
 def test_f32_weight_gradients_of_many_tokens(sf, T, dtype):
