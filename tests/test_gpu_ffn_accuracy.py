@@ -246,3 +246,23 @@ def test_many_features_of_few_tokens(sf, T, H, dtype):
         if name in through:
             bound = bound + (each + steps.get(name, 0.0)) * through[name]
         assert ffn_bounds.share(got, (value, bound)) <= 1, name
+
+
+@pytest.mark.parametrize("T", [8, 33, 300])
+def test_f32_small_values(sf, T):
+    """Values of 2^-109 keep all their bits in every form, as tokens, as weights and as gradients."""
+    H, F = 64, 136
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    small = (1 + torch.randint(0, 1 << 23, (T, F), generator=gen, device="cuda") * 2.0 ** -23) * 2.0 ** -109
+    x, wg, wu = torch.zeros((T, H), device="cuda"), torch.zeros((F, H), device="cuda"), torch.zeros((F, H), device="cuda")
+    x[:, 0], x[:, 1] = small[:, 0], 1
+    wg[:, 0], wu[:, 1] = 2.0 ** 100, 1
+    want = small[:, :1] * 2.0 ** 100
+    assert torch.equal(sf.sf_gated_ffn(x, wg, wu, act="relu"), want.expand(T, F))
+    x[:, 0], wg[:, 0] = 2.0 ** 100, small[0, 0]
+    assert torch.equal(sf.sf_gated_ffn(x, wg, wu, act="relu"), want[:1].expand(T, F))
+    x[:, 0], wg[:, 0] = 1, 1  # du = dh, dg = 0 (u is 0)
+    wu[:] = 0
+    x[:, 1] = torch.eye(T, device="cuda")[0] * 2.0 ** 100
+    r = sf.sf_gated_ffn_grad(x, wg, wu, small, act="relu")
+    assert torch.equal(r.dw_up[:, 1], small[0] * 2.0 ** 100)
