@@ -115,8 +115,10 @@ size_t value_size(int32_t dtype) { return dtype == SF_F32 ? 4 : 2; }
 size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 
 // Whether a call takes the form for a few tokens.  Products, us here against the tensor cores:
-//   f32          16 tokens through 2048 x 4096  32 / 57, 8 through 4096 x 12288  88 / 296, 64 through
-//                1024 x 4096  60 / 29; gradients have this form up to 8 tokens
+//   f32          512 x 2048: 16 tokens 6.5 / 16, 32 10.5 / 16, 48 14.6 / 16.4; 1024 x 4096: 16 18 / 31,
+//                24 24 / 31, 32 30.5 / 31.2, 48 43 / 31.5; 2048 x 8192: 16 55 / 91, 24 77 / 91, 32 96 / 91,
+//                48 142 / 94; 4096 x 12288: 12 144 / 306, 16 149 / 305, 24 208 / 305, 32 276 / 306, 48 402 / 307
+//   f32 gradient up to 8 tokens, as many as have the form: 24 / 34, 39 / 67, 126 / 177, 280 / 516
 //   16 bits      one token through 4096 x 12288  32.7 / 35.2, two 37.0 / 34.7; through 1024 x 2048
 //                one 3.7 / 5.4, four 4.4 / 5.4
 //   uneven rows  one token through 4097 x 12288  55 / 131 (with the copy of the weights), two 90 / 132

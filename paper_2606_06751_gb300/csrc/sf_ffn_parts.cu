@@ -1,6 +1,6 @@
 // sf_ffn_parts.cu - the gated feed-forward operators in f32 on the tensor cores.
 //
-// An f32 is a sum of three bf16 (a1 its upper half, a2 and a3 what is left), so that
+// An f32 of 2^-109 or more is the sum of three bf16 (a1 its upper half, a2 and a3 what is left), so that
 //   a b = a1 b1 + (a1 b2 + a2 b1) + (a2 b2 + a1 b3 + a3 b1)     to some 2^-24 of it,
 // six products of bf16 at 16 times the f32 units' rate or more.  The tensor cores
 // cut their f32 sums off instead of rounding them, by up to 2^-23 each time: a1 b1 and

@@ -54,7 +54,8 @@ __device__ __forceinline__ void store_down(T* p, int64_t ld, int step, int left,
 }
 
 // An f32 as a sum of three bf16: the upper half cut off (no overflow), then the rest's
-// nearest and its rest's.  Exact to 2^-25 of it; an infinity or NaN is the first part alone.
+// nearest and its rest's.  Exact for 2^-109 and more, where all of its bits are bf16 numbers; what is
+// below 2^-134 of a smaller one is lost.  An infinity or NaN is the first part alone.
 __device__ __forceinline__ void parts_of(float v, __nv_bfloat16 (&p)[3]) {
   const bool real = finite(v);
   const float a = real ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : v;
