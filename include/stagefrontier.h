@@ -631,8 +631,8 @@ int32_t sf_grad_needs_workspace(const int64_t* numel, const int32_t* dtype, int6
  * Products are summed in f32 and h is rounded once.  bf16 and f16 go by the
  * tensor cores; rows of x or weights that do not all start on 16 bytes are
  * copied to the workspace first.  The tensor cores cut their sums off instead of
- * rounding them: a sum of 4096 products of one sign is low by 1.4e-5 of it, of 8192
- * by 3.5e-5, where a rounding to bf16 or f16 is up to 3.9e-3 or 4.9e-4.  f32 goes by
+ * rounding them: a sum of 4096 products of one sign is low by up to 1.4e-5 of it, of
+ * 8192 by 3.5e-5, where a rounding to bf16 or f16 is up to 3.9e-3 or 4.9e-4.  f32 goes by
  * the tensor cores too, each value as the sum of three bf16 (exact for values of
  * 2^-109 and more; what is below 2^-134 is lost), in runs of 256 products that are
  * added in f32: with the error of f32 sums.  NaN and infinities go where the formula

@@ -144,3 +144,39 @@ def test_two_streams_at_once(sf, dtype):
         torch.cuda.synchronize()
         for r, w in ((a, want[0]), (b, want[1]), (c, want[0])):
             assert all(torch.equal(getattr(r, n), t) for n, t in zip(names, w))
+
+
+def test_captured_on_a_forked_stream(sf):
+    """A graph whose work goes to a second stream and back: its memory is the graph's, replay after replay, whatever
+    other calls allocate in between."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    n = lambda *s, k=1.0: (torch.randn(s, generator=g, device="cuda") * k).bfloat16()  # noqa: E731
+    x, wg, wu, dh = n(700, 264), n(520, 264, k=0.06), n(520, 264, k=0.06), n(700, 520)
+    key = torch.tensor([3, 4], device="cuda")
+    names = ("dx", "dw_gate", "dw_up", "h")
+
+    def work(stream=None):
+        y = sf.sf_dropout(x, 0.25, key, stream=stream)
+        r = sf.sf_gated_ffn_grad(x, wg, wu, dh, want=("dx", "dw", "h"), stream=stream)
+        return [y] + [getattr(r, k) for k in names]
+
+    work()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        out = work(side)
+        here.wait_stream(side)
+        twice = [t * 2 for t in out]
+    for k in range(3):
+        x.copy_(n(700, 264))
+        want = [t.clone() for t in work()]
+        work(side)
+        torch.cuda.synchronize()
+        graph.replay()
+        work(side)  # beside the graph
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert all(torch.equal(a, b * 2) for a, b in zip(twice, want))
